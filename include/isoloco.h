@@ -59,8 +59,9 @@ typedef struct {
     int32_t cols;
 } isoloco_param_t;
 
-/* Element type of the worker replicas (bf16 is upcast exactly to fp32). */
-typedef enum { ISOLOCO_F32 = 0, ISOLOCO_BF16 = 1 } isoloco_dtype_t;
+/* Element type of the worker replicas (bf16 is upcast exactly to fp32; a plan takes the first two)
+ * and of the inner step's operands. */
+typedef enum { ISOLOCO_F32 = 0, ISOLOCO_BF16 = 1, ISOLOCO_F16 = 2 } isoloco_dtype_t;
 
 typedef enum {
     ISOLOCO_OK = 0,
@@ -350,6 +351,116 @@ int isoloco_profile_read(isoloco_plan_t plan, void* stream, double* ms_host, int
 
 /* Kernels launched by the plan since its creation. */
 int64_t isoloco_plan_launches(isoloco_plan_t plan);
+
+/* ---------------------------------------------------------------------------------------------
+ * Operators of a worker's inner step: what a replica computes between two outer steps, and how a
+ * merged model is scored.  They need no plan.  Conventions:
+ * - Matrices are row-major with a row pitch `ld_*` in elements (>= the row's length); rows are
+ *   contiguous.  Data pointers need their element's alignment only; workspaces 16 bytes.  Sizes that
+ *   allow 16-byte accesses (pitches and addresses multiples of 16 bytes) run faster.
+ * - Inputs are read and outputs written in their own type (F32, BF16 or F16); every sum, softmax
+ *   statistic and norm is held in 32 bits or more, and an output is rounded once.
+ * - A workspace of at least the bytes the *_workspace function gives is the caller's, used by one
+ *   call at a time; it needs no initialisation and holds nothing between calls.
+ * - Calls enqueue work on `stream` and return.  Arguments are checked before anything is launched.
+ *   Outputs may not overlap inputs unless an entry point says so.
+ * - A token id or target outside [0, vocab) is no token: see each entry point.
+ * - Results do not depend on the order in which a GPU runs its blocks: same inputs (at addresses that
+ *   are equal modulo 16), same bits.
+ */
+
+/* Activations of the gated block: x sigmoid(x), and
+ * x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))). */
+typedef enum { ISOLOCO_SILU = 0, ISOLOCO_GELU_TANH = 1 } isoloco_act_t;
+
+/* Embedding lookup: y[t][:] = scale * weight[ids[t]][:], zeros where ids[t] is no token.
+ *   weight: vocab x width; y: tokens x width; both of `dtype`.  ids: tokens entries of
+ *   id_bytes (4 or 8) bytes, signed.  Sizes may be 0 (tokens) and up to 2^31 - 1. */
+int isoloco_embed(const void* weight, int64_t ld_weight, isoloco_dtype_t dtype, int64_t vocab, int64_t width,
+                  const void* ids, int id_bytes, int64_t tokens, float scale, void* y, int64_t ld_y, void* stream);
+
+/* The lookup's gradient: dw[v][:] = scale * sum over t with ids[t] == v of dy[t][:], every row of
+ * dw written (zeros for tokens that do not occur).  The tokens are sorted by id, and a row's terms
+ * are added in fp32 in an order that depends on the ids alone.
+ *   dy: tokens x width of `dtype`; dw: vocab x width of dw_dtype (`dtype` or F32). */
+int64_t isoloco_embed_grad_workspace(int64_t vocab, int64_t width, int64_t tokens);
+int isoloco_embed_grad(const void* dy, int64_t ld_dy, isoloco_dtype_t dtype, int64_t vocab, int64_t width,
+                       const void* ids, int id_bytes, int64_t tokens, float scale, void* dw, int64_t ld_dw,
+                       isoloco_dtype_t dw_dtype, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Gated feed-forward block: h = act(x w_gate) * (x w_up).
+ *   x: tokens x width; w_gate, w_up: width x ff (pitch ld_w, the layout of the parameter table's
+ *   matrices); h: tokens x ff.  dtype BF16 or F16 for all.
+ *   saved: NULL, or isoloco_gated_ffn_saved_bytes() bytes, 16-byte aligned, that receive x w_gate and
+ *   x w_up, rounded to `dtype` (finite), for isoloco_gated_ffn_grad. */
+int64_t isoloco_gated_ffn_saved_bytes(int64_t tokens, int64_t ff);
+int64_t isoloco_gated_ffn_workspace(int64_t tokens, int64_t width, int64_t ff);
+int isoloco_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w,
+                      isoloco_dtype_t dtype, int64_t tokens, int64_t width, int64_t ff, isoloco_act_t act, void* h,
+                      int64_t ld_h, void* saved, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Its gradient for dh (tokens x ff): with g = x w_gate, u = x w_up as saved,
+ *   dg = dh u act'(g), du = dh act(g), each rounded to `dtype`;
+ *   dx = dg w_gate^T + du w_up^T, dw_gate = x^T dg, dw_up = x^T du.
+ *   dx (pitch ld_dx) may be NULL; dw_gate and dw_up (pitch ld_dw) may be NULL together. */
+int64_t isoloco_gated_ffn_grad_workspace(int64_t tokens, int64_t width, int64_t ff);
+int isoloco_gated_ffn_grad(const void* dh, int64_t ld_dh, const void* x, int64_t ld_x, const void* w_gate,
+                           const void* w_up, int64_t ld_w, isoloco_dtype_t dtype, int64_t tokens, int64_t width,
+                           int64_t ff, isoloco_act_t act, const void* saved, void* dx, int64_t ld_dx, void* dw_gate,
+                           void* dw_up, int64_t ld_dw, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Log probabilities of given tokens.  With z = scale * logits (scale > 0: an inverse temperature),
+ * p = softmax(z) of a row:
+ *   lse = log sum_j e^{z_j};  logp = z_t - lse for the row's target t (0 if it is no token);
+ *   entropy = -sum_j p_j log p_j;  the `top` largest logits' log probabilities and indices, largest
+ *   first, the lowest index first among equals (0 <= top <= min(vocab, ISOLOCO_MAX_TOP)).
+ * Logits of -inf or the type's lowest value have probability 0.  In a row of -inf alone, lse and the
+ * log probabilities are -inf, the entropy and the gradient 0.  A NaN or +inf makes a row's
+ * statistics (and gradient) NaN; its alternatives are then some indices inside the row.
+ *   logits: rows x vocab of `dtype`; targets: rows entries of target_bytes (4 or 8), signed;
+ *   logp, entropy, lse (each may be NULL): rows fp32; top_logp fp32, top_index int64: rows x top.
+ * With grad_logits (rows x vocab of `dtype`, pitch ld_grad; may be the logits themselves, else NULL),
+ * the call also writes the gradient of sum_r grad_logp[r] logp[r] + grad_entropy[r] entropy[r]
+ * (fp32, either may be NULL for none) by the logits:
+ *   scale * (grad_logp (1[j = t] - p_j) - grad_entropy p_j (log p_j + entropy)). */
+#define ISOLOCO_MAX_TOP 32
+int64_t isoloco_token_logprobs_workspace(int64_t rows, int64_t vocab, int top);
+int isoloco_token_logprobs(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows, int64_t vocab,
+                           const void* targets, int target_bytes, float scale, float* logp, float* entropy, float* lse,
+                           int top, float* top_logp, int64_t* top_index, const float* grad_logp,
+                           const float* grad_entropy, void* grad_logits, int64_t ld_grad, void* workspace,
+                           int64_t workspace_bytes, void* stream);
+
+/* The same gradient by itself, from the lse and entropy of an earlier call on the same logits. */
+int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows,
+                                int64_t vocab, const void* targets, int target_bytes, float scale, const float* lse,
+                                const float* entropy, const float* grad_logp, const float* grad_entropy,
+                                void* grad_logits, int64_t ld_grad, void* stream);
+
+/* One tensor of a gradient: n contiguous elements, n up to 2^33. */
+typedef struct {
+    void* data;
+    int64_t n;
+    int32_t dtype; /* isoloco_dtype_t */
+} isoloco_tensor_t;
+
+/* The gradient's global norm, sqrt(sum over all tensors and entries of g^2), to norm[0] (device
+ * fp32).  Squares are taken in fp32: entries beyond 1.8e19 in magnitude give inf.
+ *   tensors: HOST array of `count` entries, read during the call. */
+int64_t isoloco_grad_norm_workspace(int count);
+int isoloco_grad_norm(const isoloco_tensor_t* tensors, int count, float* norm, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
+/* The norm, and the gradient times min(1, max_norm / norm).  outs: NULL to scale in place, or a HOST
+ * array of `count` entries of the same lengths and types that receive the result (an entry may name its
+ * input's own data).  A NaN or infinite norm scales nothing (the caller sees it in norm[0]). */
+int isoloco_clip_grads(const isoloco_tensor_t* tensors, const isoloco_tensor_t* outs, int count, float max_norm,
+                       float* norm, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Synchronizes `stream` and returns the device status of the inner step's operators on the current
+ * device since the last such call: OK, or TIMEOUT when a kernel's wait gave up (its outputs are
+ * then undefined). */
+int isoloco_inner_status(void* stream);
 
 /* Thread-local message describing the last error returned on this thread. */
 const char* isoloco_last_error(void);

@@ -6,12 +6,14 @@ replicas resident in HBM, a K-way pseudo-gradient reduction, Iso-C on every
 cores, and a fused Nesterov update.  The compute runs in the hand-written CUDA
 library ``libisoloco`` behind the C ABI declared in ``include/isoloco.h``;
 ``paper_2607_03011_gb300.isoloco`` is the thin Python binding over it.
+``paper_2607_03011_gb300.inner`` binds the operators a worker's replica runs between
+two outer steps, and a merged model is scored with.
 
 Importing this package loads nothing; the CUDA library is opened on first use
 and its absence is an error (there is no CPU fallback).
 """
 
-__all__ = ["isoloco", "workloads"]
+__all__ = ["inner", "isoloco", "workloads"]
 
 
 def __getattr__(name):

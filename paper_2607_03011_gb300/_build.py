@@ -19,7 +19,7 @@ LIB = os.path.join(BUILD, "libisoloco.so")
 INCLUDE = os.path.join(ROOT, "include")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["api.cu", "gemm.cu", "polar.cu", "stream.cu", "spectral.cu", "svd.cu", "gramside.cu",
-           "polar_loop.cu"]
+           "polar_loop.cu", "inner_api.cu", "embed.cu", "ffn.cu", "logprob.cu", "clip.cu"]
 
 
 def _nvcc() -> str:

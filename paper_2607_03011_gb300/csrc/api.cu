@@ -22,6 +22,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "inner.h"
 #include "isoloco.h"
 #include "per_device.h"
 #include "polar_loop.h"
@@ -289,6 +290,8 @@ static int fail(int code, const std::string& msg) {
     g_last_error = msg;
     return code;
 }
+
+int isoloco::set_error(int code, const char* msg) { return fail(code, msg); }
 
 #define CUDA_TRY(expr)                                                                        \
     do {                                                                                      \

@@ -1,0 +1,230 @@
+// clip.cu -- the global norm of a gradient held in many tensors, and clipping by it.
+//
+//     n = sqrt(sum over all tensors and entries of g^2),   g' = g min(1, max_norm / n)
+//
+// Two launches whatever the number of tensors (up to kMaxTensors per table): the table of addresses
+// and lengths travels in the kernel's parameters, so no copy to the device precedes the call.  The
+// first sums squares over fixed chunks (fp32 within a thread, fp64 from there on) and leaves one
+// fp64 partial per CTA; the second adds the partials, every CTA in the same order, so that all have
+// the same bits, and scales.
+#include <algorithm>
+#include <cmath>
+
+#include "inner.cuh"
+#include "inner.h"
+
+namespace isoloco {
+
+namespace {
+
+constexpr int kClipThreads = 256;
+constexpr int kMaxTensors = 512;       // of one table: 512 x 32 bytes of kernel parameters
+constexpr int kChunkBytes = 32768;     // a CTA's unit of work: 8 16-byte loads per thread
+constexpr int kCtasPerSm = 8;
+
+struct ClipTensor {
+    const void* in;
+    void* out;
+    int64_t n;
+    int32_t dtype;
+    int32_t first;  // chunk number of its first chunk
+};
+
+struct ClipTable {
+    ClipTensor t[kMaxTensors];
+    int count;
+    int chunks;
+};
+
+// The chunk's elements [lo, hi) of tensor `t` and the first of them at a 16-byte address.  Chunk 0
+// also holds the elements before the tensor's first 16-byte boundary.
+struct ChunkSpan {
+    int64_t lo, mid, hi;
+};
+
+template <class T>
+__device__ __forceinline__ ChunkSpan chunk_span(const ClipTensor& t, int c) {
+    constexpr int kElems = kChunkBytes / static_cast<int>(sizeof(T));
+    const uint32_t mis = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(t.in) & 15u);
+    const int64_t head = mis ? (16 - mis) / sizeof(T) : 0;
+    ChunkSpan s;
+    s.lo = c ? head + static_cast<int64_t>(c) * kElems : 0;
+    s.mid = min(t.n, head + static_cast<int64_t>(c) * kElems);
+    s.hi = min(t.n, head + static_cast<int64_t>(c + 1) * kElems);
+    return s;
+}
+
+__device__ __forceinline__ int find_tensor(const ClipTable& tab, int chunk) {
+    int lo = 0, hi = tab.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (tab.t[mid].first <= chunk) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+template <class T>
+__device__ __forceinline__ float chunk_squares(const ClipTensor& t, int c) {
+    const ChunkSpan s = chunk_span<T>(t, c);
+    const T* p = static_cast<const T*>(t.in);
+    constexpr int V = Vec<T>::kN;
+    float acc = 0.f;
+    for (int64_t i = s.lo + threadIdx.x; i < s.mid; i += kClipThreads) {
+        const float v = to_f32(p[i]);
+        acc += v * v;
+    }
+    const int64_t nvec = (s.hi - s.mid) / V;
+    const T* q = p + s.mid;
+#pragma unroll 8
+    for (int64_t i = threadIdx.x; i < nvec; i += kClipThreads) {
+        Vec<T> v;
+        v.raw = __ldg(reinterpret_cast<const uint4*>(q + i * V));
+        float f[V];
+        v.unpack(f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc += f[j] * f[j];
+    }
+    for (int64_t i = s.mid + nvec * V + threadIdx.x; i < s.hi; i += kClipThreads) {
+        const float v = to_f32(p[i]);
+        acc += v * v;
+    }
+    return acc;
+}
+
+template <class T>
+__device__ __forceinline__ void chunk_scale(const ClipTensor& t, int c, float coef) {
+    const ChunkSpan s = chunk_span<T>(t, c);
+    const T* p = static_cast<const T*>(t.in);
+    T* o = static_cast<T*>(t.out);
+    constexpr int V = Vec<T>::kN;
+    const bool vec = ((reinterpret_cast<uintptr_t>(t.in) ^ reinterpret_cast<uintptr_t>(t.out)) & 15u) == 0;
+    const int64_t nvec = vec ? (s.hi - s.mid) / V : 0;
+    for (int64_t i = s.lo + threadIdx.x; i < s.mid; i += kClipThreads) o[i] = coef == 1.f ? p[i] : from_f32<T>(to_f32(p[i]) * coef);
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < nvec; i += kClipThreads) {
+        Vec<T> v;
+        v.raw = ld_stream(p + s.mid + i * V);
+        if (coef != 1.f) {  // (a copy keeps every bit, a NaN's too)
+            float f[V];
+            v.unpack(f);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[j] *= coef;
+            v.pack(f);
+        }
+        st_stream(o + s.mid + i * V, v.raw);
+    }
+    for (int64_t i = s.mid + nvec * V + threadIdx.x; i < s.hi; i += kClipThreads) o[i] = coef == 1.f ? p[i] : from_f32<T>(to_f32(p[i]) * coef);
+}
+
+// Sum over the CTA; every thread gets it.
+__device__ __forceinline__ double cta_sum(double v) {
+    __shared__ double part[kClipThreads / 32];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < kClipThreads / 32; ++i) s += part[i];
+    return s;
+}
+
+__global__ void __launch_bounds__(kClipThreads) k_grad_squares(const __grid_constant__ ClipTable tab, double* part) {
+    double acc = 0.0;
+    for (int c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
+        const ClipTensor& t = tab.t[find_tensor(tab, c)];
+        const int k = c - t.first;
+        const float s = t.dtype == ISOLOCO_F32 ? chunk_squares<float>(t, k)
+                        : t.dtype == ISOLOCO_BF16 ? chunk_squares<__nv_bfloat16>(t, k) : chunk_squares<__half>(t, k);
+        acc += static_cast<double>(s);
+    }
+    const double s = cta_sum(acc);
+    if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+// tab.chunks == 0: the norm only.
+__global__ void __launch_bounds__(kClipThreads) k_grad_scale(const __grid_constant__ ClipTable tab, const double* part,
+                                                             int nparts, float max_norm, bool in_place, float* norm) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < nparts; i += kClipThreads) s += part[i];
+    const float n = static_cast<float>(sqrt(cta_sum(s)));
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = n;
+    // a norm that is not finite, or zero, scales nothing
+    const float coef = (n > max_norm && n < INFINITY) ? max_norm / n : 1.f;
+    if (in_place && coef == 1.f) return;
+    // from the last chunk down: what the first pass read last is still in L2
+    for (int c = tab.chunks - 1 - static_cast<int>(blockIdx.x); c >= 0; c -= gridDim.x) {
+        const ClipTensor& t = tab.t[find_tensor(tab, c)];
+        const int k = c - t.first;
+        if (t.dtype == ISOLOCO_F32) chunk_scale<float>(t, k, coef);
+        else if (t.dtype == ISOLOCO_BF16) chunk_scale<__nv_bfloat16>(t, k, coef);
+        else chunk_scale<__half>(t, k, coef);
+    }
+}
+
+int chunks_of(const isoloco_tensor_t& t) {
+    const int es = t.dtype == ISOLOCO_F32 ? 4 : 2;
+    const uint32_t mis = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(t.data) & 15u);
+    const int64_t head = mis ? (16 - mis) / es : 0;
+    const int64_t body = std::max<int64_t>(0, t.n - head), per = kChunkBytes / es;
+    return static_cast<int>(std::max<int64_t>(1, (body + per - 1) / per));
+}
+
+}  // namespace
+
+// One table per kMaxTensors tensors, at most kCtasPerSm partials per SM each.
+int64_t grad_norm_workspace(int count) {
+    const int64_t tables = count > 0 ? (count + kMaxTensors - 1) / kMaxTensors : 1;
+    return tables * 1024 * kCtasPerSm * static_cast<int64_t>(sizeof(double));
+}
+
+cudaError_t launch_clip(const isoloco_tensor_t* in, const isoloco_tensor_t* out, int count, bool clip, float max_norm,
+                        float* norm, void* ws, cudaStream_t st) {
+    int sms = 0;
+    cudaError_t e = device_sms(&sms);
+    if (e != cudaSuccess) return e;
+    double* part = static_cast<double*>(ws);
+    int nparts = 0;
+    const int max_grid = std::min(1024, sms) * kCtasPerSm;
+    // pass 0 the squares, pass 1 the scaling
+    for (int pass = 0; pass < (clip ? 2 : 1); ++pass) {
+        for (int first = 0; first < count;) {
+            ClipTable tab;
+            tab.count = 0;
+            tab.chunks = 0;
+            int i = first;
+            for (; i < count && tab.count < kMaxTensors; ++i) {
+                if (in[i].n == 0) continue;
+                const int c = chunks_of(in[i]);
+                ClipTensor& t = tab.t[tab.count++];
+                t.in = in[i].data;
+                t.out = out ? out[i].data : in[i].data;
+                t.n = in[i].n;
+                t.dtype = in[i].dtype;
+                t.first = tab.chunks;
+                tab.chunks += c;
+            }
+            first = i;
+            if (!tab.count) continue;
+            const int grid = std::min(tab.chunks, max_grid);
+            if (pass == 0) {
+                k_grad_squares<<<grid, kClipThreads, 0, st>>>(tab, part + nparts);
+                nparts += grid;
+            } else {
+                k_grad_scale<<<grid, kClipThreads, 0, st>>>(tab, part, nparts, max_norm, out == nullptr, norm);
+            }
+            if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        }
+    }
+    if (!clip || nparts == 0) {
+        ClipTable none;
+        none.count = none.chunks = 0;
+        k_grad_scale<<<1, kClipThreads, 0, st>>>(none, part, nparts, 0.f, true, norm);
+        e = cudaGetLastError();
+    }
+    return e;
+}
+
+}  // namespace isoloco

@@ -43,6 +43,10 @@ class Param(ctypes.Structure):
     _fields_ = [("offset", ctypes.c_int64), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32)]
 
 
+class Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
 class Opts(ctypes.Structure):
     _fields_ = [("alpha", ctypes.c_float), ("outer_lr", ctypes.c_float), ("momentum", ctypes.c_float),
                 ("reduce_mean", ctypes.c_int), ("max_iter", ctypes.c_int), ("tol", ctypes.c_float),
@@ -91,6 +95,25 @@ def lib():
                                              ctypes.c_int, ctypes.c_int, _vp, _vp, _vp, _vp]
             L.isoloco_debug_gemm_noalloc.argtypes = L.isoloco_debug_gemm.argtypes
             L.isoloco_debug_wait_timeout.argtypes = [ctypes.c_int64, ctypes.POINTER(ctypes.c_int64), _vp]
+            i64, ci, cf = ctypes.c_int64, ctypes.c_int, ctypes.c_float
+            L.isoloco_embed.argtypes = [_vp, i64, ci, i64, i64, _vp, ci, i64, cf, _vp, i64, _vp]
+            L.isoloco_embed_grad.argtypes = [_vp, i64, ci, i64, i64, _vp, ci, i64, cf, _vp, i64, ci, _vp, i64, _vp]
+            L.isoloco_gated_ffn.argtypes = [_vp, i64, _vp, _vp, i64, ci, i64, i64, i64, ci, _vp, i64, _vp, _vp, i64, _vp]
+            L.isoloco_gated_ffn_grad.argtypes = [_vp, i64, _vp, i64, _vp, _vp, i64, ci, i64, i64, i64, ci, _vp, _vp, i64,
+                                                 _vp, _vp, i64, _vp, i64, _vp]
+            L.isoloco_token_logprobs.argtypes = [_vp, i64, ci, i64, i64, _vp, ci, cf, _vp, _vp, _vp, ci, _vp, _vp, _vp,
+                                                 _vp, _vp, i64, _vp, i64, _vp]
+            L.isoloco_token_logprobs_grad.argtypes = [_vp, i64, ci, i64, i64, _vp, ci, cf, _vp, _vp, _vp, _vp, _vp, i64,
+                                                      _vp]
+            L.isoloco_grad_norm.argtypes = [ctypes.POINTER(Tensor), ci, _vp, _vp, i64, _vp]
+            L.isoloco_clip_grads.argtypes = [ctypes.POINTER(Tensor), ctypes.POINTER(Tensor), ci, cf, _vp, _vp, i64, _vp]
+            L.isoloco_inner_status.argtypes = [_vp]
+            for f in (L.isoloco_embed_grad_workspace, L.isoloco_gated_ffn_workspace, L.isoloco_gated_ffn_grad_workspace):
+                f.argtypes, f.restype = [i64, i64, i64], i64
+            L.isoloco_gated_ffn_saved_bytes.argtypes, L.isoloco_gated_ffn_saved_bytes.restype = [i64, i64], i64
+            L.isoloco_token_logprobs_workspace.argtypes = [i64, i64, ci]
+            L.isoloco_token_logprobs_workspace.restype = i64
+            L.isoloco_grad_norm_workspace.argtypes, L.isoloco_grad_norm_workspace.restype = [ci], i64
             _lib = L
     return _lib
 
