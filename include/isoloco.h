@@ -392,18 +392,22 @@ int isoloco_embed_grad(const void* dy, int64_t ld_dy, isoloco_dtype_t dtype, int
  *   x: tokens x width; w_gate, w_up: width x ff (pitch ld_w, the layout of the parameter table's
  *   matrices); h: tokens x ff.  dtype BF16 or F16 for all.
  *   saved: NULL, or isoloco_gated_ffn_saved_bytes() bytes, 16-byte aligned, that receive x w_gate and
- *   x w_up, rounded to `dtype` (finite), for isoloco_gated_ffn_grad. */
-int64_t isoloco_gated_ffn_saved_bytes(int64_t tokens, int64_t ff);
-int64_t isoloco_gated_ffn_workspace(int64_t tokens, int64_t width, int64_t ff);
+ *   x w_up for isoloco_gated_ffn_grad: in fp32 for F16, in 16 bits (10 of them significant, magnitudes
+ *   to 2^33, larger ones cut off there) for BF16.
+ *   Workspace: aligned = 1 when the addresses and pitches of all matrices (without dh) are multiples of
+ *   16 bytes, which needs little; 0 any others, which are copied to and from rows that are.
+ *   tokens up to 2^30, width and ff up to 2^20. */
+int64_t isoloco_gated_ffn_saved_bytes(int64_t tokens, int64_t ff, isoloco_dtype_t dtype);
+int64_t isoloco_gated_ffn_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned);
 int isoloco_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w,
                       isoloco_dtype_t dtype, int64_t tokens, int64_t width, int64_t ff, isoloco_act_t act, void* h,
                       int64_t ld_h, void* saved, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Its gradient for dh (tokens x ff): with g = x w_gate, u = x w_up as saved,
- *   dg = dh u act'(g), du = dh act(g), each rounded to `dtype`;
+ *   dg = dh u act'(g), du = dh act(g), each rounded to `dtype` (operands of the tensor cores);
  *   dx = dg w_gate^T + du w_up^T, dw_gate = x^T dg, dw_up = x^T du.
  *   dx (pitch ld_dx) may be NULL; dw_gate and dw_up (pitch ld_dw) may be NULL together. */
-int64_t isoloco_gated_ffn_grad_workspace(int64_t tokens, int64_t width, int64_t ff);
+int64_t isoloco_gated_ffn_grad_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned);
 int isoloco_gated_ffn_grad(const void* dh, int64_t ld_dh, const void* x, int64_t ld_x, const void* w_gate,
                            const void* w_up, int64_t ld_w, isoloco_dtype_t dtype, int64_t tokens, int64_t width,
                            int64_t ff, isoloco_act_t act, const void* saved, void* dx, int64_t ld_dx, void* dw_gate,

@@ -1,154 +1,954 @@
-// ffn.cu -- gated feed-forward block, h = act(x Wg) * (x Wu), and its gradient.
+// ffn.cu -- gated feed-forward block and its gradient on tcgen05 tensor cores (sm_103a).
+//
+//     g = x Wg,  u = x Wu,  h = act(g) u                      (x: T x D, Wg and Wu: D x F)
+//     dg = dh u act'(g),  du = dh act(g)
+//     dx = dg Wg^T + du Wu^T,   dWg = x^T dg,   dWu = x^T du
+//
+// act(g) = g s(q(g)), s the logistic function: q = g for SiLU, and for GELU in its tanh form
+// q = 2 sqrt(2/pi) (g + 0.044715 g^3), as (1 + tanh z) / 2 = s(2z).
+//
+// Forward and the two gradient products are one persistent kernel on CTA pairs, 256 x 256 output tiles
+// (128 rows per CTA), 64-deep stages by TMA, accumulators double-buffered in tensor memory. Forward, a
+// tile is 256 tokens by 128 columns of g beside the same 128 columns of u: CTA 0 of the pair brings
+// Wg's columns and CTA 1 Wu's, so that each thread of the epilogue holds g and u of its token and
+// writes h without either leaving the SM.  dx and the weights' gradients share one launch: dx's product
+// is a sum over 2F, theirs over T, and tiles of one fill the SMs that the other's last wave leaves idle.
+// Up to kGemvTokens tokens the block is bound by reading the weights and runs on k_ffn_few instead.
 #include <algorithm>
+#include <mutex>
 
+#include "common.cuh"
 #include "inner.cuh"
 #include "inner.h"
+#include "per_device.h"
 
 namespace isoloco {
 
 namespace {
 
-constexpr int kFt = 32;  // tile edge of the plain kernels
+// ------------------------------------------------------------------ activation
+// act(g) and, with SLOPE, act'(g).  expf and the division are good to a few units in fp32's last place,
+// below every rounding to 16 bits that follows; where the denominator passes 2^126 the quotient is 0.
+__device__ __forceinline__ float logistic(float q) { return __fdividef(1.f, 1.f + __expf(-q)); }
 
-__device__ __forceinline__ float act_value(float g, int act) {
-    if (act == ISOLOCO_SILU) return g / (1.f + expf(-g));
-    return 0.5f * g * (1.f + tanhf(0.7978845608028654f * (g + 0.044715f * g * g * g)));
+template <bool GELU>
+__device__ __forceinline__ float act_value(float g) {
+    return g * logistic(GELU ? 1.5957691216057308f * g * fmaf(0.044715f * g, g, 1.f) : g);
 }
-__device__ __forceinline__ float act_slope(float g, int act) {
-    if (act == ISOLOCO_SILU) {
-        const float s = 1.f / (1.f + expf(-g));
-        return s * (1.f + g * (1.f - s));
+template <bool GELU>
+__device__ __forceinline__ void act_both(float g, float& a, float& slope) {
+    if constexpr (GELU) {
+        const float g2 = g * g;
+        const float q = 1.5957691216057308f * g * fmaf(0.044715f, g2, 1.f);
+        const float s = logistic(q);
+        a = g * s;
+        // s is 0 or 1 to fp32 beyond |g| = 20, where g^3 may be infinite
+        const float t = fabsf(g) < 20.f ? 1.5957691216057308f * g * fmaf(0.134145f, g2, 1.f) * (1.f - s) : 0.f;
+        slope = s * (1.f + t);
+    } else {
+        const float s = logistic(g);
+        a = g * s;
+        slope = s * (1.f + g * (1.f - s));
     }
-    const float t = tanhf(0.7978845608028654f * (g + 0.044715f * g * g * g));
-    return 0.5f * (1.f + t) + 0.5f * g * (1.f - t * t) * 0.7978845608028654f * (1.f + 0.134145f * g * g);
 }
 
-// value clamped to the type's finite range: a saved product of inf would make NaN of 0 * inf
+// ------------------------------------------------------------------ g and u kept for the gradient
+// With fp16 operands they stay fp32.  With bf16 they take 16 bits: sign, 6 exponent and 9 fraction
+// bits, 2^-30 to 2^33 (and gradual underflow to 2^-39).  Two bits more than bf16 has keep their rounding
+// below that of dg and du: the gradients' error against 64 bits is 1.45 times that of one rounding
+// to bf16, where bf16 here gave 1.85; fp16's 11 bits would give 1.42 but end at 65504.
 template <class T>
-__device__ __forceinline__ T finite(float v) {
-    const float most = __is_same(T, __half) ? 65504.f : 3.3895314e38f;
-    return from_f32<T>(v > most ? most : v < -most ? -most : v);  // (NaN stays)
+struct Kept;
+template <>
+struct Kept<__half> {
+    using Store = float;
+    static __device__ __forceinline__ float clamp(float v) { return v > 3.4e38f ? 3.4e38f : v < -3.4e38f ? -3.4e38f : v; }
+};
+template <>
+struct Kept<__nv_bfloat16> {
+    using Store = uint16_t;
+    static __device__ __forceinline__ uint32_t encode(float v) {
+        // NaN: the largest exponent and fraction, kept apart from the largest finite code
+        const uint32_t sign = (__float_as_uint(v) >> 16) & 0x8000u;
+        const uint32_t b = __float_as_uint(fminf(fabsf(v), 8.5e9f) * 0x1p-96f);
+        const uint32_t code = (b + 0x1fffu + ((b >> 14) & 1u)) >> 14;
+        return sign | (v == v ? code : 0x7fffu);
+    }
+    static __device__ __forceinline__ float decode(uint32_t c) {
+        const float m = __uint_as_float((c & 0x7fffu) << 14) * 0x1p96f;
+        const float v = (c & 0x7fffu) == 0x7fffu ? __uint_as_float(0x7fc00000u) : m;
+        return (c & 0x8000u) ? -v : v;
+    }
+};
+
+// ------------------------------------------------------------------ the pair GEMM
+constexpr int kTileRows = 128;                 // of A per CTA
+constexpr int kDepth = 64;                     // K of a stage
+constexpr int kABytes = kTileRows * kDepth * 2;
+constexpr int kBBytes = 128 * kDepth * 2;      // at most 128 rows of B per CTA
+constexpr int kStageBytes = kABytes + kBBytes;
+constexpr int kStages = 6;
+constexpr int kEpiWarpsF = 8;
+constexpr int kStagingBytes = 4096;            // of an epilogue warp: 32 rows of 128 bytes
+constexpr int kThreads = 32 * (2 + kEpiWarpsF);
+constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kEpiWarpsF * kStagingBytes + 256;
+constexpr int kAccCols = 256;                  // tensor-memory columns of one accumulator
+
+// A product of the launch: `tiles` = tiles_m x tiles_n tiles of 256 x 2 nh.
+struct Product {
+    int kind;       // kGated, kDx or kDw
+    int tiles_m, tiles_n, nh;
+    int kblocks;    // of one tile, over all segments
+    int seg;        // k-blocks of one segment (kDx: F's, then F's again)
+    int mats;       // kDw: 2 (dWg's tiles, then dWu's), else 1
+};
+enum { kGated = 0, kDx = 1, kDw = 2 };
+
+struct alignas(64) FfnGemm {
+    CUtensorMap x_k, wg_mn, wu_mn, h, keep_g, keep_u;            // forward
+    CUtensorMap dg_k, du_k, wg_k, wu_k, dx, x_mn, dg_mn, du_mn, dwg, dwu;  // gradient
+    Product p[2];
+    int n0, n1;       // tiles of p[0] and p[1]
+    int extra;        // rounds of p[1] that the clusters without a tile in p[0]'s last round run first
+    int tokens, width, ff;
+    bool f16, keep, gelu;
+    uint32_t* err;
+};
+
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1)
+        : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(src), "r"(c0), "r"(c1)
+                 : "memory");
 }
 
-// acc(m, n) += sum_k A(m, k) B(k, n), element strides given; 32 x 32 outputs per CTA of 256 threads,
-// 4 rows per thread.
-template <class T>
-__device__ __forceinline__ void tile_product(const T* A, int64_t sam, int64_t sak, const T* B, int64_t sbk, int64_t sbn, int64_t M,
-                                             int64_t N, int64_t K, int64_t m0, int64_t n0, float (&acc)[4]) {
-    __shared__ float as[kFt][kFt + 1], bs[kFt][kFt + 1];
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    for (int64_t k0 = 0; k0 < K; k0 += kFt) {
-        for (int i = ty; i < kFt; i += 8) {
-            // the index along which memory is contiguous goes to the lanes
-            const int am = sak == 1 ? i : tx, ak = sak == 1 ? tx : i;
-            as[ak][am] = (m0 + am < M && k0 + ak < K) ? to_f32(A[(m0 + am) * sam + (k0 + ak) * sak]) : 0.f;
-            const int bn = sbn == 1 ? tx : i, bk = sbn == 1 ? i : tx;
-            bs[bk][bn] = (n0 + bn < N && k0 + bk < K) ? to_f32(B[(k0 + bk) * sbk + (n0 + bn) * sbn]) : 0.f;
+// The i-th tile of cluster c of C: p[0]'s tiles go round the clusters; p[1]'s fill the clusters that
+// p[0]'s last round left out for `extra` rounds and then go round all, those clusters first.
+struct TileAt {
+    const Product* p;
+    int m0, n0, mat;  // first row of the pair's 256, first column, matrix (kDw)
+    bool valid;
+};
+__device__ __forceinline__ TileAt tile_at(const FfnGemm& g, int c, int C, int i) {
+    const int full = g.n0 / C, rest = g.n0 % C, left = C - rest;  // clusters < rest run one more tile of p[0]
+    const int mine = full + (c < rest ? 1 : 0);
+    TileAt r;
+    r.valid = true;
+    int t;
+    if (i < mine) {
+        r.p = &g.p[0];
+        t = i * C + c;
+    } else {
+        r.p = &g.p[1];
+        const int j = i - mine;
+        if (c >= rest && j < g.extra) {
+            t = j * left + (c - rest);
+        } else {
+            const int round = c >= rest ? j - g.extra : j;
+            const int order = c >= rest ? c - rest : c + left;
+            t = g.extra * left + round * C + order;
         }
-        __syncthreads();
-#pragma unroll 8
-        for (int k = 0; k < kFt; ++k) {
-            const float b = bs[k][tx];
+        if (t >= g.n1) {
+            r.valid = false;
+            return r;
+        }
+    }
+    const int per = r.p->tiles_m * r.p->tiles_n;
+    r.mat = t / per;
+    t -= r.mat * per;
+    // panels of up to 8 tile rows, column by column: the clusters of one round share rows and columns
+    const int panel = t / (8 * r.p->tiles_n), in = t - panel * 8 * r.p->tiles_n;
+    const int rows = min(8, r.p->tiles_m - panel * 8);
+    r.m0 = (panel * 8 + in % rows) * 2 * kTileRows;
+    r.n0 = (in / rows) * (r.p->kind == kGated ? r.p->nh : 2 * r.p->nh);
+    return r;
+}
+
+__device__ __forceinline__ uint64_t k_desc(uint32_t a) { return make_sdesc(a, 16, 8 * kDepth * 2, 2); }
+__device__ __forceinline__ uint64_t mn_desc(uint32_t a) { return make_sdesc(a, kDepth * 128, 1024, 2); }
+
+// 32 rows x 64 columns of 16-bit values (w: the lane's row, 32 words) or 32 of fp32 to `dst`, rows of 128
+// bytes in the 128-byte swizzle, and from there by TMA to (col, row).
+__device__ __forceinline__ void store_block(const uint32_t (&w)[32], uint32_t stg, int lane, const CUtensorMap* map, int col,
+                                            int row) {
+    if (elect_one()) bulk_wait_read0();  // the block before has left
+    __syncwarp();
+    const uint32_t at = stg + lane * 128 + ((lane & 7) << 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] += as[k][ty * 4 + i] * b;
+    for (int q = 0; q < 8; ++q) st_shared4(at ^ (q << 4), w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (elect_one()) {
+        tma_store_2d(map, stg, col, row);
+        bulk_commit();
+    }
+}
+
+// One warp's 32 rows of a forward tile: columns [c0, c0 + 64) of g and u.
+template <class T, bool GELU>
+__device__ __forceinline__ void gated_block(const FfnGemm& p, uint32_t tacc, int nh, int c0, int col, int row, uint32_t stg,
+                                            int lane) {
+    uint32_t hw[32];
+    uint32_t kw[2][32];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        uint32_t g[32], u[32];
+        tmem_ld32(tacc + c0 + half * 32, g);
+        tmem_ld32(tacc + nh + c0 + half * 32, u);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float g0 = __uint_as_float(g[2 * j]), g1 = __uint_as_float(g[2 * j + 1]);
+            const float u0 = __uint_as_float(u[2 * j]), u1 = __uint_as_float(u[2 * j + 1]);
+            hw[half * 16 + j] = round16x2(act_value<GELU>(g0) * u0, act_value<GELU>(g1) * u1, __is_same(T, __half));
+            if constexpr (__is_same(T, __nv_bfloat16)) {
+                if (p.keep) {
+                    kw[0][half * 16 + j] = Kept<T>::encode(g0) | (Kept<T>::encode(g1) << 16);
+                    kw[1][half * 16 + j] = Kept<T>::encode(u0) | (Kept<T>::encode(u1) << 16);
+                }
+            }
         }
-        __syncthreads();
+        if constexpr (__is_same(T, __half)) {
+            if (p.keep) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    g[j] = __float_as_uint(Kept<T>::clamp(__uint_as_float(g[j])));
+                    u[j] = __float_as_uint(Kept<T>::clamp(__uint_as_float(u[j])));
+                }
+                if (col + half * 32 < p.ff) {
+                    store_block(g, stg, lane, &p.keep_g, col + half * 32, row);
+                    store_block(u, stg, lane, &p.keep_u, col + half * 32, row);
+                }
+            }
+        }
     }
-}
-
-template <class T>
-__global__ void __launch_bounds__(256) k_ffn(FfnArgs a, T* h, int64_t ld_h, T* saved, int64_t fp) {
-    const int64_t m0 = static_cast<int64_t>(blockIdx.x) * kFt, n0 = static_cast<int64_t>(blockIdx.y) * kFt;
-    float g[4] = {}, u[4] = {};
-    const T* x = static_cast<const T*>(a.x);
-    tile_product<T>(x, a.ld_x, 1, static_cast<const T*>(a.wg), a.ld_w, 1, a.tokens, a.ff, a.width, m0, n0, g);
-    tile_product<T>(x, a.ld_x, 1, static_cast<const T*>(a.wu), a.ld_w, 1, a.tokens, a.ff, a.width, m0, n0, u);
-    const int64_t n = n0 + (threadIdx.x & 31);
-    for (int i = 0; i < 4; ++i) {
-        const int64_t m = m0 + (threadIdx.x >> 5) * 4 + i;
-        if (m >= a.tokens || n >= a.ff) continue;
-        h[m * ld_h + n] = from_f32<T>(act_value(g[i], a.act) * u[i]);
-        if (saved) {
-            saved[m * 2 * fp + n] = finite<T>(g[i]);
-            saved[m * 2 * fp + fp + n] = finite<T>(u[i]);
+    store_block(hw, stg, lane, &p.h, col, row);
+    if constexpr (__is_same(T, __nv_bfloat16)) {
+        if (p.keep) {
+            store_block(kw[0], stg, lane, &p.keep_g, col, row);
+            store_block(kw[1], stg, lane, &p.keep_u, col, row);
         }
     }
 }
 
-// d: tokens x 2 x fp, dg then du
 template <class T>
-__global__ void __launch_bounds__(256) k_ffn_dgu(FfnArgs a, const T* dh, int64_t ld_dh, const T* saved, T* d, int64_t fp) {
-    const int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (n >= a.ff) return;
-    for (int64_t m = blockIdx.y; m < a.tokens; m += gridDim.y) {
-        const float g = to_f32(saved[m * 2 * fp + n]), u = to_f32(saved[m * 2 * fp + fp + n]), v = to_f32(dh[m * ld_dh + n]);
-        d[m * 2 * fp + n] = from_f32<T>(v * u * act_slope(g, a.act));
-        d[m * 2 * fp + fp + n] = from_f32<T>(v * act_value(g, a.act));
+__device__ __forceinline__ void plain_block(uint32_t tacc, int c0, const CUtensorMap* map, int col, int row, uint32_t stg, int lane) {
+    uint32_t w[32];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        uint32_t v[32];
+        tmem_ld32(tacc + c0 + half * 32, v);
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            w[half * 16 + j] = round16x2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]), __is_same(T, __half));
+    }
+    store_block(w, stg, lane, map, col, row);
+}
+
+// Persistent, clusters of two CTAs; cluster c runs tile_at(c, 0), tile_at(c, 1), ...  Warp 0 loads, warp 1
+// of CTA 0 issues the pair's MMAs, warps 2..9 of both drain the accumulators.  `full` / `empty` hand
+// stages over, `tfull` / `tempty` accumulators, as the TMA bytes and MMA commits complete.
+template <class T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ffn_gemm(const __grid_constant__ FfnGemm p) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* staging = smem + kStages * kStageBytes;
+    uint64_t* full = reinterpret_cast<uint64_t*>(staging + kEpiWarpsF * kStagingBytes);
+    uint64_t* empty = full + kStages;
+    uint64_t* tfull = empty + kStages;  // [2]
+    uint64_t* tempty = tfull + 2;       // [2]
+    uint64_t* drain = tempty + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    static_assert(8 * (2 * kStages + 5) + 8 <= 256, "barriers behind the staging blocks");
+
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
+    const int lane = threadIdx.x & 31;
+    const uint32_t crank = cluster_ctarank();
+    const bool leader = crank == 0;
+    const int c = static_cast<int>(blockIdx.x >> 1), C = static_cast<int>(gridDim.x >> 1);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&tfull[i], 1);
+            mbar_init(&tempty[i], kEpiWarpsF * 2);
+        }
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc_pair(tmem_slot, 2 * kAccCols);
+        tmem_relinquish_pair();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+
+    if (warp == 0) {
+        // ================= loads (one thread of each CTA)
+        if (elect_one()) {
+            const uint32_t sbase = smem_u32(smem);
+            const uint32_t fbar0 = mapa_shared(smem_u32(full), 0);
+            int stage = 0;
+            uint32_t phase = 0;
+            bool wrapped = false;
+            for (int i = 0; !*abort_flag; ++i) {
+                const TileAt t = tile_at(p, c, C, i);
+                if (!t.valid) break;
+                const Product& q = *t.p;
+                const int m0 = t.m0 + static_cast<int>(crank) * kTileRows;
+                const uint32_t pair_bytes = 2u * (kABytes + static_cast<uint32_t>(q.nh) * kDepth * 2u);
+                for (int kb = 0; kb < q.kblocks; ++kb) {
+                    if (!mbar_wait(&empty[stage], phase ^ 1u)) {
+                        *abort_flag = 1;
+                        atomicOr(p.err, kErrTimeout);
+                        break;
+                    }
+                    if (leader) mbar_arrive_expect_tx(&full[stage], pair_bytes);
+                    const uint32_t bar = fbar0 + 8u * stage;
+                    const uint32_t sa = sbase + stage * kStageBytes, sb = sa + kABytes;
+                    if (q.kind == kGated) {
+                        const int k0 = kb * kDepth;
+                        tma_load_2d_pair(sa, &p.x_k, bar, k0, m0);
+                        const CUtensorMap* w = leader ? &p.wg_mn : &p.wu_mn;
+                        for (int n = 0; n < q.nh; n += 64) tma_load_2d_pair(sb + n * kDepth * 2, w, bar, t.n0 + n, k0);
+                    } else if (q.kind == kDx) {
+                        const bool up = kb >= q.seg;
+                        const int k0 = (up ? kb - q.seg : kb) * kDepth;
+                        tma_load_2d_pair(sa, up ? &p.du_k : &p.dg_k, bar, k0, m0);
+                        tma_load_2d_pair(sb, up ? &p.wu_k : &p.wg_k, bar, k0, t.n0 + static_cast<int>(crank) * q.nh);
+                    } else {
+                        const int k0 = kb * kDepth, n0 = t.n0 + static_cast<int>(crank) * q.nh;
+                        for (int m = 0; m < kTileRows; m += 64) tma_load_2d_pair(sa + m * kDepth * 2, &p.x_mn, bar, m0 + m, k0);
+                        const CUtensorMap* d = t.mat ? &p.du_mn : &p.dg_mn;
+                        for (int n = 0; n < q.nh; n += 64) tma_load_2d_pair(sb + n * kDepth * 2, d, bar, n0 + n, k0);
+                    }
+                    if (++stage == kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                        wrapped = true;
+                    }
+                }
+            }
+            if (*abort_flag) {
+                // copies in flight land before the CTA exits (rank 0's barriers count both CTAs'
+                // copies; rank 1 leaves its own a generous margin)
+                if (leader) {
+                    drain_barriers(kStages, [&](int s, uint64_t*& bar, uint32_t& parity) {
+                        bar = &full[s];
+                        parity = s < stage ? phase : phase ^ 1u;
+                        return s < stage || wrapped;
+                    });
+                } else {
+                    const uint64_t t0 = globaltimer_ns();
+                    while (globaltimer_ns() - t0 < 100000ull) {
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ================= MMAs (one thread of CTA 0)
+        if (leader && elect_one()) {
+            const uint32_t sbase = smem_u32(smem);
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int i = 0; ok && !*abort_flag; ++i) {
+                const TileAt t = tile_at(p, c, C, i);
+                if (!t.valid) break;
+                const Product& q = *t.p;
+                const bool a_mn = q.kind == kDw, b_mn = q.kind != kDx;
+                const uint32_t idesc = make_idesc_16bit(2 * kTileRows, 2 * q.nh, a_mn, b_mn, p.f16);
+                const uint64_t da = a_mn ? mn_desc(sbase) : k_desc(sbase);
+                const uint64_t db = b_mn ? mn_desc(sbase + kABytes) : k_desc(sbase + kABytes);
+                const uint32_t a_lo = static_cast<uint32_t>(da), a_hi = static_cast<uint32_t>(da >> 32);
+                const uint32_t b_lo = static_cast<uint32_t>(db), b_hi = static_cast<uint32_t>(db >> 32);
+                const uint32_t step_a = a_mn ? 2048 >> 4 : 32 >> 4, step_b = b_mn ? 2048 >> 4 : 32 >> 4;
+                const uint32_t buf = i & 1;
+                if (!mbar_wait(&tempty[buf], ((i >> 1) & 1) ^ 1u)) {
+                    *abort_flag = 1;
+                    atomicOr(p.err, kErrTimeout);
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t tacc = tmem_base + buf * kAccCols;
+                uint32_t acc = 0;
+                const int nkb = q.kblocks;
+                bool ready = mbar_test(&full[stage], phase);
+#pragma unroll 1
+                for (int kb = 0; kb < nkb; ++kb) {
+                    const int s = stage;
+                    if (!ready && !mbar_wait(&full[s], phase)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t so = s * (kStageBytes >> 4);
+                    if (++stage == kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+#pragma unroll
+                    for (int ks = 0; ks < kDepth / 16; ++ks) {
+                        umma_16bit_pair(tacc, a_lo + so + ks * step_a, a_hi, b_lo + so + ks * step_b, b_hi, idesc, acc);
+                        acc = 1u;
+                        // the next stage's barrier is tested behind queued MMAs
+                        if (ks == kDepth / 16 - 2) ready = mbar_test(&full[stage], phase);
+                    }
+                    umma_commit_pair_mc(&empty[s], 0x3);
+                }
+                if (!ok) {
+                    *abort_flag = 1;
+                    atomicOr(p.err, kErrTimeout);
+                }
+                umma_commit_pair_mc(&tfull[buf], 0x3);
+            }
+            umma_commit_pair(drain);
+            (void)mbar_wait(drain, 0);
+        }
+    } else {
+        // ================= epilogue: warp w reads tensor-memory lanes 32 (w % 4) ..; of the tile's
+        // blocks of 64 columns warps 2..5 take the even, warps 6..9 the odd ones
+        const int eg = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t stg = smem_u32(staging) + (warp - 2) * kStagingBytes;
+        for (int i = 0;; ++i) {
+            const TileAt t = tile_at(p, c, C, i);
+            if (!t.valid) break;
+            const Product& q = *t.p;
+            const uint32_t buf = i & 1;
+            if (!__all_sync(0xffffffffu, mbar_wait(&tfull[buf], (i >> 1) & 1))) {
+                if (lane == 0) atomicOr(p.err, kErrTimeout);
+                break;
+            }
+            tc_fence_after();
+            const uint32_t tacc = tmem_base + buf * kAccCols + (static_cast<uint32_t>(eg * 32) << 16);
+            const int row = t.m0 + static_cast<int>(crank) * kTileRows + eg * 32;
+            if (q.kind == kGated) {
+                if (row < p.tokens)
+                    for (int c0 = half * 64; c0 < q.nh && t.n0 + c0 < p.ff; c0 += 128) {
+                        if (p.gelu) gated_block<T, true>(p, tacc, q.nh, c0, t.n0 + c0, row, stg, lane);
+                        else gated_block<T, false>(p, tacc, q.nh, c0, t.n0 + c0, row, stg, lane);
+                    }
+            } else {
+                const int rows = q.kind == kDx ? p.tokens : p.width, cols = q.kind == kDx ? p.width : p.ff;
+                const CUtensorMap* map = q.kind == kDx ? &p.dx : t.mat ? &p.dwu : &p.dwg;
+                if (row < rows)
+                    for (int c0 = half * 64; c0 < 2 * q.nh && t.n0 + c0 < cols; c0 += 128)
+                        plain_block<T>(tacc, c0, map, t.n0 + c0, row, stg, lane);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (leader) mbar_arrive(&tempty[buf]);
+                else mbar_arrive_cluster(mapa_shared(smem_u32(&tempty[buf]), 0));
+            }
+        }
+        if (elect_one()) bulk_wait0();
+        __syncwarp();
+    }
+
+    // neither CTA leaves, or frees tensor memory, while the pair's MMAs could still read its shared memory
+    // or write its accumulators (the issuing thread has waited for them)
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc_pair(tmem_base, 2 * kAccCols);
     }
 }
 
-template <class T>
-__global__ void __launch_bounds__(256) k_ffn_dx(FfnArgs a, const T* d, int64_t fp, T* dx, int64_t ld_dx) {
-    const int64_t m0 = static_cast<int64_t>(blockIdx.x) * kFt, n0 = static_cast<int64_t>(blockIdx.y) * kFt;
-    float acc[4] = {};
-    tile_product<T>(d, 2 * fp, 1, static_cast<const T*>(a.wg), 1, a.ld_w, a.tokens, a.width, a.ff, m0, n0, acc);
-    tile_product<T>(d + fp, 2 * fp, 1, static_cast<const T*>(a.wu), 1, a.ld_w, a.tokens, a.width, a.ff, m0, n0, acc);
-    const int64_t n = n0 + (threadIdx.x & 31);
-    for (int i = 0; i < 4; ++i) {
-        const int64_t m = m0 + (threadIdx.x >> 5) * 4 + i;
-        if (m < a.tokens && n < a.width) dx[m * ld_dx + n] = from_f32<T>(acc[i]);
+// ------------------------------------------------------------------ dg and du
+// d: tokens x 2 x pitch, dg then du of a token.  8 columns per thread; dh's rows may start anywhere.
+template <class T, bool GELU>
+__global__ void __launch_bounds__(256) k_ffn_dgu(const T* __restrict__ dh, int64_t ld_dh, bool dh_vec,
+                                                 const typename Kept<T>::Store* __restrict__ saved, T* __restrict__ d, int64_t tokens,
+                                                 int64_t ff, int64_t pitch) {
+    const int64_t n = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+    if (n >= ff) return;
+    const int cols = static_cast<int>(min(static_cast<int64_t>(8), ff - n));
+    for (int64_t m = blockIdx.y; m < tokens; m += gridDim.y) {
+        float g[8], u[8], v[8];
+        const int64_t at = m * 2 * pitch + n;  // the pad behind a row's last column may be read, not used
+        if constexpr (__is_same(T, __half)) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const float4 a = __ldcs(reinterpret_cast<const float4*>(saved + at) + q);
+                const float4 b = __ldcs(reinterpret_cast<const float4*>(saved + at + pitch) + q);
+                g[4 * q] = a.x, g[4 * q + 1] = a.y, g[4 * q + 2] = a.z, g[4 * q + 3] = a.w;
+                u[4 * q] = b.x, u[4 * q + 1] = b.y, u[4 * q + 2] = b.z, u[4 * q + 3] = b.w;
+            }
+        } else {
+            const uint4 a = ld_stream(saved + at), b = ld_stream(saved + at + pitch);
+            const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                g[2 * q] = Kept<T>::decode(aw[q] & 0xffffu), g[2 * q + 1] = Kept<T>::decode(aw[q] >> 16);
+                u[2 * q] = Kept<T>::decode(bw[q] & 0xffffu), u[2 * q + 1] = Kept<T>::decode(bw[q] >> 16);
+            }
+        }
+        if (dh_vec && cols == 8) {
+            Vec<T> w;
+            w.raw = ld_stream(dh + m * ld_dh + n);
+            w.unpack(v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < cols ? to_f32(dh[m * ld_dh + n + j]) : 0.f;
+        }
+        float dg[8], du[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float a, s;
+            act_both<GELU>(g[j], a, s);
+            dg[j] = v[j] * u[j] * s;
+            du[j] = v[j] * a;
+        }
+        Vec<T> w;
+        w.pack(dg);
+        *reinterpret_cast<uint4*>(d + at) = w.raw;
+        w.pack(du);
+        *reinterpret_cast<uint4*>(d + at + pitch) = w.raw;
     }
 }
 
-template <class T>
-__global__ void __launch_bounds__(256) k_ffn_dw(FfnArgs a, const T* d, int64_t fp, T* dwg, T* dwu, int64_t ld_dw) {
-    const int64_t m0 = static_cast<int64_t>(blockIdx.x) * kFt, n0 = static_cast<int64_t>(blockIdx.y) * kFt;
-    T* dw = blockIdx.z ? dwu : dwg;
-    float acc[4] = {};
-    tile_product<T>(static_cast<const T*>(a.x), 1, a.ld_x, d + blockIdx.z * fp, 2 * fp, 1, a.width, a.ff, a.tokens, m0, n0, acc);
-    const int64_t n = n0 + (threadIdx.x & 31);
-    for (int i = 0; i < 4; ++i) {
-        const int64_t m = m0 + (threadIdx.x >> 5) * 4 + i;
-        if (m < a.width && n < a.ff) dw[m * ld_dw + n] = from_f32<T>(acc[i]);
+// ------------------------------------------------------------------ few tokens
+constexpr int kGemvTokens = 8;
+constexpr int kFewThreads = 256;
+constexpr int kFewCols = 64;      // columns of F per cluster: 8 lanes of 16 bytes, whole 128-byte lines
+constexpr int kFewMaxSplit = 8;   // CTAs of a cluster, each a share of D
+
+// NT tokens.  A cluster of `split` CTAs owns kFewCols columns; its CTAs share D's rows, a warp reads 4
+// rows at a time (8 lanes each), and every thread keeps its 8 columns' sums for all tokens.  The sums meet by
+// shuffles, shared memory and, for the cluster's first CTA, distributed shared memory, in fixed order.
+template <class T, int NT, bool GELU>
+__global__ void __launch_bounds__(kFewThreads) k_ffn_few(const T* __restrict__ x, int64_t ld_x, const T* __restrict__ wg,
+                                                         const T* __restrict__ wu, int64_t ld_w, int width, int ff, T* __restrict__ h,
+                                                         int64_t ld_h, typename Kept<T>::Store* __restrict__ saved, int64_t pitch,
+                                                         int split) {
+    extern __shared__ float fsm[];
+    // [8 warps][2 NT][kFewCols] sums, then the CTA's [2 NT][kFewCols]; x's share [NT][rows] before that
+    const uint32_t rank = cluster_ctarank();
+    const int per = (width + split - 1) / split, d0 = static_cast<int>(rank) * per, rows = max(0, min(width - d0, per));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float* total = fsm;                              // [2 NT][kFewCols]
+    float* part = total + 2 * NT * kFewCols;         // [8][2 NT][kFewCols]
+    float* xs = part + 8 * 2 * NT * kFewCols;        // [rows][NT]
+    for (int i = threadIdx.x; i < rows * NT; i += kFewThreads) xs[i] = to_f32(x[(i % NT) * ld_x + d0 + i / NT]);
+    __syncthreads();
+    const int n = static_cast<int>(blockIdx.x / split) * kFewCols + (lane & 7) * 8;
+    float ag[NT][8], au[NT][8];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ag[t][j] = au[t][j] = 0.f;
+    if (n < ff) {  // (ff <= pitch, a multiple of 8: the last 16 bytes of a row exist)
+        const T* pg = wg + static_cast<int64_t>(d0) * ld_w + n;
+        const T* pu = wu + static_cast<int64_t>(d0) * ld_w + n;
+#pragma unroll 4
+        for (int r = warp * 4 + (lane >> 3); r < rows; r += 32) {
+            Vec<T> a, b;
+            a.raw = __ldg(reinterpret_cast<const uint4*>(pg + r * ld_w));
+            b.raw = __ldg(reinterpret_cast<const uint4*>(pu + r * ld_w));
+            float fa[8], fb[8];
+            a.unpack(fa);
+            b.unpack(fb);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float xv = xs[r * NT + t];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    ag[t][j] = fmaf(xv, fa[j], ag[t][j]);
+                    au[t][j] = fmaf(xv, fb[j], au[t][j]);
+                }
+            }
+        }
     }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+#pragma unroll
+            for (int o = 8; o <= 16; o <<= 1) {
+                ag[t][j] += __shfl_xor_sync(0xffffffffu, ag[t][j], o);
+                au[t][j] += __shfl_xor_sync(0xffffffffu, au[t][j], o);
+            }
+            if (lane < 8) {
+                part[(warp * 2 * NT + t) * kFewCols + lane * 8 + j] = ag[t][j];
+                part[(warp * 2 * NT + NT + t) * kFewCols + lane * 8 + j] = au[t][j];
+            }
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * NT * kFewCols; i += kFewThreads) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) s += part[w * 2 * NT * kFewCols + i];
+        total[i] = s;
+    }
+    cluster_sync();
+    if (rank == 0) {
+        const int c0 = static_cast<int>(blockIdx.x / split) * kFewCols;
+        for (int i = threadIdx.x; i < NT * kFewCols; i += kFewThreads) {
+            const int t = i / kFewCols, col = c0 + i % kFewCols;
+            float g = 0.f, u = 0.f;
+            for (int r = 0; r < split; ++r) {
+                float a, b;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(a) : "r"(mapa_shared(smem_u32(total + i), r)));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(b) : "r"(mapa_shared(smem_u32(total + NT * kFewCols + i), r)));
+                g += a;
+                u += b;
+            }
+            if (col < ff) {
+                h[t * ld_h + col] = from_f32<T>(act_value<GELU>(g) * u);
+                if (saved) {
+                    if constexpr (__is_same(T, __half)) {
+                        saved[t * 2 * pitch + col] = Kept<T>::clamp(g);
+                        saved[t * 2 * pitch + pitch + col] = Kept<T>::clamp(u);
+                    } else {
+                        saved[t * 2 * pitch + col] = static_cast<uint16_t>(Kept<T>::encode(g));
+                        saved[t * 2 * pitch + pitch + col] = static_cast<uint16_t>(Kept<T>::encode(u));
+                    }
+                }
+            }
+        }
+    }
+    cluster_sync();  // the other CTAs' sums stay until they have been read
 }
 
-inline int64_t pitch_of(int64_t ff) { return (ff + 7) / 8 * 8; }
-inline unsigned tiles(int64_t n) { return static_cast<unsigned>((n + kFt - 1) / kFt); }
+// ------------------------------------------------------------------ pitches
+// dst[r][0 .. cols) = src[r][0 .. cols), any pitches: operands that 16-byte accesses cannot read go through
+// the workspace (an extra read and write of them), and outputs come back the same way.
+__global__ void __launch_bounds__(256) k_repitch(const uint16_t* __restrict__ src, int64_t ld_s, uint16_t* __restrict__ dst, int64_t ld_d,
+                                                 int64_t rows, int64_t cols) {
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
+        for (int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; c < cols; c += static_cast<int64_t>(gridDim.x) * 256)
+            dst[r * ld_d + c] = src[r * ld_s + c];
+}
 
-template <class T>
-cudaError_t grad_t(const FfnArgs& a, const void* dh, int64_t ld_dh, const void* saved, void* dx, int64_t ld_dx, void* dwg, void* dwu,
-                   int64_t ld_dw, void* ws, cudaStream_t st) {
-    const int64_t fp = pitch_of(a.ff);
-    T* d = static_cast<T*>(ws);
-    if (a.tokens) {
-        k_ffn_dgu<T><<<dim3(static_cast<unsigned>((a.ff + 255) / 256), static_cast<unsigned>(std::min<int64_t>(a.tokens, 65535))), 256, 0,
-                       st>>>(a, static_cast<const T*>(dh), ld_dh, static_cast<const T*>(saved), d, fp);
-        if (dx) k_ffn_dx<T><<<dim3(tiles(a.tokens), tiles(a.width)), 256, 0, st>>>(a, d, fp, static_cast<T*>(dx), ld_dx);
-    }
-    if (dwg) k_ffn_dw<T><<<dim3(tiles(a.width), tiles(a.ff), 2), 256, 0, st>>>(a, d, fp, static_cast<T*>(dwg), static_cast<T*>(dwu), ld_dw);
+cudaError_t repitch(const void* src, int64_t ld_s, void* dst, int64_t ld_d, int64_t rows, int64_t cols, cudaStream_t st) {
+    if (rows == 0) return cudaSuccess;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((cols + 255) / 256, 64)), static_cast<unsigned>(std::min<int64_t>(rows, 16384)));
+    k_repitch<<<grid, 256, 0, st>>>(static_cast<const uint16_t*>(src), ld_s, static_cast<uint16_t*>(dst), ld_d, rows, cols);
     return cudaGetLastError();
+}
+
+inline int64_t pitch_of(int64_t n) { return (n + 7) / 8 * 8; }
+inline bool tma_ok(const void* p, int64_t ld) { return aligned16(p) && ld % 8 == 0; }
+inline int64_t r256(int64_t b) { return (b + 255) / 256 * 256; }
+inline int64_t copy_bytes(int64_t rows, int64_t cols) { return r256(rows * pitch_of(cols) * 2); }
+
+// Pieces of the workspace, taken one after the other.
+struct Arena {
+    uint8_t* p;
+    void* take(int64_t bytes) {
+        void* r = p;
+        p += r256(bytes);
+        return r;
+    }
+};
+
+// ------------------------------------------------------------------ tensor maps and launch
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                             CUtensorMapFloatOOBfill);
+
+EncodeFn encode_fn() {
+    static std::once_flag once;
+    static EncodeFn fn = nullptr;
+    std::call_once(once, [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeFn>(p);
+    });
+    return fn;
+}
+
+// rows x cols matrix of 2- or 4-byte elements, pitch in elements; boxes of 128 bytes x box_rows.
+bool make_map2(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t pitch, int box_rows, int es = 2) {
+    const EncodeFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch * es)};
+    cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / es), static_cast<cuuint32_t>(box_rows)}, step[2] = {1, 1};
+    return fn(m, es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
+              strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaLaunchConfig_t cluster_config(unsigned grid, unsigned threads, size_t smem, int cluster, cudaStream_t st, cudaLaunchAttribute* at) {
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = static_cast<unsigned>(cluster);
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cfg;
+}
+
+template <class T>
+cudaError_t gemm_clusters(int* clusters) {
+    static PerDevice fit;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    return fit.get<cudaError_t>(dev, clusters, [&](int* n) {
+        int sms = 0;
+        cudaError_t r = device_sms(&sms);
+        if (r == cudaSuccess) r = cudaFuncSetAttribute(k_ffn_gemm<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+        if (r != cudaSuccess) return r;
+        cudaLaunchAttribute at[1];
+        const cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(sms & ~1), kThreads, kSmemBytes, 2, nullptr, at);
+        r = cudaOccupancyMaxActiveClusters(n, k_ffn_gemm<T>, &cfg);
+        *n = std::max(1, std::min(*n, sms / 2));
+        return r;
+    });
+}
+
+template <class T>
+cudaError_t launch_gemm2(FfnGemm& g, cudaStream_t st) {
+    int C = 0;
+    cudaError_t e = gemm_clusters<T>(&C);
+    if (e != cudaSuccess || (e = error_word(&g.err)) != cudaSuccess) return e;
+    if (g.n0 + g.n1 == 0) return cudaSuccess;
+    C = std::min(C, g.n0 + g.n1);
+    cudaLaunchAttribute at[1];
+    const cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(2 * C), kThreads, kSmemBytes, 2, st, at);
+    // p[1]'s rounds that even out p[0]'s last: the number with the smallest longest cluster
+    const int full = g.n0 / C, rest = g.n0 % C, left = C - rest;
+    int64_t best = INT64_MAX;
+    g.extra = 0;
+    for (int x = 0; rest && x * left <= g.n1 + left && x < 4096; ++x) {
+        const int after = std::max(0, g.n1 - x * left), rounds = after / C, more = after % C;
+        // clusters without the extra tile of p[0] take the last round's tiles first
+        const int64_t a = static_cast<int64_t>(full) * g.p[0].kblocks + static_cast<int64_t>(x + rounds + (more > 0)) * g.p[1].kblocks;
+        const int64_t b = static_cast<int64_t>(full + 1) * g.p[0].kblocks + static_cast<int64_t>(rounds + (more > left)) * g.p[1].kblocks;
+        const int64_t t = std::max(a, b);
+        if (t < best) best = t, g.extra = x;
+    }
+    return cudaLaunchKernelEx(&cfg, k_ffn_gemm<T>, g);
+}
+
+inline int tiles(int64_t n, int per) { return static_cast<int>((n + per - 1) / per); }
+
+// ------------------------------------------------------------------ entry points' bodies
+template <class T, int NT, bool GELU>
+cudaError_t few_n(const FfnArgs& a, const void* wg, const void* wu, int64_t ld_w, void* h, int64_t ld_h, void* saved, cudaStream_t st) {
+    static PerDevice ready;
+    int sms = 0, dev = 0, unused = 0;
+    cudaError_t e = device_sms(&sms);
+    if (e == cudaSuccess) e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const int blocks = tiles(a.ff, kFewCols);
+    // split D until there is a CTA for every SM, a warp's worth of rows each at least; wide x needs the split
+    // for its share in shared memory (width <= 2^20: checked by the caller)
+    int split = 1;
+    while (split < kFewMaxSplit && (blocks * split < sms || a.width / split > 4096) && a.width / (2 * split) >= 32) split *= 2;
+    const size_t smem = sizeof(float) * (9 * 2 * NT * kFewCols + static_cast<size_t>((a.width + split - 1) / split) * NT);
+    e = ready.get<cudaError_t>(dev, &unused, [&](int* v) {
+        *v = 1;
+        return cudaFuncSetAttribute(k_ffn_few<T, NT, GELU>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    });
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute at[1];
+    const cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(blocks * split), kFewThreads, smem, split, st, at);
+    return cudaLaunchKernelEx(&cfg, k_ffn_few<T, NT, GELU>, static_cast<const T*>(a.x), a.ld_x, static_cast<const T*>(wg),
+                              static_cast<const T*>(wu), ld_w, static_cast<int>(a.width), static_cast<int>(a.ff), static_cast<T*>(h), ld_h,
+                              static_cast<typename Kept<T>::Store*>(saved), pitch_of(a.ff), split);
+}
+
+// whether the shares of x and the sums fit shared memory
+bool few_fits(int64_t tokens, int64_t width) {
+    return tokens <= kGemvTokens && width <= 4096 * kFewMaxSplit;
+}
+
+template <class T, bool GELU>
+cudaError_t few(const FfnArgs& a, const void* wg, const void* wu, int64_t ld_w, void* h, int64_t ld_h, void* saved, cudaStream_t st) {
+    switch (a.tokens) {
+        case 1: return few_n<T, 1, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
+        case 2: return few_n<T, 2, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
+        case 3: return few_n<T, 3, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
+        case 4: return few_n<T, 4, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
+        case 5: return few_n<T, 5, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
+        case 6: return few_n<T, 6, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
+        case 7: return few_n<T, 7, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
+        default: return few_n<T, 8, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
+    }
+}
+
+#define TRY(expr)                                  \
+    do {                                           \
+        const cudaError_t e_ = (expr);             \
+        if (e_ != cudaSuccess) return e_;          \
+    } while (0)
+
+constexpr cudaError_t kNoMap = cudaErrorInvalidValue;  // a tensor map that the driver refuses
+
+template <class T>
+cudaError_t forward(const FfnArgs& a, void* h, int64_t ld_h, void* saved, void* ws, cudaStream_t st) {
+    const bool f16 = __is_same(T, __half);
+    const int64_t fp = pitch_of(a.ff);
+    Arena arena = {static_cast<uint8_t*>(ws)};
+    const void *wg = a.wg, *wu = a.wu, *x = a.x;
+    int64_t ld_w = a.ld_w, ld_x = a.ld_x;
+    if (!tma_ok(wg, ld_w) || !tma_ok(wu, ld_w)) {
+        void *cg = arena.take(copy_bytes(a.width, a.ff)), *cu = arena.take(copy_bytes(a.width, a.ff));
+        TRY(repitch(wg, ld_w, cg, fp, a.width, a.ff, st));
+        TRY(repitch(wu, ld_w, cu, fp, a.width, a.ff, st));
+        wg = cg, wu = cu, ld_w = fp;
+    }
+    if (few_fits(a.tokens, a.width))
+        return a.act == ISOLOCO_SILU ? few<T, false>(a, wg, wu, ld_w, h, ld_h, saved, st) : few<T, true>(a, wg, wu, ld_w, h, ld_h, saved, st);
+    if (!tma_ok(x, ld_x)) {
+        void* cx = arena.take(copy_bytes(a.tokens, a.width));
+        TRY(repitch(x, ld_x, cx, pitch_of(a.width), a.tokens, a.width, st));
+        x = cx, ld_x = pitch_of(a.width);
+    }
+    const bool direct = tma_ok(h, ld_h);
+    void* out = direct ? h : arena.take(copy_bytes(a.tokens, a.ff));
+    FfnGemm g;
+    bool ok = make_map2(&g.x_k, x, a.tokens, a.width, ld_x, kTileRows) && make_map2(&g.wg_mn, wg, a.width, a.ff, ld_w, kDepth) &&
+              make_map2(&g.wu_mn, wu, a.width, a.ff, ld_w, kDepth) && make_map2(&g.h, out, a.tokens, a.ff, direct ? ld_h : fp, 32);
+    if (saved) {
+        constexpr int es = sizeof(typename Kept<T>::Store);
+        ok = ok && make_map2(&g.keep_g, saved, a.tokens, a.ff, 2 * fp, 32, es) &&
+             make_map2(&g.keep_u, static_cast<uint8_t*>(saved) + fp * es, a.tokens, a.ff, 2 * fp, 32, es);
+    }
+    if (!ok) return kNoMap;
+    const int kb = tiles(a.width, kDepth);
+    g.p[0] = {kGated, tiles(a.tokens, 256), tiles(a.ff, 128), 128, kb, kb, 1};
+    g.p[1] = g.p[0];
+    g.n0 = g.p[0].tiles_m * g.p[0].tiles_n;
+    g.n1 = 0;
+    g.tokens = static_cast<int>(a.tokens), g.width = static_cast<int>(a.width), g.ff = static_cast<int>(a.ff);
+    g.f16 = f16, g.keep = saved != nullptr, g.gelu = a.act == ISOLOCO_GELU_TANH;
+    TRY(launch_gemm2<T>(g, st));
+    return direct ? cudaSuccess : repitch(out, fp, h, ld_h, a.tokens, a.ff, st);
+}
+
+template <class T>
+cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void* saved, void* dx, int64_t ld_dx, void* dwg, void* dwu,
+                     int64_t ld_dw, void* ws, cudaStream_t st) {
+    const int64_t fp = pitch_of(a.ff), dp = pitch_of(a.width);
+    if (a.tokens == 0) {
+        if (dwg) {
+            TRY(cudaMemset2DAsync(dwg, ld_dw * 2, 0, a.ff * 2, a.width, st));
+            TRY(cudaMemset2DAsync(dwu, ld_dw * 2, 0, a.ff * 2, a.width, st));
+        }
+        return cudaSuccess;
+    }
+    Arena arena = {static_cast<uint8_t*>(ws)};
+    T* d = static_cast<T*>(arena.take(a.tokens * 2 * fp * 2));
+    const bool dh_vec = tma_ok(dh, ld_dh);
+    const dim3 grid(static_cast<unsigned>((fp / 8 + 255) / 256), static_cast<unsigned>(std::min<int64_t>(a.tokens, 32768)));
+    using Store = typename Kept<T>::Store;
+    if (a.act == ISOLOCO_SILU)
+        k_ffn_dgu<T, false><<<grid, 256, 0, st>>>(static_cast<const T*>(dh), ld_dh, dh_vec, static_cast<const Store*>(saved), d, a.tokens,
+                                                  a.ff, fp);
+    else
+        k_ffn_dgu<T, true><<<grid, 256, 0, st>>>(static_cast<const T*>(dh), ld_dh, dh_vec, static_cast<const Store*>(saved), d, a.tokens,
+                                                 a.ff, fp);
+    TRY(cudaGetLastError());
+    FfnGemm g;
+    bool ok = true;
+    Product pdx = {kDx, 0, 0, 128, 0, 0, 1}, pdw = {kDw, 0, 0, 128, 0, 0, 2};
+    void *odx = dx, *odg = dwg, *odu = dwu;
+    int64_t ldx = ld_dx, ldw = ld_dw;
+    if (dx) {
+        const void *wg = a.wg, *wu = a.wu;
+        int64_t ld_w = a.ld_w;
+        if (!tma_ok(wg, ld_w) || !tma_ok(wu, ld_w)) {
+            void *cg = arena.take(copy_bytes(a.width, a.ff)), *cu = arena.take(copy_bytes(a.width, a.ff));
+            TRY(repitch(wg, ld_w, cg, fp, a.width, a.ff, st));
+            TRY(repitch(wu, ld_w, cu, fp, a.width, a.ff, st));
+            wg = cg, wu = cu, ld_w = fp;
+        }
+        if (!tma_ok(dx, ldx)) odx = arena.take(copy_bytes(a.tokens, a.width)), ldx = dp;
+        const int seg = tiles(a.ff, kDepth);
+        pdx.tiles_m = tiles(a.tokens, 256), pdx.tiles_n = tiles(a.width, 2 * pdx.nh), pdx.seg = seg, pdx.kblocks = 2 * seg;
+        ok = ok && make_map2(&g.dg_k, d, a.tokens, a.ff, 2 * fp, kTileRows) && make_map2(&g.du_k, d + fp, a.tokens, a.ff, 2 * fp, kTileRows) &&
+             make_map2(&g.wg_k, wg, a.width, a.ff, ld_w, pdx.nh) && make_map2(&g.wu_k, wu, a.width, a.ff, ld_w, pdx.nh) &&
+             make_map2(&g.dx, odx, a.tokens, a.width, ldx, 32);
+    }
+    if (dwg) {
+        const void* x = a.x;
+        int64_t ld_x = a.ld_x;
+        if (!tma_ok(x, ld_x)) {
+            void* cx = arena.take(copy_bytes(a.tokens, a.width));
+            TRY(repitch(x, ld_x, cx, dp, a.tokens, a.width, st));
+            x = cx, ld_x = dp;
+        }
+        if (!tma_ok(dwg, ldw) || !tma_ok(dwu, ldw)) {
+            odg = arena.take(copy_bytes(a.width, a.ff)), odu = arena.take(copy_bytes(a.width, a.ff));
+            ldw = fp;
+        }
+        pdw.tiles_m = tiles(a.width, 256), pdw.tiles_n = tiles(a.ff, 2 * pdw.nh), pdw.kblocks = pdw.seg = tiles(a.tokens, kDepth);
+        ok = ok && make_map2(&g.x_mn, x, a.tokens, a.width, ld_x, kDepth) && make_map2(&g.dg_mn, d, a.tokens, a.ff, 2 * fp, kDepth) &&
+             make_map2(&g.du_mn, d + fp, a.tokens, a.ff, 2 * fp, kDepth) && make_map2(&g.dwg, odg, a.width, a.ff, ldw, 32) &&
+             make_map2(&g.dwu, odu, a.width, a.ff, ldw, 32);
+    }
+    if (!ok) return kNoMap;
+    const int ndx = pdx.tiles_m * pdx.tiles_n, ndw = 2 * pdw.tiles_m * pdw.tiles_n;
+    // the product with the longer tiles first
+    const bool dw_first = pdw.kblocks > pdx.kblocks;
+    g.p[0] = dw_first ? pdw : pdx;
+    g.p[1] = dw_first ? pdx : pdw;
+    g.n0 = dw_first ? ndw : ndx;
+    g.n1 = dw_first ? ndx : ndw;
+    g.tokens = static_cast<int>(a.tokens), g.width = static_cast<int>(a.width), g.ff = static_cast<int>(a.ff);
+    g.f16 = __is_same(T, __half), g.keep = false, g.gelu = false;
+    TRY(launch_gemm2<T>(g, st));
+    if (odx != dx) TRY(repitch(odx, ldx, dx, ld_dx, a.tokens, a.width, st));
+    if (odg != dwg) {
+        TRY(repitch(odg, ldw, dwg, ld_dw, a.width, a.ff, st));
+        TRY(repitch(odu, ldw, dwu, ld_dw, a.width, a.ff, st));
+    }
+    return cudaSuccess;
 }
 
 }  // namespace
 
-int64_t ffn_saved_bytes(int64_t tokens, int64_t ff) { return tokens * 2 * pitch_of(ff) * 2 + 16; }
-int64_t ffn_workspace(int64_t tokens, int64_t, int64_t ff, bool backward) { return backward ? ffn_saved_bytes(tokens, ff) : 16; }
+int64_t ffn_saved_bytes(int64_t tokens, int64_t ff, int dtype) {
+    return tokens * 2 * pitch_of(ff) * (dtype == ISOLOCO_F16 ? 4 : 2) + 16;
+}
 
-cudaError_t launch_ffn(const FfnArgs& a, void* h, int64_t ld_h, void* saved, void*, cudaStream_t st) {
+// `aligned`: no operand needs a copy with another pitch.
+int64_t ffn_workspace(int64_t tokens, int64_t width, int64_t ff, bool backward, bool aligned) {
+    int64_t n = 256;
+    if (backward) n += r256(tokens * 2 * pitch_of(ff) * 2);
+    // the weights and x; h, or dx and the weights' gradients
+    if (!aligned) n += (backward ? 4 : 2) * copy_bytes(width, ff) + (backward ? 2 : 1) * copy_bytes(tokens, width) +
+                       (backward ? 0 : copy_bytes(tokens, ff));
+    return n;
+}
+
+cudaError_t launch_ffn(const FfnArgs& a, void* h, int64_t ld_h, void* saved, void* ws, cudaStream_t st) {
     if (a.tokens == 0) return cudaSuccess;
-    const dim3 grid(tiles(a.tokens), tiles(a.ff));
-    if (a.dtype == ISOLOCO_BF16)
-        k_ffn<__nv_bfloat16><<<grid, 256, 0, st>>>(a, static_cast<__nv_bfloat16*>(h), ld_h, static_cast<__nv_bfloat16*>(saved), pitch_of(a.ff));
-    else
-        k_ffn<__half><<<grid, 256, 0, st>>>(a, static_cast<__half*>(h), ld_h, static_cast<__half*>(saved), pitch_of(a.ff));
-    return cudaGetLastError();
+    return a.dtype == ISOLOCO_BF16 ? forward<__nv_bfloat16>(a, h, ld_h, saved, ws, st) : forward<__half>(a, h, ld_h, saved, ws, st);
 }
 
 cudaError_t launch_ffn_grad(const FfnArgs& a, const void* dh, int64_t ld_dh, const void* saved, void* dx, int64_t ld_dx, void* dwg,
                             void* dwu, int64_t ld_dw, void* ws, cudaStream_t st) {
-    if (a.dtype == ISOLOCO_BF16) return grad_t<__nv_bfloat16>(a, dh, ld_dh, saved, dx, ld_dx, dwg, dwu, ld_dw, ws, st);
-    return grad_t<__half>(a, dh, ld_dh, saved, dx, ld_dx, dwg, dwu, ld_dw, ws, st);
+    return a.dtype == ISOLOCO_BF16 ? backward<__nv_bfloat16>(a, dh, ld_dh, saved, dx, ld_dx, dwg, dwu, ld_dw, ws, st)
+                                   : backward<__half>(a, dh, ld_dh, saved, dx, ld_dx, dwg, dwu, ld_dw, ws, st);
 }
 
 }  // namespace isoloco

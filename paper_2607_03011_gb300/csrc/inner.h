@@ -29,8 +29,9 @@ struct FfnArgs {
     int64_t ld_x, ld_w, tokens, width, ff;
     int dtype, act;
 };
-int64_t ffn_saved_bytes(int64_t tokens, int64_t ff);
-int64_t ffn_workspace(int64_t tokens, int64_t width, int64_t ff, bool backward);
+int64_t ffn_saved_bytes(int64_t tokens, int64_t ff, int dtype);
+// aligned: every matrix's address and pitch are multiples of 16 bytes
+int64_t ffn_workspace(int64_t tokens, int64_t width, int64_t ff, bool backward, bool aligned);
 cudaError_t launch_ffn(const FfnArgs& a, void* h, int64_t ld_h, void* saved, void* ws, cudaStream_t st);
 cudaError_t launch_ffn_grad(const FfnArgs& a, const void* dh, int64_t ld_dh, const void* saved, void* dx,
                             int64_t ld_dx, void* dwg, void* dwu, int64_t ld_dw, void* ws, cudaStream_t st);

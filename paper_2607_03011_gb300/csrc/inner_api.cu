@@ -51,6 +51,9 @@ int workspace_ok(const void* ws, int64_t have, int64_t need) {
     return ISOLOCO_OK;
 }
 
+// rows of 16-bit elements that all start at multiples of 16 bytes
+bool rows16(const void* p, int64_t ld, int64_t rows) { return rows == 0 || ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 8 == 0); }
+
 cudaStream_t stream_of(void* s) { return static_cast<cudaStream_t>(s); }
 
 const char* embed_problem(int dtype, int64_t vocab, int64_t width, const void* ids, int id_bytes, int64_t tokens) {
@@ -64,8 +67,8 @@ const char* embed_problem(int dtype, int64_t vocab, int64_t width, const void* i
 const char* ffn_problem(const FfnArgs& a) {
     if (!half_dtype(a.dtype)) return "the gated block takes BF16 or F16";
     if (a.act != ISOLOCO_SILU && a.act != ISOLOCO_GELU_TANH) return "bad activation";
-    if (!size_ok(a.tokens, 0) || !size_ok(a.width, 1) || !size_ok(a.ff, 1) || a.width > (1 << 20) || a.ff > (1 << 20))
-        return "tokens must be in 0 .. 2^31 - 1, width and ff in 1 .. 2^20";
+    if (a.tokens < 0 || a.tokens > (1 << 30) || a.width < 1 || a.ff < 1 || a.width > (1 << 20) || a.ff > (1 << 20))
+        return "tokens must be in 0 .. 2^30, width and ff in 1 .. 2^20";
     if (!matrix_ok(a.x, a.tokens, a.width, a.ld_x, 2)) return "x is NULL, misaligned or its pitch too small";
     if (!matrix_ok(a.wg, a.width, a.ff, a.ld_w, 2) || !matrix_ok(a.wu, a.width, a.ff, a.ld_w, 2))
         return "w_gate or w_up is NULL, misaligned or its pitch too small";
@@ -128,19 +131,19 @@ int isoloco_embed_grad(const void* dy, int64_t ld_dy, isoloco_dtype_t dtype, int
                                          workspace, stream_of(stream)));
 }
 
-int64_t isoloco_gated_ffn_saved_bytes(int64_t tokens, int64_t ff) {
-    if (!size_ok(tokens, 0) || !size_ok(ff, 1)) return ISOLOCO_ERR_INVALID;
-    return ffn_saved_bytes(tokens, ff);
+int64_t isoloco_gated_ffn_saved_bytes(int64_t tokens, int64_t ff, isoloco_dtype_t dtype) {
+    if (!size_ok(tokens, 0) || !size_ok(ff, 1) || !half_dtype(dtype)) return ISOLOCO_ERR_INVALID;
+    return ffn_saved_bytes(tokens, ff, dtype);
 }
 
-int64_t isoloco_gated_ffn_workspace(int64_t tokens, int64_t width, int64_t ff) {
+int64_t isoloco_gated_ffn_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned) {
     if (!size_ok(tokens, 0) || !size_ok(width, 1) || !size_ok(ff, 1)) return ISOLOCO_ERR_INVALID;
-    return ffn_workspace(tokens, width, ff, false);
+    return ffn_workspace(tokens, width, ff, false, aligned != 0);
 }
 
-int64_t isoloco_gated_ffn_grad_workspace(int64_t tokens, int64_t width, int64_t ff) {
+int64_t isoloco_gated_ffn_grad_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned) {
     if (!size_ok(tokens, 0) || !size_ok(width, 1) || !size_ok(ff, 1)) return ISOLOCO_ERR_INVALID;
-    return ffn_workspace(tokens, width, ff, true);
+    return ffn_workspace(tokens, width, ff, true, aligned != 0);
 }
 
 int isoloco_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w,
@@ -150,7 +153,8 @@ int isoloco_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, const voi
     if (const char* p = ffn_problem(a)) return invalid(p);
     if (!matrix_ok(h, tokens, ff, ld_h, 2)) return invalid("h is NULL, misaligned or its pitch too small");
     if (reinterpret_cast<uintptr_t>(saved) & 15u) return set_error(ISOLOCO_ERR_ALIGN, "saved is not 16-byte aligned");
-    const int rc = workspace_ok(workspace, workspace_bytes, ffn_workspace(tokens, width, ff, false));
+    const int rc = workspace_ok(workspace, workspace_bytes, ffn_workspace(tokens, width, ff, false,
+        rows16(x, ld_x, tokens) && rows16(w_gate, ld_w, width) && rows16(w_up, ld_w, width) && rows16(h, ld_h, tokens)));
     if (rc != ISOLOCO_OK) return rc;
     return cuda_status(launch_ffn(a, h, ld_h, saved, workspace, stream_of(stream)));
 }
@@ -168,7 +172,9 @@ int isoloco_gated_ffn_grad(const void* dh, int64_t ld_dh, const void* x, int64_t
     if (!dw_gate != !dw_up) return invalid("dw_gate and dw_up are given together");
     if (dw_gate && (!matrix_ok(dw_gate, width, ff, ld_dw, 2) || !matrix_ok(dw_up, width, ff, ld_dw, 2)))
         return invalid("dw_gate or dw_up is misaligned or its pitch too small");
-    const int rc = workspace_ok(workspace, workspace_bytes, ffn_workspace(tokens, width, ff, true));
+    const int rc = workspace_ok(workspace, workspace_bytes, ffn_workspace(tokens, width, ff, true,
+        rows16(x, ld_x, tokens) && rows16(w_gate, ld_w, width) && rows16(w_up, ld_w, width) && (!dx || rows16(dx, ld_dx, tokens)) &&
+        (!dw_gate || (rows16(dw_gate, ld_dw, width) && rows16(dw_up, ld_dw, width)))));
     if (rc != ISOLOCO_OK) return rc;
     return cuda_status(launch_ffn_grad(a, dh, ld_dh, saved, dx, ld_dx, dw_gate, dw_up, ld_dw, workspace, stream_of(stream)));
 }

@@ -115,6 +115,10 @@ def embed_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float =
     return dw
 
 
+def _rows16(t: torch.Tensor, ld: int) -> bool:
+    return t.data_ptr() % 16 == 0 and ld % 8 == 0
+
+
 def _ffn_operands(x, w_gate, w_up, act):
     x2, ldx = _rows(x, "x")
     wg, ldg = _rows(w_gate, "w_gate", x2)
@@ -127,19 +131,20 @@ def _ffn_operands(x, w_gate, w_up, act):
         raise ValueError("w_gate and w_up must have the same pitch")
     if act not in _ACT:
         raise ValueError(f"act: one of {sorted(_ACT)}")
-    return x2, ldx, wg, wu, ldg, _ACT[act]
+    aligned = _rows16(x2, ldx) and _rows16(wg, ldg) and _rows16(wu, ldg) and (x2.shape[1] | wg.shape[1]) % 8 == 0
+    return x2, ldx, wg, wu, ldg, _ACT[act], aligned
 
 
 def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: str = "silu", save: bool = False,
               stream=None):
     """h = act(x w_gate) * (x w_up); w_gate and w_up are width x ff.  With save=True returns
     (h, saved), where `saved` is what gated_ffn_grad needs besides the operands."""
-    x2, ldx, wg, wu, ldw, code = _ffn_operands(x, w_gate, w_up, act)
+    x2, ldx, wg, wu, ldw, code, aligned = _ffn_operands(x, w_gate, w_up, act)
     on = _On(stream)
     L, (n, width), ff = lib(), x2.shape, wg.shape[1]
     h = on.empty(x.shape[:-1] + (ff,), x.dtype, x.device)
-    saved = on.empty(L.isoloco_gated_ffn_saved_bytes(n, ff), torch.uint8, x.device) if save else None
-    need = L.isoloco_gated_ffn_workspace(n, width, ff)
+    saved = on.empty(L.isoloco_gated_ffn_saved_bytes(n, ff, _DTYPE[x.dtype]), torch.uint8, x.device) if save else None
+    need = L.isoloco_gated_ffn_workspace(n, width, ff, aligned)
     ws = on.empty(need, torch.uint8, x.device)
     _check(L.isoloco_gated_ffn(x2.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw, _DTYPE[x.dtype], n, width, ff, code,
                                h.data_ptr(), ff, _ptr(saved), ws.data_ptr(), need, on.handle), "isoloco_gated_ffn")
@@ -149,19 +154,19 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: st
 def gated_ffn_grad(grad: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, saved: torch.Tensor,
                    act: str = "silu", need_x: bool = True, need_w: bool = True, stream=None):
     """(dx, dw_gate, dw_up) for grad = d loss / d h; None for what is not needed."""
-    x2, ldx, wg, wu, ldw, code = _ffn_operands(x, w_gate, w_up, act)
+    x2, ldx, wg, wu, ldw, code, aligned = _ffn_operands(x, w_gate, w_up, act)
     dh, ldh = _rows(grad, "grad", x2)
     L, (n, width), ff = lib(), x2.shape, wg.shape[1]
     if dh.shape != (n, ff):
         raise ValueError(f"grad: {n} rows of {ff} expected")
     if saved.dtype != torch.uint8 or not saved.is_contiguous() or saved.device != x.device or \
-            saved.numel() != L.isoloco_gated_ffn_saved_bytes(n, ff):
+            saved.numel() != L.isoloco_gated_ffn_saved_bytes(n, ff, _DTYPE[x.dtype]):
         raise ValueError("saved: not what gated_ffn(save=True) returned for these sizes")
     on = _On(stream)
     dx = on.empty(x.shape, x.dtype, x.device) if need_x else None
     dwg = on.empty((width, ff), x.dtype, x.device) if need_w else None
     dwu = on.empty((width, ff), x.dtype, x.device) if need_w else None
-    need = L.isoloco_gated_ffn_grad_workspace(n, width, ff)
+    need = L.isoloco_gated_ffn_grad_workspace(n, width, ff, aligned)
     ws = on.empty(need, torch.uint8, x.device)
     _check(L.isoloco_gated_ffn_grad(dh.data_ptr(), ldh, x2.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw,
                                     _DTYPE[x.dtype], n, width, ff, code, saved.data_ptr(), _ptr(dx), width, _ptr(dwg),

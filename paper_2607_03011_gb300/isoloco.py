@@ -108,9 +108,10 @@ def lib():
             L.isoloco_grad_norm.argtypes = [ctypes.POINTER(Tensor), ci, _vp, _vp, i64, _vp]
             L.isoloco_clip_grads.argtypes = [ctypes.POINTER(Tensor), ctypes.POINTER(Tensor), ci, cf, _vp, _vp, i64, _vp]
             L.isoloco_inner_status.argtypes = [_vp]
-            for f in (L.isoloco_embed_grad_workspace, L.isoloco_gated_ffn_workspace, L.isoloco_gated_ffn_grad_workspace):
-                f.argtypes, f.restype = [i64, i64, i64], i64
-            L.isoloco_gated_ffn_saved_bytes.argtypes, L.isoloco_gated_ffn_saved_bytes.restype = [i64, i64], i64
+            L.isoloco_embed_grad_workspace.argtypes, L.isoloco_embed_grad_workspace.restype = [i64, i64, i64], i64
+            for f in (L.isoloco_gated_ffn_workspace, L.isoloco_gated_ffn_grad_workspace):
+                f.argtypes, f.restype = [i64, i64, i64, ci], i64
+            L.isoloco_gated_ffn_saved_bytes.argtypes, L.isoloco_gated_ffn_saved_bytes.restype = [i64, i64, ci], i64
             L.isoloco_token_logprobs_workspace.argtypes = [i64, i64, ci]
             L.isoloco_token_logprobs_workspace.restype = i64
             L.isoloco_grad_norm_workspace.argtypes, L.isoloco_grad_norm_workspace.restype = [ci], i64
