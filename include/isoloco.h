@@ -361,7 +361,7 @@ int64_t isoloco_plan_launches(isoloco_plan_t plan);
  * - Inputs are read and outputs written in their own type (F32, BF16 or F16); every sum, softmax
  *   statistic and norm is held in 32 bits or more, and an output is rounded once.
  * - A workspace of at least the bytes the *_workspace function gives is the caller's, used by one
- *   call at a time; it needs no initialisation and holds nothing between calls.
+ *   call at a time; it needs no initialisation and holds nothing between calls (0 bytes: it may be NULL).
  * - Calls enqueue work on `stream` and return.  Arguments are checked before anything is launched.
  *   Outputs may not overlap inputs unless an entry point says so.
  * - A token id or target outside [0, vocab) is no token: see each entry point.
@@ -395,7 +395,7 @@ int isoloco_embed_grad(const void* dy, int64_t ld_dy, isoloco_dtype_t dtype, int
  *   x w_up for isoloco_gated_ffn_grad: in fp32 for F16, in 16 bits (10 of them significant, magnitudes
  *   to 2^33, larger ones cut off there) for BF16.
  *   Workspace: aligned = 1 when the addresses and pitches of all matrices (without dh) are multiples of
- *   16 bytes, which needs little; 0 any others, which are copied to and from rows that are.
+ *   16 bytes; 0 any others, which are copied to and from rows that are.
  *   tokens up to 2^30, width and ff up to 2^20. */
 int64_t isoloco_gated_ffn_saved_bytes(int64_t tokens, int64_t ff, isoloco_dtype_t dtype);
 int64_t isoloco_gated_ffn_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned);
@@ -428,14 +428,13 @@ int isoloco_gated_ffn_grad(const void* dh, int64_t ld_dh, const void* x, int64_t
  * (fp32, either may be NULL for none) by the logits:
  *   scale * (grad_logp (1[j = t] - p_j) - grad_entropy p_j (log p_j + entropy)). */
 #define ISOLOCO_MAX_TOP 32
-int64_t isoloco_token_logprobs_workspace(int64_t rows, int64_t vocab, int top);
 int isoloco_token_logprobs(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows, int64_t vocab,
                            const void* targets, int target_bytes, float scale, float* logp, float* entropy, float* lse,
                            int top, float* top_logp, int64_t* top_index, const float* grad_logp,
-                           const float* grad_entropy, void* grad_logits, int64_t ld_grad, void* workspace,
-                           int64_t workspace_bytes, void* stream);
+                           const float* grad_entropy, void* grad_logits, int64_t ld_grad, void* stream);
 
-/* The same gradient by itself, from the lse and entropy of an earlier call on the same logits. */
+/* The same gradient by itself, from the lse and entropy of an earlier call on the same logits.  (p comes
+ * from z - lse here: a row whose logits all lie near the type's lowest value has lost log s in lse.) */
 int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows,
                                 int64_t vocab, const void* targets, int target_bytes, float scale, const float* lse,
                                 const float* entropy, const float* grad_logp, const float* grad_entropy,

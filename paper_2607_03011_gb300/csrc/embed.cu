@@ -80,6 +80,7 @@ __device__ void sort_ids(SortSmem& sm, const I* ids, int64_t n, int64_t vocab, i
     const SortRange rg = sort_range(n, rank, warp);
     const int passes = (bits + 7) / 8, dbits = (bits + passes - 1) / passes;
     const uint32_t dmask = (1u << dbits) - 1u;
+    cluster_sync();  // every CTA runs before another writes its shared memory
     for (int pass = 0; pass < passes; ++pass) {
         uint32_t* kdst = key[(passes - pass) & 1];  // key[1] in the last pass
         uint32_t* pdst = pos[(passes - pass) & 1];

@@ -932,7 +932,7 @@ int64_t ffn_saved_bytes(int64_t tokens, int64_t ff, int dtype) {
 
 // `aligned`: no operand needs a copy with another pitch.
 int64_t ffn_workspace(int64_t tokens, int64_t width, int64_t ff, bool backward, bool aligned) {
-    int64_t n = 256;
+    int64_t n = 0;
     if (backward) n += r256(tokens * 2 * pitch_of(ff) * 2);
     // the weights and x; h, or dx and the weights' gradients
     if (!aligned) n += (backward ? 4 : 2) * copy_bytes(width, ff) + (backward ? 2 : 1) * copy_bytes(tokens, width) +

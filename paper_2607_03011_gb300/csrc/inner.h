@@ -51,8 +51,7 @@ struct LogprobArgs {
     void* grad_logits;
     int64_t ld_grad;
 };
-int64_t logprob_workspace(int64_t rows, int64_t vocab, int top);
-cudaError_t launch_logprobs(const LogprobArgs& a, void* ws, cudaStream_t st);
+cudaError_t launch_logprobs(const LogprobArgs& a, cudaStream_t st);
 // a.lse and a.entropy are read
 cudaError_t launch_logprobs_grad(const LogprobArgs& a, cudaStream_t st);
 

@@ -46,6 +46,7 @@ bool matrix_ok(const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes)
 bool array_ok(const void* p, int64_t n, int bytes) { return n == 0 || (p && reinterpret_cast<uintptr_t>(p) % bytes == 0); }
 
 int workspace_ok(const void* ws, int64_t have, int64_t need) {
+    if (need == 0) return ISOLOCO_OK;
     if (!ws || have < need) return set_error(ISOLOCO_ERR_INVALID, ("workspace of " + std::to_string(need) + " bytes needed").c_str());
     if (reinterpret_cast<uintptr_t>(ws) & 15u) return set_error(ISOLOCO_ERR_ALIGN, "workspace is not 16-byte aligned");
     return ISOLOCO_OK;
@@ -179,24 +180,16 @@ int isoloco_gated_ffn_grad(const void* dh, int64_t ld_dh, const void* x, int64_t
     return cuda_status(launch_ffn_grad(a, dh, ld_dh, saved, dx, ld_dx, dw_gate, dw_up, ld_dw, workspace, stream_of(stream)));
 }
 
-int64_t isoloco_token_logprobs_workspace(int64_t rows, int64_t vocab, int top) {
-    if (!size_ok(rows, 0) || !size_ok(vocab, 1) || top < 0 || top > ISOLOCO_MAX_TOP) return ISOLOCO_ERR_INVALID;
-    return logprob_workspace(rows, vocab, top);
-}
-
 int isoloco_token_logprobs(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows, int64_t vocab,
                            const void* targets, int target_bytes, float scale, float* logp, float* entropy, float* lse,
                            int top, float* top_logp, int64_t* top_index, const float* grad_logp,
-                           const float* grad_entropy, void* grad_logits, int64_t ld_grad, void* workspace,
-                           int64_t workspace_bytes, void* stream) {
+                           const float* grad_entropy, void* grad_logits, int64_t ld_grad, void* stream) {
     const LogprobArgs a = {logits, ld_logits, rows, vocab, dtype, targets, target_bytes == 8, scale, logp, entropy, lse, top,
                            top_logp, top_index, grad_logp, grad_entropy, grad_logits, ld_grad};
     if (const char* p = logprob_problem(a, target_bytes)) return invalid(p);
     if (top < 0 || top > ISOLOCO_MAX_TOP || top > vocab) return invalid("top must be in 0 .. min(vocab, 32)");
     if (top && (!array_ok(top_logp, rows, 4) || !array_ok(top_index, rows, 8))) return invalid("top_logp or top_index is NULL or misaligned");
-    const int rc = workspace_ok(workspace, workspace_bytes, logprob_workspace(rows, vocab, top));
-    if (rc != ISOLOCO_OK) return rc;
-    return cuda_status(launch_logprobs(a, workspace, stream_of(stream)));
+    return cuda_status(launch_logprobs(a, stream_of(stream)));
 }
 
 int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows,

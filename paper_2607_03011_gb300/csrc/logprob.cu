@@ -1,7 +1,22 @@
 // logprob.cu -- log probabilities of given tokens, entropy, largest alternatives, and the gradient
 // of the first two by the logits.
+//
+// With z = scale x, M the row's largest x and d = (x - M) scale / ln 2:
+//     s = sum 2^d,  w = sum d 2^d:   lse = scale M + ln s,  entropy = ln s - ln 2 w / s
+// in one pass with a running maximum (s and w are rescaled when it rises).  M is the row's own
+// entry and d a difference first, so nothing overflows at the types' ends; d is cut off at kLowest, where
+// 2^d is 0 and d 2^d must be, too (masked logits; max.NaN keeps a NaN's row NaN).
+//
+// A row belongs to a cluster of `split` CTAs, each a contiguous share: one CTA where there are many
+// rows, up to 8 where few would leave SMs idle.  The gradient's second pass finds its row in L2.
+//
+// The `top` largest: the threads' own maxima, taken by groups, bound the top-th largest from below
+// (the top-th largest of kGroups group maxima); only threads whose maximum reaches the bound look
+// at their entries again, and the few entries found are ranked by counting.
 #include <algorithm>
+#include <type_traits>
 
+#include "common.cuh"
 #include "inner.cuh"
 #include "inner.h"
 
@@ -9,157 +24,470 @@ namespace isoloco {
 
 namespace {
 
-constexpr int kLpThreads = 256;
+constexpr float kLowest = -1000.f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kNoMax = -3.402823466e38f;
+constexpr int kGroups = 64;         // of threads, at least 2 ISOLOCO_MAX_TOP
+constexpr int kCandidates = 2048;   // entries a CTA ranks: all a row of equal logits gives, 64 (top - 1) + 64
+constexpr int kMaxSplit = 8;
+constexpr int kUnroll = 4;
 
-template <class I>
-__device__ __forceinline__ int64_t target_at(const I* t, int64_t r, int64_t vocab) { return token_at(t, r, vocab); }
-
-__device__ __forceinline__ float cta_max(float v, float* sm) {
-    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
-    __syncthreads();
-    for (int i = 0; i < kLpThreads / 32; ++i) v = fmaxf(v, sm[i]);
-    return v;
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-__device__ __forceinline__ float cta_sum(float v, float* sm) {
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = 0.f;
-    for (int i = 0; i < kLpThreads / 32; ++i) v += sm[i];
-    return v;
+// max(d, kLowest); NaN stays
+__device__ __forceinline__ float cut(float d) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(d), "f"(kLowest));
+    return y;
 }
 
-// Greater logits first, then lower indices.
-__device__ __forceinline__ bool before(float a, int64_t ia, float b, int64_t ib) { return a > b || (a == b && ia < ib); }
-
-// One row per CTA, one pass over it for each of the maximum, the sums and every alternative.
-template <class T, class I>
-__global__ void __launch_bounds__(kLpThreads) k_logprobs(LogprobArgs a) {
-    __shared__ float sm[kLpThreads / 32];
-    __shared__ float sv[kLpThreads / 32];
-    __shared__ int64_t si[kLpThreads / 32];
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const T* x = static_cast<const T*>(a.logits) + r * a.ld;
-        float m = -INFINITY;
-        for (int64_t j = threadIdx.x; j < a.vocab; j += kLpThreads) m = fmaxf(m, to_f32(x[j]));
-        m = cta_max(m, sm);
-        float s = 0.f, w = 0.f;
-        for (int64_t j = threadIdx.x; j < a.vocab; j += kLpThreads) {
-            const float v = to_f32(x[j]);
-            const float d = v == m ? 0.f : (v - m) * a.scale;
-            const float e = expf(d);
-            s += e;
-            if (e != 0.f) w += e * d;
-        }
-        s = cta_sum(s, sm);
-        w = cta_sum(w, sm);
-        const bool none = m == -INFINITY && s == s;  // (s is NaN if an entry is)
-        const float lse = none ? m : a.scale * m + logf(s);
-        if (m == INFINITY) s = NAN;
-        const float ent = none ? 0.f : logf(s) - w / s;
-        const int64_t t = target_at(static_cast<const I*>(a.targets), r, a.vocab);
-        if (threadIdx.x == 0) {
-            if (a.logp) a.logp[r] = t < 0 ? 0.f : none ? m : (to_f32(x[t]) - m) * a.scale - logf(s);
-            if (a.entropy) a.entropy[r] = ent;
-            if (a.lse) a.lse[r] = m == INFINITY ? NAN : lse;
-        }
-        float pv = INFINITY;
-        int64_t pi = -1;
-        for (int k = 0; k < a.top; ++k) {
-            float bv = -INFINITY;
-            int64_t bi = a.vocab;
-            for (int64_t j = threadIdx.x; j < a.vocab; j += kLpThreads) {
-                const float v = to_f32(x[j]);
-                if (before(pv, pi, v, j) && before(v, j, bv, bi)) {
-                    bv = v;
-                    bi = j;
-                }
-            }
-            for (int o = 16; o; o >>= 1) {
-                const float ov = __shfl_xor_sync(0xffffffffu, bv, o);
-                const int64_t oi = __shfl_xor_sync(0xffffffffu, bi, o);
-                if (before(ov, oi, bv, bi)) bv = ov, bi = oi;
-            }
-            __syncthreads();
-            if ((threadIdx.x & 31) == 0) sv[threadIdx.x >> 5] = bv, si[threadIdx.x >> 5] = bi;
-            __syncthreads();
-            for (int i = 0; i < kLpThreads / 32; ++i)
-                if (before(sv[i], si[i], bv, bi)) bv = sv[i], bi = si[i];
-            if (bi >= a.vocab) bi = a.vocab - 1;  // fewer comparable logits than asked for (NaN)
-            if (threadIdx.x == 0) {
-                a.top_index[r * a.top + k] = bi;
-                a.top_logp[r * a.top + k] = none ? m : (to_f32(x[bi]) - m) * a.scale - logf(s);
-            }
-            pv = bv;
-            pi = bi;
-        }
-        if (a.grad_logits) {
-            const float gl = (t >= 0 && a.grad_logp) ? a.grad_logp[r] : 0.f;
-            const float ge = a.grad_entropy ? a.grad_entropy[r] : 0.f;
-            const float ls = logf(s);
-            T* o = static_cast<T*>(a.grad_logits) + r * a.ld_grad;
-            __syncthreads();
-            for (int64_t j = threadIdx.x; j < a.vocab; j += kLpThreads) {
-                const float v = to_f32(x[j]);
-                const float lp = (v == m ? 0.f : (v - m) * a.scale) - ls;
-                const float p = expf(lp);
-                float g = (j == t ? gl : 0.f) - gl * p;
-                if (p != 0.f) g -= ge * p * (lp + ent);
-                o[j] = from_f32<T>(none ? 0.f : g * a.scale);
-            }
-        }
-        __syncthreads();
+// Running sums about their own maximum.
+struct Stat {
+    float m, s, w;
+    __device__ __forceinline__ void raise(float to, float c) {
+        const float d = cut((m - to) * c), f = ex2(d);
+        w = (w + s * d) * f;
+        s *= f;
+        m = to;
     }
-}
-
-template <class T, class I>
-__global__ void __launch_bounds__(kLpThreads) k_logprobs_grad(LogprobArgs a) {
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const T* x = static_cast<const T*>(a.logits) + r * a.ld;
-        T* o = static_cast<T*>(a.grad_logits) + r * a.ld_grad;
-        const int64_t t = target_at(static_cast<const I*>(a.targets), r, a.vocab);
-        const float lse = a.lse[r], ent = a.entropy ? a.entropy[r] : 0.f;
-        const bool none = lse == -INFINITY;
-        const float gl = (t >= 0 && a.grad_logp) ? a.grad_logp[r] : 0.f;
-        const float ge = a.grad_entropy ? a.grad_entropy[r] : 0.f;
-        for (int64_t j = threadIdx.x; j < a.vocab; j += kLpThreads) {
-            const float lp = to_f32(x[j]) * a.scale - lse;
-            const float p = expf(lp);
-            float g = (j == t ? gl : 0.f) - gl * p;
-            if (p != 0.f) g -= ge * p * (lp + ent);
-            o[j] = from_f32<T>(none ? 0.f : g * a.scale);
-        }
+    __device__ __forceinline__ void add(float x, float c) {
+        const float d = cut((x - m) * c), p = ex2(d);
+        s += p;
+        w = fmaf(d, p, w);
     }
-}
+    __device__ __forceinline__ void merge(float om, float os, float ow, float c) {
+        const float to = fmaxf(m, om);
+        const float d0 = cut((m - to) * c), d1 = cut((om - to) * c), f0 = ex2(d0), f1 = ex2(d1);
+        w = (w + s * d0) * f0 + (ow + os * d1) * f1;
+        s = s * f0 + os * f1;
+        m = to;
+    }
+};
 
 template <class T>
-cudaError_t run(const LogprobArgs& a, bool grad_only, cudaStream_t st) {
-    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(a.rows, 1 << 20));
-    if (grad_only) {
-        if (a.targets64) k_logprobs_grad<T, int64_t><<<grid, kLpThreads, 0, st>>>(a);
-        else k_logprobs_grad<T, int32_t><<<grid, kLpThreads, 0, st>>>(a);
+__device__ __forceinline__ float vec_max(const Vec<T>& v) {
+    if constexpr (sizeof(T) == 4) {
+        float f[4];
+        v.unpack(f);
+        return fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3]));
     } else {
-        if (a.targets64) k_logprobs<T, int64_t><<<grid, kLpThreads, 0, st>>>(a);
-        else k_logprobs<T, int32_t><<<grid, kLpThreads, 0, st>>>(a);
+        const uint32_t w[4] = {v.raw.x, v.raw.y, v.raw.z, v.raw.w};
+        if constexpr (__is_same(T, __half)) {
+            const __half2* h = reinterpret_cast<const __half2*>(w);
+            const float2 f = __half22float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+            return fmaxf(f.x, f.y);
+        } else {
+            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(w);
+            const float2 f = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+            return fmaxf(f.x, f.y);
+        }
     }
-    return cudaGetLastError();
 }
 
-cudaError_t dispatch(const LogprobArgs& a, bool grad_only, cudaStream_t st) {
-    if (a.rows == 0) return cudaSuccess;
-    if (a.dtype == ISOLOCO_F32) return run<float>(a, grad_only, st);
-    if (a.dtype == ISOLOCO_BF16) return run<__nv_bfloat16>(a, grad_only, st);
-    return run<__half>(a, grad_only, st);
+// Order of (value, index): greater values first, then lower indices; -0 and 0 are equal.
+__device__ __forceinline__ uint64_t rank_key(float v, uint32_t idx) {
+    const uint32_t u = __float_as_uint(v + 0.f);
+    const uint32_t o = (u & 0x80000000u) ? ~u : u | 0x80000000u;
+    return (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~idx);
+}
+
+struct TopSmem {
+    uint64_t group[kGroups];
+    uint64_t bound;
+    int count;
+    uint64_t cand[kCandidates];
+    uint64_t best[kMaxSplit][ISOLOCO_MAX_TOP];  // of every CTA of the cluster (read in the first)
+};
+
+// A CTA's share of a row: entries before the first 16-byte boundary, vectors, entries behind.
+template <class T>
+struct Share {
+    static constexpr int V = Vec<T>::kN;
+    const T* x;      // the share's first entry
+    uint32_t first;  // its index in the row
+    uint32_t n, head, nvec;
+    __device__ __forceinline__ Share(const T* row, uint32_t vocab, uint32_t rank, uint32_t split) {
+        const uint32_t per = ((vocab + split - 1) / split + 63u) & ~63u;
+        const uint64_t b = static_cast<uint64_t>(per) * rank;
+        first = b < vocab ? static_cast<uint32_t>(b) : vocab;
+        n = min(per, vocab - first);
+        x = row + first;
+        const uint32_t mis = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x) & 15u);
+        head = min(n, mis ? (16u - mis) / static_cast<uint32_t>(sizeof(T)) : 0u);
+        nvec = (n - head) / V;
+    }
+    __device__ __forceinline__ uint32_t tail() const { return head + nvec * V; }
+    __device__ __forceinline__ const uint4* vec(uint32_t i) const { return reinterpret_cast<const uint4*>(x + head) + i; }
+};
+
+template <int THREADS>
+__device__ __forceinline__ void merge_cta(Stat& st, float c, float (*sm)[3]) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1)
+        st.merge(__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.w, o), c);
+    if ((threadIdx.x & 31) == 0) {
+        float* e = sm[threadIdx.x >> 5];
+        e[0] = st.m, e[1] = st.s, e[2] = st.w;
+    }
+    __syncthreads();
+    const int l = threadIdx.x & 31;
+    constexpr int W = THREADS / 32;
+    st.m = l < W ? sm[l][0] : kNoMax;
+    st.s = l < W ? sm[l][1] : 0.f;
+    st.w = l < W ? sm[l][2] : 0.f;
+#pragma unroll
+    for (int o = W / 2; o; o >>= 1)
+        st.merge(__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.w, o), c);
+    st.m = __shfl_sync(0xffffffffu, st.m, 0);
+    st.s = __shfl_sync(0xffffffffu, st.s, 0);
+    st.w = __shfl_sync(0xffffffffu, st.w, 0);
+}
+
+// The CTA's k largest entries, in order, to best[0 .. k) (keys; 0 where there are fewer).  bv, bi: this
+// thread's largest value and an index not below its first place.
+template <class T, int THREADS>
+__device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int k, float bv, uint32_t bi, uint64_t* best) {
+    constexpr int kPer = THREADS / kGroups, V = Vec<T>::kN;
+    // keys not above and not below that of the thread's largest entry, which lies within a vector of bi
+    const bool any = bi != 0xffffffffu;
+    const uint64_t least = any ? rank_key(bv, sh.first + bi) : 0, most = any ? rank_key(bv, sh.first + (bi >= V - 1 ? bi - (V - 1) : 0)) : 0;
+    uint64_t g = least;
+#pragma unroll
+    for (int o = 1; o < kPer; o <<= 1) {
+        const uint64_t other = __shfl_xor_sync(0xffffffffu, g, o);
+        g = other > g ? other : g;
+    }
+    if (threadIdx.x % kPer == 0) sm.group[threadIdx.x / kPer] = g;
+    if (threadIdx.x == 0) sm.count = 0;
+    if (threadIdx.x < k) best[threadIdx.x] = 0;
+    __syncthreads();
+    if (threadIdx.x < kGroups) {
+        const uint64_t own = sm.group[threadIdx.x];
+        int r = 0;
+#pragma unroll 16
+        for (int j = 0; j < kGroups; ++j) {
+            const uint64_t v = sm.group[j];
+            r += (v > own || (v == own && j < static_cast<int>(threadIdx.x))) ? 1 : 0;  // (equal keys: groups without entries)
+        }
+        if (r == k - 1) sm.bound = own;
+    }
+    __syncthreads();
+    const uint64_t bound = sm.bound;
+    auto look = [&](float v, uint32_t i) {
+        if (v != v) return;  // NaN ranks nowhere
+        const uint64_t key = rank_key(v, sh.first + i);
+        if (key >= bound) {
+            const int at = atomicAdd(&sm.count, 1);
+            if (at < kCandidates) sm.cand[at] = key;
+        }
+    };
+    if (any && most >= bound) {
+        if (threadIdx.x < sh.head) look(to_f32(sh.x[threadIdx.x]), threadIdx.x);
+        for (uint32_t i = threadIdx.x; i < sh.nvec; i += THREADS) {
+            Vec<T> v;
+            v.raw = *sh.vec(i);
+            float f[V];
+            v.unpack(f);
+#pragma unroll
+            for (int j = 0; j < V; ++j) look(f[j], sh.head + i * V + j);
+        }
+        if (threadIdx.x < sh.n - sh.tail()) look(to_f32(sh.x[sh.tail() + threadIdx.x]), sh.tail() + threadIdx.x);
+    }
+    __syncthreads();
+    const int n = sm.count;
+    if (n <= kCandidates) {
+        for (int i = threadIdx.x; i < n; i += THREADS) {
+            const uint64_t own = sm.cand[i];
+            int r = 0;
+            for (int j = 0; j < n; ++j) r += sm.cand[j] > own ? 1 : 0;
+            if (r < k) best[r] = own;
+        }
+    } else {
+        // more entries above the bound than fit (most of the row's largest lie in few threads' shares):
+        // one at a time, the largest below the one before
+        uint64_t below = ~uint64_t(0);
+        for (int q = 0; q < k; ++q) {
+            uint64_t b = 0;
+            for (uint32_t i = threadIdx.x; i < sh.n; i += THREADS) {
+                const float v = to_f32(sh.x[i]);
+                const uint64_t key = v == v ? rank_key(v, sh.first + i) : 0;
+                if (key < below && key > b) b = key;
+            }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) {
+                const uint64_t other = __shfl_xor_sync(0xffffffffu, b, o);
+                b = other > b ? other : b;
+            }
+            __syncthreads();
+            if ((threadIdx.x & 31) == 0) sm.group[threadIdx.x >> 5] = b;
+            __syncthreads();
+            b = 0;
+            for (int i = 0; i < THREADS / 32; ++i) b = sm.group[i] > b ? sm.group[i] : b;
+            if (threadIdx.x == 0) best[q] = b;
+            below = b;
+        }
+    }
+    __syncthreads();
+}
+
+template <class T, class I, int THREADS, bool TOP, bool GRAD>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(LogprobArgs a, uint32_t split) {
+    constexpr int V = Vec<T>::kN;
+    __shared__ float sm[THREADS / 32][3];
+    __shared__ float peer[kMaxSplit][3];
+    __shared__ typename std::conditional<TOP, TopSmem, int>::type top_sm;
+    const uint32_t rank = split > 1 ? cluster_ctarank() : 0u;
+    const float c = a.scale * kLog2e;
+    const uint32_t vocab = static_cast<uint32_t>(a.vocab);
+    bool started = split == 1;  // every CTA of the cluster runs (before its shared memory is written)
+    if (!started) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    for (int64_t r = blockIdx.x / split; r < a.rows; r += gridDim.x / split) {
+        const T* row = static_cast<const T*>(a.logits) + r * a.ld;
+        const Share<T> sh(row, vocab, rank, split);
+        const int64_t t = token_at(static_cast<const I*>(a.targets), r, a.vocab);
+        const float xt = t >= 0 ? to_f32(row[t]) : 0.f;  // (early: its latency passes behind the row's)
+        Stat st = {kNoMax, 0.f, 0.f};
+        float bv = -INFINITY;
+        uint32_t bi = 0xffffffffu;
+        if (threadIdx.x < sh.head) {
+            const float v = to_f32(sh.x[threadIdx.x]);
+            if (v > st.m) st.m = v;
+            st.add(v, c);
+            if (TOP) bi = threadIdx.x, bv = v == v ? v : -INFINITY;
+        }
+        // kUnroll vectors in flight per thread; ALL: every one of them exists
+        auto batch = [&](uint32_t i, auto all) {
+            constexpr bool ALL = decltype(all)::value;
+            Vec<T> v[kUnroll];
+#pragma unroll
+            for (int q = 0; q < kUnroll; ++q)
+                if (ALL || i + q * THREADS < sh.nvec) {
+                    // (read again below: plain loads, which stay in L2; the gradient may overwrite the logits)
+                    if constexpr (GRAD || TOP) v[q].raw = *sh.vec(i + q * THREADS);
+                    else v[q].raw = ld_stream(sh.vec(i + q * THREADS));
+                }
+            float vm[kUnroll], most = -INFINITY;
+#pragma unroll
+            for (int q = 0; q < kUnroll; ++q)
+                if (ALL || i + q * THREADS < sh.nvec) {
+                    vm[q] = vec_max(v[q]);
+                    most = fmaxf(most, vm[q]);
+                }
+            if (most > st.m) st.raise(most, c);
+#pragma unroll
+            for (int q = 0; q < kUnroll; ++q)
+                if (ALL || i + q * THREADS < sh.nvec) {
+                    float f[V];
+                    v[q].unpack(f);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) st.add(f[j], c);
+                    if (TOP && (vm[q] > bv || bi == 0xffffffffu)) {
+                        bv = fmaxf(vm[q], bv);
+                        bi = sh.head + (i + q * THREADS) * V + V - 1;
+                    }
+                }
+        };
+        uint32_t i = threadIdx.x;
+        for (; i + (kUnroll - 1) * THREADS < sh.nvec; i += kUnroll * THREADS) batch(i, std::true_type());
+        if (i < sh.nvec) batch(i, std::false_type());
+        if (threadIdx.x < sh.n - sh.tail()) {
+            const float v = to_f32(sh.x[sh.tail() + threadIdx.x]);
+            if (v > st.m) st.raise(v, c);
+            st.add(v, c);
+            if (TOP && (v > bv || bi == 0xffffffffu)) bv = fmaxf(v, bv), bi = sh.tail() + threadIdx.x;
+        }
+        merge_cta<THREADS>(st, c, sm);
+        if (split > 1) {
+            if (!started) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+            started = true;
+            if (threadIdx.x < split) {
+                const uint32_t at = mapa_shared(smem_u32(peer[rank]), threadIdx.x);
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(st.m) : "memory");
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(st.s) : "memory");
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 8), "f"(st.w) : "memory");
+            }
+        }
+        if constexpr (TOP) {
+            // every CTA's largest go to the first CTA's shared memory
+            top_of_cta<T, THREADS>(top_sm, sh, a.top, bv, bi, top_sm.best[rank]);
+            if (split > 1 && rank > 0 && threadIdx.x < a.top) {
+                const uint32_t at = mapa_shared(smem_u32(&top_sm.best[rank][threadIdx.x]), 0);
+                asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(at), "l"(top_sm.best[rank][threadIdx.x]) : "memory");
+            }
+        }
+        if (split > 1) {
+            cluster_sync();
+            st = {kNoMax, 0.f, 0.f};
+            for (uint32_t q = 0; q < split; ++q) st.merge(peer[q][0], peer[q][1], peer[q][2], c);
+        }
+        const bool none = st.s == 0.f;  // every logit is -inf
+        const float lns = logf(st.s), ent = none ? 0.f : lns - kLn2 * (st.w / st.s);
+        if (rank == 0 && threadIdx.x == 0) {
+            if (a.logp) a.logp[r] = t < 0 ? 0.f : none ? -INFINITY : (xt - st.m) * a.scale - lns;
+            if (a.entropy) a.entropy[r] = ent;
+            if (a.lse) a.lse[r] = none ? -INFINITY : fmaf(st.m, a.scale, lns);
+        }
+        if constexpr (TOP) {
+            if (rank == 0) {
+                auto put = [&](int q, uint64_t key) {
+                    const uint32_t o = static_cast<uint32_t>(key >> 32);
+                    const float v = key ? __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o) : NAN;
+                    a.top_index[r * a.top + q] = key ? static_cast<int64_t>(static_cast<uint32_t>(~key)) : 0;
+                    a.top_logp[r * a.top + q] = none ? -INFINITY : (v - st.m) * a.scale - lns;
+                };
+                if (split == 1) {
+                    if (threadIdx.x < a.top) put(threadIdx.x, top_sm.best[0][threadIdx.x]);
+                } else {
+                    // ranks among all CTAs' largest (equal keys: places that hold none, key 0)
+                    const int n = static_cast<int>(split) * a.top;
+                    for (int e = threadIdx.x; e < n; e += THREADS) {
+                        const uint64_t own = top_sm.best[e / a.top][e % a.top];
+                        int rk = 0;
+                        for (int j = 0; j < n; ++j) {
+                            const uint64_t v = top_sm.best[j / a.top][j % a.top];
+                            rk += (v > own || (v == own && j < e)) ? 1 : 0;
+                        }
+                        if (rk < a.top) put(rk, own);
+                    }
+                }
+            }
+        }
+        if constexpr (GRAD) {
+            const float gl = (t >= 0 && !none && a.grad_logp) ? a.grad_logp[r] : 0.f;
+            const float ge = (!none && a.grad_entropy) ? a.grad_entropy[r] : 0.f;
+            // scale (-gl p - ge p (ln p + entropy)) = p (A + B log2 p)
+            const float A = -a.scale * fmaf(ge, ent, gl), B = -a.scale * ge * kLn2, l2 = none ? 0.f : log2f(st.s), m = st.m;
+            const float hot = gl * a.scale;
+            T* out = static_cast<T*>(a.grad_logits) + r * a.ld_grad + sh.first;
+            const uint32_t tt = t >= static_cast<int64_t>(sh.first) && t < static_cast<int64_t>(sh.first) + sh.n
+                                    ? static_cast<uint32_t>(t) - sh.first : 0xffffffffu;
+            auto grad = [&](float x) {
+                const float lp = cut(fmaf(x - m, c, -l2)), p = ex2(lp);
+                return p * fmaf(B, lp, A);
+            };
+            const bool vec_out = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(sh.x)) & 15u) == 0;
+            if (threadIdx.x < sh.head) out[threadIdx.x] = from_f32<T>(grad(to_f32(sh.x[threadIdx.x])) + (threadIdx.x == tt ? hot : 0.f));
+#pragma unroll 2
+            for (uint32_t v = threadIdx.x; v < sh.nvec; v += THREADS) {
+                Vec<T> x;
+                x.raw = *sh.vec(v);
+                float f[V];
+                x.unpack(f);
+                const uint32_t at = sh.head + v * V, hit = tt - at;
+#pragma unroll
+                for (int j = 0; j < V; ++j) f[j] = grad(f[j]);
+                if (hit < V) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) f[j] += static_cast<uint32_t>(j) == hit ? hot : 0.f;
+                }
+                if (vec_out) {
+                    x.pack(f);
+                    st_stream(out + at, x.raw);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) out[at + j] = from_f32<T>(f[j]);
+                }
+            }
+            const uint32_t e = sh.tail() + threadIdx.x;
+            if (e < sh.n) out[e] = from_f32<T>(grad(to_f32(sh.x[e])) + (e == tt ? hot : 0.f));
+        }
+        // the next row's sums overwrite shared memory that this row's threads (and CTAs) may still read
+        if (r + gridDim.x / split < a.rows) {
+            if (split > 1) cluster_sync();
+            else __syncthreads();
+        }
+    }
+}
+
+template <class T, class I>
+__global__ void __launch_bounds__(256) k_logprobs_grad(LogprobArgs a) {
+    constexpr int V = Vec<T>::kN;
+    for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
+        const T* row = static_cast<const T*>(a.logits) + r * a.ld;
+        T* out = static_cast<T*>(a.grad_logits) + r * a.ld_grad;
+        const int64_t t = token_at(static_cast<const I*>(a.targets), r, a.vocab);
+        const float lse = a.lse[r], ent = a.grad_entropy ? a.entropy[r] : 0.f;
+        const bool none = lse == -INFINITY;
+        const float gl = (t >= 0 && !none && a.grad_logp) ? a.grad_logp[r] : 0.f;
+        const float ge = (!none && a.grad_entropy) ? a.grad_entropy[r] : 0.f;
+        const float A = -a.scale * fmaf(ge, ent, gl), B = -a.scale * ge * kLn2;
+        auto grad = [&](float x, int64_t j) {
+            const float lp = cut(none ? kLowest : fmaf(x, a.scale, -lse) * kLog2e), p = ex2(lp);
+            return fmaf(p, fmaf(B, lp, A), j == t ? gl * a.scale : 0.f);
+        };
+        const bool vec = aligned16(row) && aligned16(out);
+        const int64_t nvec = vec ? a.vocab / V : 0;
+        for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < nvec; i += static_cast<int64_t>(gridDim.x) * 256) {
+            Vec<T> v;
+            v.raw = ld_stream(row + i * V);
+            float f[V];
+            v.unpack(f);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[j] = grad(f[j], i * V + j);
+            v.pack(f);
+            st_stream(out + i * V, v.raw);
+        }
+        for (int64_t i = nvec * V + static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < a.vocab; i += static_cast<int64_t>(gridDim.x) * 256)
+            out[i] = from_f32<T>(grad(to_f32(row[i]), i));
+    }
+}
+
+template <class T, class I, int THREADS, bool TOP, bool GRAD>
+cudaError_t launch_rows(const LogprobArgs& a, int sms, cudaStream_t st) {
+    // a row to one CTA where rows fill the GPU; else a cluster of up to 8, at least 4096 entries each
+    uint32_t split = 1;
+    while (split < kMaxSplit && a.rows * split * 2 <= 2 * sms && a.vocab / (2 * split) >= 4096) split *= 2;
+    const int64_t rows = std::min<int64_t>(a.rows, int64_t(1) << 24);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = split;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(rows * split));
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = split > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, k_logprobs<T, I, THREADS, TOP, GRAD>, a, split);
+}
+
+template <class T, class I>
+cudaError_t run(const LogprobArgs& a, cudaStream_t st) {
+    int sms = 0;
+    const cudaError_t e = device_sms(&sms);
+    if (e != cudaSuccess) return e;
+#define ROWS(N)                                                                                   \
+    (a.grad_logits ? (a.top ? launch_rows<T, I, N, true, true>(a, sms, st) : launch_rows<T, I, N, false, true>(a, sms, st)) \
+                   : (a.top ? launch_rows<T, I, N, true, false>(a, sms, st) : launch_rows<T, I, N, false, false>(a, sms, st)))
+    return a.vocab <= 4096 ? ROWS(128) : ROWS(512);
+#undef ROWS
+}
+
+template <class T, class I>
+cudaError_t run_grad(const LogprobArgs& a, cudaStream_t st) {
+    const unsigned rows = static_cast<unsigned>(std::min<int64_t>(a.rows, 65535));
+    const unsigned cols = static_cast<unsigned>(std::min<int64_t>((a.vocab + 8191) / 8192, 64));
+    k_logprobs_grad<T, I><<<dim3(cols, rows), 256, 0, st>>>(a);
+    return cudaGetLastError();
 }
 
 }  // namespace
 
-int64_t logprob_workspace(int64_t, int64_t, int) { return 16; }
+cudaError_t launch_logprobs(const LogprobArgs& a, cudaStream_t st) {
+    if (a.rows == 0) return cudaSuccess;
+    if (a.dtype == ISOLOCO_F32) return a.targets64 ? run<float, int64_t>(a, st) : run<float, int32_t>(a, st);
+    if (a.dtype == ISOLOCO_BF16) return a.targets64 ? run<__nv_bfloat16, int64_t>(a, st) : run<__nv_bfloat16, int32_t>(a, st);
+    return a.targets64 ? run<__half, int64_t>(a, st) : run<__half, int32_t>(a, st);
+}
 
-cudaError_t launch_logprobs(const LogprobArgs& a, void*, cudaStream_t st) { return dispatch(a, false, st); }
-cudaError_t launch_logprobs_grad(const LogprobArgs& a, cudaStream_t st) { return dispatch(a, true, st); }
+cudaError_t launch_logprobs_grad(const LogprobArgs& a, cudaStream_t st) {
+    if (a.rows == 0) return cudaSuccess;
+    if (a.dtype == ISOLOCO_F32) return a.targets64 ? run_grad<float, int64_t>(a, st) : run_grad<float, int32_t>(a, st);
+    if (a.dtype == ISOLOCO_BF16) return a.targets64 ? run_grad<__nv_bfloat16, int64_t>(a, st) : run_grad<__nv_bfloat16, int32_t>(a, st);
+    return a.targets64 ? run_grad<__half, int64_t>(a, st) : run_grad<__half, int32_t>(a, st);
+}
 
 }  // namespace isoloco

@@ -64,6 +64,8 @@ _vp = ctypes.c_void_p
 def lib():
     """Loads (building first if needed) the CUDA library; raises if that fails."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             path = _build.build()
@@ -102,18 +104,16 @@ def lib():
             L.isoloco_gated_ffn_grad.argtypes = [_vp, i64, _vp, i64, _vp, _vp, i64, ci, i64, i64, i64, ci, _vp, _vp, i64,
                                                  _vp, _vp, i64, _vp, i64, _vp]
             L.isoloco_token_logprobs.argtypes = [_vp, i64, ci, i64, i64, _vp, ci, cf, _vp, _vp, _vp, ci, _vp, _vp, _vp,
-                                                 _vp, _vp, i64, _vp, i64, _vp]
+                                                 _vp, _vp, i64, _vp]
             L.isoloco_token_logprobs_grad.argtypes = [_vp, i64, ci, i64, i64, _vp, ci, cf, _vp, _vp, _vp, _vp, _vp, i64,
                                                       _vp]
-            L.isoloco_grad_norm.argtypes = [ctypes.POINTER(Tensor), ci, _vp, _vp, i64, _vp]
-            L.isoloco_clip_grads.argtypes = [ctypes.POINTER(Tensor), ctypes.POINTER(Tensor), ci, cf, _vp, _vp, i64, _vp]
+            L.isoloco_grad_norm.argtypes = [_vp, ci, _vp, _vp, i64, _vp]
+            L.isoloco_clip_grads.argtypes = [_vp, _vp, ci, cf, _vp, _vp, i64, _vp]
             L.isoloco_inner_status.argtypes = [_vp]
             L.isoloco_embed_grad_workspace.argtypes, L.isoloco_embed_grad_workspace.restype = [i64, i64, i64], i64
             for f in (L.isoloco_gated_ffn_workspace, L.isoloco_gated_ffn_grad_workspace):
                 f.argtypes, f.restype = [i64, i64, i64, ci], i64
             L.isoloco_gated_ffn_saved_bytes.argtypes, L.isoloco_gated_ffn_saved_bytes.restype = [i64, i64, ci], i64
-            L.isoloco_token_logprobs_workspace.argtypes = [i64, i64, ci]
-            L.isoloco_token_logprobs_workspace.restype = i64
             L.isoloco_grad_norm_workspace.argtypes, L.isoloco_grad_norm_workspace.restype = [ci], i64
             _lib = L
     return _lib

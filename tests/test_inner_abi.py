@@ -60,10 +60,10 @@ def test_gated_ffn(iso, ptr):
         return L.isoloco_gated_ffn(x, ldx, wg, wu, ldw, dt, n, d, f, act, h, ldh, saved, ws, wsb, None)
 
     for kw in (dict(x=None), dict(ldx=7), dict(wg=None), dict(wu=None), dict(ldw=15), dict(dt=0), dict(dt=3), dict(act=2), dict(act=-1),
-               dict(n=-1), dict(d=0), dict(f=0), dict(f=(1 << 20) + 1), dict(h=None), dict(ldh=15), dict(ws=None), dict(wsb=0),
-               dict(x=odd(p)), dict(wu=odd(p))):
+               dict(n=-1), dict(d=0), dict(f=0), dict(f=(1 << 20) + 1), dict(h=None), dict(ldh=15),
+               dict(ldw=17, ws=None), dict(ldh=17, wsb=0), dict(x=odd(p)), dict(wu=odd(p))):
         assert call(**kw) == bad, kw
-    assert call(saved=odd(p, 8)) == iso.ERR_ALIGN and call(ws=odd(p, 8)) == iso.ERR_ALIGN
+    assert call(saved=odd(p, 8)) == iso.ERR_ALIGN and call(ldx=9, ws=odd(p, 8)) == iso.ERR_ALIGN
 
 
 def test_gated_ffn_grad(iso, ptr):
@@ -82,12 +82,12 @@ def test_gated_ffn_grad(iso, ptr):
 def test_token_logprobs(iso, ptr):
     L, bad, p = iso.lib(), iso.ERR_INVALID, ptr
 
-    def call(z=p, ld=8, dt=0, n=2, v=8, t=p, tb=8, scale=1.0, top=0, tl=None, ti=None, gz=None, ldg=8, ws=p, wsb=BIG):
-        return L.isoloco_token_logprobs(z, ld, dt, n, v, t, tb, scale, None, None, None, top, tl, ti, None, None, gz, ldg, ws, wsb, None)
+    def call(z=p, ld=8, dt=0, n=2, v=8, t=p, tb=8, scale=1.0, top=0, tl=None, ti=None, gz=None, ldg=8):
+        return L.isoloco_token_logprobs(z, ld, dt, n, v, t, tb, scale, None, None, None, top, tl, ti, None, None, gz, ldg, None)
 
     for kw in (dict(z=None), dict(ld=7), dict(dt=9), dict(n=-1), dict(v=0), dict(t=None), dict(tb=1), dict(scale=0.0), dict(scale=-1.0),
                dict(scale=float("nan")), dict(scale=float("inf")), dict(top=9, tl=p, ti=p), dict(top=33, v=64, ld=64, tl=p, ti=p),
-               dict(top=-1), dict(top=2, tl=p), dict(top=2, ti=p), dict(gz=p, ldg=7), dict(ws=None), dict(wsb=0), dict(z=odd(p))):
+               dict(top=-1), dict(top=2, tl=p), dict(top=2, ti=p), dict(gz=p, ldg=7), dict(z=odd(p))):
         assert call(**kw) == bad, kw
 
     def grad(lse=p, ent=p, ge=p, gz=p, ldg=8):
