@@ -1,11 +1,12 @@
 // logprob.cu -- log probabilities of given tokens, entropy, largest alternatives, and the gradient
 // of the first two by the logits.
 //
-// With z = scale x, M the row's largest x and d = (x - M) scale / ln 2:
+// With M the row's largest logit and d = (x - M) scale / ln 2:
 //     s = sum 2^d,  w = sum d 2^d:   lse = scale M + ln s,  entropy = ln s - ln 2 w / s
-// in one pass with a running maximum (s and w are rescaled when it rises).  M is the row's own
-// entry and d a difference first, so nothing overflows at the types' ends; d is cut off at kLowest, where
-// 2^d is 0 and d 2^d must be, too (masked logits; max.NaN keeps a NaN's row NaN).
+// in one pass with a running maximum (s and w are rescaled when it rises).  The difference comes first,
+// so that the largest entry's power is 1 exactly and nothing overflows at the types' ends (folding it
+// into one multiply-add, x c - M c, needs both handled apart).  d is cut off at kLowest, where 2^d
+// is 0 and d 2^d must be, too (masked logits; max.NaN keeps a NaN's row NaN).
 //
 // A row belongs to a cluster of `split` CTAs, each a contiguous share: one CTA where there are many
 // rows, up to 8 where few would leave SMs idle.  The gradient's second pass finds its row in L2.
@@ -26,11 +27,13 @@ namespace {
 
 constexpr float kLowest = -1000.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kNoMax = -3.402823466e38f;
 constexpr int kGroups = 64;         // of threads, at least 2 ISOLOCO_MAX_TOP
 constexpr int kCandidates = 2048;   // entries a CTA ranks: all a row of equal logits gives, 64 (top - 1) + 64
 constexpr int kMaxSplit = 8;
 constexpr int kUnroll = 4;
+// Threads per SM the registers are cut for: 5 CTAs of 256 (8192 x 32000 bf16 with gradient 180 us; 4 CTAs, with
+// 64 registers, 194; 6, with 40, 188; 8 of 128 threads 229).
+constexpr int kThreadsPerSm = 1280;
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -44,12 +47,47 @@ __device__ __forceinline__ float cut(float d) {
     return y;
 }
 
-// Running sums about their own maximum.
+// Two fp32 operations per instruction (sm_100's packed forms; each rounds as its scalar form does).
+struct F2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ F2 pair(float a, float b) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(F2 a, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a.v)); }
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+// d of two logits, from -M and c
+__device__ __forceinline__ F2 exponents(float x0, float x1, F2 minus_m, F2 c2, float& d0, float& d1) {
+    unpair(mul2(add2(pair(x0, x1), minus_m), c2), d0, d1);
+    d0 = cut(d0);
+    d1 = cut(d1);
+    return pair(d0, d1);
+}
+
+// Running sums about the largest logit so far (no logit: the least number, with sums of 0).
 struct Stat {
     float m, s, w;
+    __device__ __forceinline__ void clear() { m = -3.402823466e38f, s = w = 0.f; }
+    // the same sums about `to` >= m
     __device__ __forceinline__ void raise(float to, float c) {
         const float d = cut((m - to) * c), f = ex2(d);
-        w = (w + s * d) * f;
+        w = fmaf(s, d, w) * f;
         s *= f;
         m = to;
     }
@@ -58,34 +96,57 @@ struct Stat {
         s += p;
         w = fmaf(d, p, w);
     }
-    __device__ __forceinline__ void merge(float om, float os, float ow, float c) {
-        const float to = fmaxf(m, om);
-        const float d0 = cut((m - to) * c), d1 = cut((om - to) * c), f0 = ex2(d0), f1 = ex2(d1);
-        w = (w + s * d0) * f0 + (ow + os * d1) * f1;
-        s = s * f0 + os * f1;
+};
+
+// A thread's running sums, of even and odd entries apart.
+struct Stat2 {
+    float m;
+    F2 s, w;
+    __device__ __forceinline__ void raise(float to, float c) {
+        const float d = cut((m - to) * c), f = ex2(d);
+        w = mul2(fma2(s, pair(d, d), w), pair(f, f));
+        s = mul2(s, pair(f, f));
         m = to;
+    }
+    __device__ __forceinline__ void add(float x0, float x1, F2 minus_m, F2 c2) {
+        float d0, d1;
+        const F2 d = exponents(x0, x1, minus_m, c2, d0, d1), p = pair(ex2(d0), ex2(d1));
+        s = add2(s, p);
+        w = fma2(d, p, w);
     }
 };
 
+// Largest entries of vectors: pairs of 16-bit entries (or four fp32 ones) are compared at once.
 template <class T>
-__device__ __forceinline__ float vec_max(const Vec<T>& v) {
-    if constexpr (sizeof(T) == 4) {
-        float f[4];
-        v.unpack(f);
-        return fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3]));
-    } else {
-        const uint32_t w[4] = {v.raw.x, v.raw.y, v.raw.z, v.raw.w};
-        if constexpr (__is_same(T, __half)) {
-            const __half2* h = reinterpret_cast<const __half2*>(w);
-            const float2 f = __half22float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
-            return fmaxf(f.x, f.y);
+struct Largest {
+    uint32_t w[4];
+    __device__ __forceinline__ void set(const Vec<T>& v) { w[0] = v.raw.x, w[1] = v.raw.y, w[2] = v.raw.z, w[3] = v.raw.w; }
+    static __device__ __forceinline__ uint32_t more(uint32_t a, uint32_t b) {
+        if constexpr (sizeof(T) == 4) {
+            return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+        } else if constexpr (__is_same(T, __half)) {
+            const __half2 h = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+            return *reinterpret_cast<const uint32_t*>(&h);
         } else {
-            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(w);
-            const float2 f = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
-            return fmaxf(f.x, f.y);
+            const __nv_bfloat162 h = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+            return *reinterpret_cast<const uint32_t*>(&h);
         }
     }
-}
+    __device__ __forceinline__ void take(const Largest& o) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = more(w[i], o.w[i]);
+    }
+    __device__ __forceinline__ float value() const {
+        const uint32_t m = more(more(w[0], w[1]), more(w[2], w[3]));
+        if constexpr (sizeof(T) == 4) return __uint_as_float(m);
+        else if constexpr (__is_same(T, __half)) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&m));
+            return fmaxf(f.x, f.y);
+        } else {
+            return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+        }
+    }
+};
 
 // Order of (value, index): greater values first, then lower indices; -0 and 0 are equal.
 __device__ __forceinline__ uint64_t rank_key(float v, uint32_t idx) {
@@ -97,7 +158,8 @@ __device__ __forceinline__ uint64_t rank_key(float v, uint32_t idx) {
 struct TopSmem {
     uint64_t group[kGroups];
     uint64_t bound;
-    int count;
+    int count, threads;
+    uint16_t thread[1024];  // those whose entries may reach the bound
     uint64_t cand[kCandidates];
     uint64_t best[kMaxSplit][ISOLOCO_MAX_TOP];  // of every CTA of the cluster (read in the first)
 };
@@ -123,27 +185,29 @@ struct Share {
     __device__ __forceinline__ const uint4* vec(uint32_t i) const { return reinterpret_cast<const uint4*>(x + head) + i; }
 };
 
-template <int THREADS>
-__device__ __forceinline__ void merge_cta(Stat& st, float c, float (*sm)[3]) {
+// Sums over W lanes (every lane gets them): first the common maximum, then one rescaling.
+template <int W>
+__device__ __forceinline__ void merge_lanes(Stat& st, float c) {
+    float m = st.m;
 #pragma unroll
-    for (int o = 16; o; o >>= 1)
-        st.merge(__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.w, o), c);
-    if ((threadIdx.x & 31) == 0) {
-        float* e = sm[threadIdx.x >> 5];
-        e[0] = st.m, e[1] = st.s, e[2] = st.w;
+    for (int o = W / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    st.raise(m, c);
+#pragma unroll
+    for (int o = W / 2; o; o >>= 1) {
+        st.s += __shfl_xor_sync(0xffffffffu, st.s, o);
+        st.w += __shfl_xor_sync(0xffffffffu, st.w, o);
     }
+}
+
+// Over the CTA; every thread gets the sums.
+template <int THREADS>
+__device__ __forceinline__ void merge_cta(Stat& st, float c, Stat* sm) {
+    merge_lanes<32>(st, c);
+    if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = st;
     __syncthreads();
-    const int l = threadIdx.x & 31;
     constexpr int W = THREADS / 32;
-    st.m = l < W ? sm[l][0] : kNoMax;
-    st.s = l < W ? sm[l][1] : 0.f;
-    st.w = l < W ? sm[l][2] : 0.f;
-#pragma unroll
-    for (int o = W / 2; o; o >>= 1)
-        st.merge(__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.w, o), c);
-    st.m = __shfl_sync(0xffffffffu, st.m, 0);
-    st.s = __shfl_sync(0xffffffffu, st.s, 0);
-    st.w = __shfl_sync(0xffffffffu, st.w, 0);
+    st = sm[threadIdx.x & (W - 1)];
+    merge_lanes<W>(st, c);
 }
 
 // The CTA's k largest entries, in order, to best[0 .. k) (keys; 0 where there are fewer).  bv, bi: this
@@ -161,7 +225,7 @@ __device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int 
         g = other > g ? other : g;
     }
     if (threadIdx.x % kPer == 0) sm.group[threadIdx.x / kPer] = g;
-    if (threadIdx.x == 0) sm.count = 0;
+    if (threadIdx.x == 0) sm.count = sm.threads = 0;
     if (threadIdx.x < k) best[threadIdx.x] = 0;
     __syncthreads();
     if (threadIdx.x < kGroups) {
@@ -184,9 +248,13 @@ __device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int 
             if (at < kCandidates) sm.cand[at] = key;
         }
     };
-    if (any && most >= bound) {
-        if (threadIdx.x < sh.head) look(to_f32(sh.x[threadIdx.x]), threadIdx.x);
-        for (uint32_t i = threadIdx.x; i < sh.nvec; i += THREADS) {
+    if (any && most >= bound) sm.thread[atomicAdd(&sm.threads, 1)] = static_cast<uint16_t>(threadIdx.x);
+    __syncthreads();
+    // their vectors, dealt to all threads
+    const uint32_t found = sm.threads, each = (sh.nvec + THREADS - 1) / THREADS;
+    for (uint32_t e = threadIdx.x; e < found * each; e += THREADS) {
+        const uint32_t i = sm.thread[e / each] + (e % each) * THREADS;
+        if (i < sh.nvec) {
             Vec<T> v;
             v.raw = *sh.vec(i);
             float f[V];
@@ -194,8 +262,9 @@ __device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int 
 #pragma unroll
             for (int j = 0; j < V; ++j) look(f[j], sh.head + i * V + j);
         }
-        if (threadIdx.x < sh.n - sh.tail()) look(to_f32(sh.x[sh.tail() + threadIdx.x]), sh.tail() + threadIdx.x);
     }
+    if (threadIdx.x < sh.head) look(to_f32(sh.x[threadIdx.x]), threadIdx.x);
+    if (threadIdx.x < sh.n - sh.tail()) look(to_f32(sh.x[sh.tail() + threadIdx.x]), sh.tail() + threadIdx.x);
     __syncthreads();
     const int n = sm.count;
     if (n <= kCandidates) {
@@ -234,10 +303,10 @@ __device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int 
 }
 
 template <class T, class I, int THREADS, bool TOP, bool GRAD>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(LogprobArgs a, uint32_t split) {
+__global__ void __launch_bounds__(THREADS, kThreadsPerSm / THREADS) k_logprobs(LogprobArgs a, uint32_t split) {
     constexpr int V = Vec<T>::kN;
-    __shared__ float sm[THREADS / 32][3];
-    __shared__ float peer[kMaxSplit][3];
+    __shared__ Stat sm[THREADS / 32];
+    __shared__ Stat peer[kMaxSplit];  // the sums of every CTA of the cluster
     __shared__ typename std::conditional<TOP, TopSmem, int>::type top_sm;
     const uint32_t rank = split > 1 ? cluster_ctarank() : 0u;
     const float c = a.scale * kLog2e;
@@ -249,15 +318,18 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(LogprobArg
         const Share<T> sh(row, vocab, rank, split);
         const int64_t t = token_at(static_cast<const I*>(a.targets), r, a.vocab);
         const float xt = t >= 0 ? to_f32(row[t]) : 0.f;  // (early: its latency passes behind the row's)
-        Stat st = {kNoMax, 0.f, 0.f};
+        Stat st;
+        st.clear();
         float bv = -INFINITY;
         uint32_t bi = 0xffffffffu;
         if (threadIdx.x < sh.head) {
             const float v = to_f32(sh.x[threadIdx.x]);
-            if (v > st.m) st.m = v;
+            if (v > st.m) st.raise(v, c);
             st.add(v, c);
             if (TOP) bi = threadIdx.x, bv = v == v ? v : -INFINITY;
         }
+        Stat2 two = {st.m, pair(st.s, 0.f), pair(st.w, 0.f)};
+        const F2 c2 = pair(c, c);
         // kUnroll vectors in flight per thread; ALL: every one of them exists
         auto batch = [&](uint32_t i, auto all) {
             constexpr bool ALL = decltype(all)::value;
@@ -270,20 +342,35 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(LogprobArg
                     else v[q].raw = ld_stream(sh.vec(i + q * THREADS));
                 }
             float vm[kUnroll], most = -INFINITY;
+            if constexpr (TOP) {
 #pragma unroll
-            for (int q = 0; q < kUnroll; ++q)
-                if (ALL || i + q * THREADS < sh.nvec) {
-                    vm[q] = vec_max(v[q]);
-                    most = fmaxf(most, vm[q]);
-                }
-            if (most > st.m) st.raise(most, c);
+                for (int q = 0; q < kUnroll; ++q)
+                    if (ALL || i + q * THREADS < sh.nvec) {
+                        Largest<T> l;
+                        l.set(v[q]);
+                        vm[q] = l.value();
+                        most = fmaxf(most, vm[q]);
+                    }
+            } else {
+                Largest<T> l, o;
+                l.set(v[0]);
+#pragma unroll
+                for (int q = 1; q < kUnroll; ++q)
+                    if (ALL || i + q * THREADS < sh.nvec) {
+                        o.set(v[q]);
+                        l.take(o);
+                    }
+                most = l.value();
+            }
+            if (most > two.m) two.raise(most, c);
+            const F2 minus_m = pair(-two.m, -two.m);
 #pragma unroll
             for (int q = 0; q < kUnroll; ++q)
                 if (ALL || i + q * THREADS < sh.nvec) {
                     float f[V];
                     v[q].unpack(f);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) st.add(f[j], c);
+                    for (int j = 0; j < V; j += 2) two.add(f[j], f[j + 1], minus_m, c2);
                     if (TOP && (vm[q] > bv || bi == 0xffffffffu)) {
                         bv = fmaxf(vm[q], bv);
                         bi = sh.head + (i + q * THREADS) * V + V - 1;
@@ -293,6 +380,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(LogprobArg
         uint32_t i = threadIdx.x;
         for (; i + (kUnroll - 1) * THREADS < sh.nvec; i += kUnroll * THREADS) batch(i, std::true_type());
         if (i < sh.nvec) batch(i, std::false_type());
+        {
+            float a0, a1, b0, b1;
+            unpair(two.s, a0, a1);
+            unpair(two.w, b0, b1);
+            st = {two.m, a0 + a1, b0 + b1};
+        }
         if (threadIdx.x < sh.n - sh.tail()) {
             const float v = to_f32(sh.x[sh.tail() + threadIdx.x]);
             if (v > st.m) st.raise(v, c);
@@ -304,7 +397,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(LogprobArg
             if (!started) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
             started = true;
             if (threadIdx.x < split) {
-                const uint32_t at = mapa_shared(smem_u32(peer[rank]), threadIdx.x);
+                const uint32_t at = mapa_shared(smem_u32(peer + rank), threadIdx.x);
                 asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(st.m) : "memory");
                 asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(st.s) : "memory");
                 asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 8), "f"(st.w) : "memory");
@@ -320,13 +413,20 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(LogprobArg
         }
         if (split > 1) {
             cluster_sync();
-            st = {kNoMax, 0.f, 0.f};
-            for (uint32_t q = 0; q < split; ++q) st.merge(peer[q][0], peer[q][1], peer[q][2], c);
+            st.clear();
+            for (uint32_t q = 0; q < split; ++q) {
+                Stat o = peer[q];
+                const float m = fmaxf(st.m, o.m);
+                st.raise(m, c);
+                o.raise(m, c);
+                st.s += o.s, st.w += o.w;
+            }
         }
         const bool none = st.s == 0.f;  // every logit is -inf
         const float lns = logf(st.s), ent = none ? 0.f : lns - kLn2 * (st.w / st.s);
+        auto logp_of = [&](float x) { return none ? -INFINITY : fmaf(x - st.m, a.scale, -lns); };
         if (rank == 0 && threadIdx.x == 0) {
-            if (a.logp) a.logp[r] = t < 0 ? 0.f : none ? -INFINITY : (xt - st.m) * a.scale - lns;
+            if (a.logp) a.logp[r] = t < 0 ? 0.f : logp_of(xt);
             if (a.entropy) a.entropy[r] = ent;
             if (a.lse) a.lse[r] = none ? -INFINITY : fmaf(st.m, a.scale, lns);
         }
@@ -336,7 +436,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(LogprobArg
                     const uint32_t o = static_cast<uint32_t>(key >> 32);
                     const float v = key ? __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o) : NAN;
                     a.top_index[r * a.top + q] = key ? static_cast<int64_t>(static_cast<uint32_t>(~key)) : 0;
-                    a.top_logp[r * a.top + q] = none ? -INFINITY : (v - st.m) * a.scale - lns;
+                    a.top_logp[r * a.top + q] = logp_of(v);
                 };
                 if (split == 1) {
                     if (threadIdx.x < a.top) put(threadIdx.x, top_sm.best[0][threadIdx.x]);
@@ -358,41 +458,53 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(LogprobArg
         if constexpr (GRAD) {
             const float gl = (t >= 0 && !none && a.grad_logp) ? a.grad_logp[r] : 0.f;
             const float ge = (!none && a.grad_entropy) ? a.grad_entropy[r] : 0.f;
-            // scale (-gl p - ge p (ln p + entropy)) = p (A + B log2 p)
-            const float A = -a.scale * fmaf(ge, ent, gl), B = -a.scale * ge * kLn2, l2 = none ? 0.f : log2f(st.s), m = st.m;
+            // scale (-gl p - ge p (ln p + entropy)) = 2^d (A + B d)
+            const float inv = none ? 0.f : 1.f / st.s;
+            const float A = -a.scale * inv * (gl + ge * (ent - (none ? 0.f : lns))), B = -a.scale * inv * ge * kLn2;
             const float hot = gl * a.scale;
             T* out = static_cast<T*>(a.grad_logits) + r * a.ld_grad + sh.first;
             const uint32_t tt = t >= static_cast<int64_t>(sh.first) && t < static_cast<int64_t>(sh.first) + sh.n
                                     ? static_cast<uint32_t>(t) - sh.first : 0xffffffffu;
-            auto grad = [&](float x) {
-                const float lp = cut(fmaf(x - m, c, -l2)), p = ex2(lp);
-                return p * fmaf(B, lp, A);
-            };
             const bool vec_out = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(sh.x)) & 15u) == 0;
-            if (threadIdx.x < sh.head) out[threadIdx.x] = from_f32<T>(grad(to_f32(sh.x[threadIdx.x])) + (threadIdx.x == tt ? hot : 0.f));
-#pragma unroll 2
-            for (uint32_t v = threadIdx.x; v < sh.nvec; v += THREADS) {
-                Vec<T> x;
-                x.raw = *sh.vec(v);
-                float f[V];
-                x.unpack(f);
-                const uint32_t at = sh.head + v * V, hit = tt - at;
+            const F2 A2 = pair(A, A), B2 = pair(B, B), minus_m = pair(-st.m, -st.m);
+            auto grad = [&](float x) {
+                const float d = cut((x - st.m) * c);
+                return ex2(d) * fmaf(B, d, A);
+            };
+            // (a NaN among the gradients or logits spreads by itself)
+            if (threadIdx.x < sh.head) out[threadIdx.x] = from_f32<T>(grad(to_f32(sh.x[threadIdx.x])));
+            auto body = [&](auto vector_out) {
+                T* o = out + sh.head;
+#pragma unroll 4
+                for (uint32_t v = threadIdx.x; v < sh.nvec; v += THREADS) {
+                    Vec<T> x;
+                    x.raw = *sh.vec(v);
+                    float f[V];
+                    x.unpack(f);
 #pragma unroll
-                for (int j = 0; j < V; ++j) f[j] = grad(f[j]);
-                if (hit < V) {
+                    for (int j = 0; j < V; j += 2) {
+                        float d0, d1;
+                        const F2 d = exponents(f[j], f[j + 1], minus_m, c2, d0, d1);
+                        unpair(mul2(pair(ex2(d0), ex2(d1)), fma2(B2, d, A2)), f[j], f[j + 1]);
+                    }
+                    if constexpr (decltype(vector_out)::value) {
+                        x.pack(f);
+                        st_stream(o + v * V, x.raw);
+                    } else {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) f[j] += static_cast<uint32_t>(j) == hit ? hot : 0.f;
+                        for (int j = 0; j < V; ++j) o[v * V + j] = from_f32<T>(f[j]);
+                    }
                 }
-                if (vec_out) {
-                    x.pack(f);
-                    st_stream(out + at, x.raw);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) out[at + j] = from_f32<T>(f[j]);
-                }
-            }
+            };
+            if (vec_out) body(std::true_type());
+            else body(std::false_type());
             const uint32_t e = sh.tail() + threadIdx.x;
-            if (e < sh.n) out[e] = from_f32<T>(grad(to_f32(sh.x[e])) + (e == tt ? hot : 0.f));
+            if (e < sh.n) out[e] = from_f32<T>(grad(to_f32(sh.x[e])));
+            // the target's entry once more, with its own term, by the thread that wrote it
+            if (tt != 0xffffffffu) {
+                const uint32_t by = tt < sh.head ? tt : tt < sh.tail() ? (tt - sh.head) / V % THREADS : tt - sh.tail();
+                if (threadIdx.x == by) out[tt] = from_f32<T>(grad(xt) + hot);
+            }
         }
         // the next row's sums overwrite shared memory that this row's threads (and CTAs) may still read
         if (r + gridDim.x / split < a.rows) {
@@ -462,7 +574,8 @@ cudaError_t run(const LogprobArgs& a, cudaStream_t st) {
 #define ROWS(N)                                                                                   \
     (a.grad_logits ? (a.top ? launch_rows<T, I, N, true, true>(a, sms, st) : launch_rows<T, I, N, false, true>(a, sms, st)) \
                    : (a.top ? launch_rows<T, I, N, true, false>(a, sms, st) : launch_rows<T, I, N, false, false>(a, sms, st)))
-    return a.vocab <= 4096 ? ROWS(128) : ROWS(512);
+    // (a short row is a few vectors per thread: more rows at once instead)
+    return a.vocab <= 4096 ? ROWS(128) : ROWS(256);
 #undef ROWS
 }
 
