@@ -19,8 +19,10 @@ namespace {
 
 constexpr int kClipThreads = 256;
 constexpr int kMaxTensors = 512;       // of one table: 512 x 32 bytes of kernel parameters
+constexpr int kFewTensors = 32;        // a short list's parameters are a 16th of that (launch and first reads)
 constexpr int kChunkBytes = 32768;     // a CTA's unit of work: 8 16-byte loads per thread
 constexpr int kCtasPerSm = 8;
+constexpr int kKeepChunks = 2048;      // the last 64 MB stay in L2 for the scaling, which begins with them
 
 struct ClipTensor {
     const void* in;
@@ -30,8 +32,9 @@ struct ClipTensor {
     int32_t first;  // chunk number of its first chunk
 };
 
+template <int N>
 struct ClipTable {
-    ClipTensor t[kMaxTensors];
+    ClipTensor t[N];
     int count;
     int chunks;
 };
@@ -54,7 +57,8 @@ __device__ __forceinline__ ChunkSpan chunk_span(const ClipTensor& t, int c) {
     return s;
 }
 
-__device__ __forceinline__ int find_tensor(const ClipTable& tab, int chunk) {
+template <int N>
+__device__ __forceinline__ int find_tensor(const ClipTable<N>& tab, int chunk) {
     int lo = 0, hi = tab.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -65,7 +69,7 @@ __device__ __forceinline__ int find_tensor(const ClipTable& tab, int chunk) {
 }
 
 template <class T>
-__device__ __forceinline__ float chunk_squares(const ClipTensor& t, int c) {
+__device__ __forceinline__ float chunk_squares(const ClipTensor& t, int c, bool keep) {
     const ChunkSpan s = chunk_span<T>(t, c);
     const T* p = static_cast<const T*>(t.in);
     constexpr int V = Vec<T>::kN;
@@ -79,7 +83,7 @@ __device__ __forceinline__ float chunk_squares(const ClipTensor& t, int c) {
 #pragma unroll 8
     for (int64_t i = threadIdx.x; i < nvec; i += kClipThreads) {
         Vec<T> v;
-        v.raw = __ldg(reinterpret_cast<const uint4*>(q + i * V));
+        v.raw = keep ? __ldg(reinterpret_cast<const uint4*>(q + i * V)) : ld_stream(q + i * V);
         float f[V];
         v.unpack(f);
 #pragma unroll
@@ -131,25 +135,46 @@ __device__ __forceinline__ double cta_sum(double v) {
     return s;
 }
 
-__global__ void __launch_bounds__(kClipThreads) k_grad_squares(const __grid_constant__ ClipTable tab, double* part) {
+template <int N>
+__global__ void __launch_bounds__(kClipThreads) k_grad_squares(const __grid_constant__ ClipTable<N> tab, double* part) {
+    next_may_start();
     double acc = 0.0;
     for (int c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
         const ClipTensor& t = tab.t[find_tensor(tab, c)];
         const int k = c - t.first;
-        const float s = t.dtype == ISOLOCO_F32 ? chunk_squares<float>(t, k)
-                        : t.dtype == ISOLOCO_BF16 ? chunk_squares<__nv_bfloat16>(t, k) : chunk_squares<__half>(t, k);
+        const bool keep = tab.chunks - c <= kKeepChunks;
+        const float s = t.dtype == ISOLOCO_F32 ? chunk_squares<float>(t, k, keep)
+                        : t.dtype == ISOLOCO_BF16 ? chunk_squares<__nv_bfloat16>(t, k, keep) : chunk_squares<__half>(t, k, keep);
         acc += static_cast<double>(s);
     }
     const double s = cta_sum(acc);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
+// The norm from the partials, the same bits in every thread of every CTA.  (fp64 is slow here: warps without
+// partials add nothing, and the root is fp32's, of a sum brought into its range.)
+__device__ __forceinline__ float norm_of(const double* part, int nparts) {
+    __shared__ double sum[kClipThreads / 32];
+    const int warp = threadIdx.x >> 5, warps = min(kClipThreads / 32, (nparts + 31) / 32);
+    if (warp < warps) {
+        double s = 0.0;
+        for (int i = threadIdx.x; i < nparts; i += kClipThreads) s += part[i];
+#pragma unroll
+        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if ((threadIdx.x & 31) == 0) sum[warp] = s;
+    }
+    __syncthreads();
+    double s = warps ? sum[0] : 0.0;
+    for (int i = 1; i < warps; ++i) s += sum[i];
+    return s > 1e30 ? sqrtf(static_cast<float>(s * 0x1p-64)) * 0x1p32f : sqrtf(static_cast<float>(s));
+}
+
 // tab.chunks == 0: the norm only.
-__global__ void __launch_bounds__(kClipThreads) k_grad_scale(const __grid_constant__ ClipTable tab, const double* part,
+template <int N>
+__global__ void __launch_bounds__(kClipThreads) k_grad_scale(const __grid_constant__ ClipTable<N> tab, const double* part,
                                                              int nparts, float max_norm, bool in_place, float* norm) {
-    double s = 0.0;
-    for (int i = threadIdx.x; i < nparts; i += kClipThreads) s += part[i];
-    const float n = static_cast<float>(sqrt(cta_sum(s)));
+    after_previous();
+    const float n = norm_of(part, nparts);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = n;
     // a norm that is not finite, or zero, scales nothing
     const float coef = (n > max_norm && n < INFINITY) ? max_norm / n : 1.f;
@@ -180,51 +205,65 @@ int64_t grad_norm_workspace(int count) {
     return tables * 1024 * kCtasPerSm * static_cast<int64_t>(sizeof(double));
 }
 
+namespace {
+
+// Fills `tab` with the tensors from `i` on that have entries; returns the next one's place.
+template <int N>
+int fill_table(ClipTable<N>& tab, const isoloco_tensor_t* in, const isoloco_tensor_t* out, int i, int count) {
+    tab.count = tab.chunks = 0;
+    for (; i < count && tab.count < N; ++i) {
+        if (in[i].n == 0) continue;
+        ClipTensor& t = tab.t[tab.count++];
+        t.in = in[i].data;
+        t.out = out ? out[i].data : in[i].data;
+        t.n = in[i].n;
+        t.dtype = in[i].dtype;
+        t.first = tab.chunks;
+        tab.chunks += chunks_of(in[i]);  // (below 2^21 each: lengths are at most 2^33)
+    }
+    return i;
+}
+
+template <int N>
+cudaError_t clip_n(const isoloco_tensor_t* in, const isoloco_tensor_t* out, int count, bool clip, float max_norm, float* norm, double* part,
+                   int max_grid, cudaStream_t st) {
+    int nparts = 0;
+    cudaError_t e = cudaSuccess;
+    ClipTable<N> tab;
+    for (int i = 0; i < count;) {
+        i = fill_table(tab, in, out, i, count);
+        if (!tab.count) continue;
+        const int grid = std::min(tab.chunks, max_grid);
+        k_grad_squares<N><<<grid, kClipThreads, 0, st>>>(tab, part + nparts);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        nparts += grid;
+    }
+    const double* sums = part;
+    bool written = false;
+    for (int i = 0; clip && i < count;) {
+        if (count > N || i > 0) i = fill_table(tab, in, out, i, count);  // (one table: it is the squares')
+        else i = count;
+        if (!tab.count) continue;
+        const int grid = std::min(tab.chunks, max_grid);
+        if ((e = launch_next(k_grad_scale<N>, grid, kClipThreads, st, tab, sums, nparts, max_norm, out == nullptr, norm)) != cudaSuccess) return e;
+        written = true;
+    }
+    if (written) return e;
+    tab.count = tab.chunks = 0;
+    return launch_next(k_grad_scale<N>, 1, kClipThreads, st, tab, sums, nparts, 0.f, true, norm);
+}
+
+}  // namespace
+
 cudaError_t launch_clip(const isoloco_tensor_t* in, const isoloco_tensor_t* out, int count, bool clip, float max_norm,
                         float* norm, void* ws, cudaStream_t st) {
     int sms = 0;
-    cudaError_t e = device_sms(&sms);
+    const cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;
-    double* part = static_cast<double*>(ws);
-    int nparts = 0;
     const int max_grid = std::min(1024, sms) * kCtasPerSm;
-    // pass 0 the squares, pass 1 the scaling
-    for (int pass = 0; pass < (clip ? 2 : 1); ++pass) {
-        for (int first = 0; first < count;) {
-            ClipTable tab;
-            tab.count = 0;
-            tab.chunks = 0;
-            int i = first;
-            for (; i < count && tab.count < kMaxTensors; ++i) {
-                if (in[i].n == 0) continue;
-                const int c = chunks_of(in[i]);
-                ClipTensor& t = tab.t[tab.count++];
-                t.in = in[i].data;
-                t.out = out ? out[i].data : in[i].data;
-                t.n = in[i].n;
-                t.dtype = in[i].dtype;
-                t.first = tab.chunks;
-                tab.chunks += c;
-            }
-            first = i;
-            if (!tab.count) continue;
-            const int grid = std::min(tab.chunks, max_grid);
-            if (pass == 0) {
-                k_grad_squares<<<grid, kClipThreads, 0, st>>>(tab, part + nparts);
-                nparts += grid;
-            } else {
-                k_grad_scale<<<grid, kClipThreads, 0, st>>>(tab, part, nparts, max_norm, out == nullptr, norm);
-            }
-            if ((e = cudaGetLastError()) != cudaSuccess) return e;
-        }
-    }
-    if (!clip || nparts == 0) {
-        ClipTable none;
-        none.count = none.chunks = 0;
-        k_grad_scale<<<1, kClipThreads, 0, st>>>(none, part, nparts, 0.f, true, norm);
-        e = cudaGetLastError();
-    }
-    return e;
+    double* part = static_cast<double*>(ws);
+    return count <= kFewTensors ? clip_n<kFewTensors>(in, out, count, clip, max_norm, norm, part, max_grid, st)
+                                : clip_n<kMaxTensors>(in, out, count, clip, max_norm, norm, part, max_grid, st);
 }
 
 }  // namespace isoloco

@@ -5,10 +5,10 @@
 // The gradient sorts the positions by token id (stable least-significant-digit radix sort in one
 // thread-block cluster), so that a row's terms stand together, in the order of their positions:
 //   k_embed_sort   cluster 0 sorts; the other CTAs meanwhile write the zeros of every row of dW.
-//   k_embed_sum    a CTA adds kSpan consecutive sorted positions, in fp32, all columns; a row whose
-//                  positions lie within one span is written at once, the sums at a span's ends
-//                  that belong to a row shared with other spans go to the workspace.
-//   k_embed_join   adds those, span by span in order, and writes their rows.
+//   k_embed_sum    a CTA adds a span of consecutive sorted positions in fp32.  A row whose positions lie in one
+//                  span, or in two neighbouring ones, is added by the CTA it begins in and written at
+//                  once; what each span adds to a row that lies in three or more goes to the workspace.
+//   k_embed_join   adds those shares in the order of their spans and writes their rows.
 // Which terms are added in which order depends on the ids alone.
 #include <algorithm>
 
@@ -23,30 +23,53 @@ namespace {
 constexpr int kRowThreads = 128;
 
 // ------------------------------------------------------------------ lookup
-// One row of y per CTA and step; 16 bytes per access when VEC.
-template <class T, class I, bool VEC>
-__global__ void __launch_bounds__(kRowThreads) k_embed(const T* __restrict__ w, int64_t ld_w, int64_t vocab, int64_t width,
-                                                       const I* __restrict__ ids, int64_t tokens, float scale,
-                                                       T* __restrict__ y, int64_t ld_y) {
+// Pieces (16 bytes when VEC, else one element) of all rows of y in one sequence; a thread takes N of them,
+// kLookThreads apart, so that N rows' ids and then N pieces of the table are in flight.
+constexpr int kLookThreads = 256;
+
+template <class T, class I, bool VEC, int N>
+__global__ void __launch_bounds__(kLookThreads) k_embed(const T* __restrict__ w, int64_t ld_w, int64_t vocab, uint32_t pieces,
+                                                        const I* __restrict__ ids, int64_t tokens, float scale, T* __restrict__ y,
+                                                        int64_t ld_y) {
     constexpr int V = VEC ? Vec<T>::kN : 1;
-    const int64_t c = (static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x) * V;
-    if (c >= width) return;
-    for (int64_t t = blockIdx.y; t < tokens; t += gridDim.y) {
-        const int64_t id = token_at(ids, t, vocab);
-        if constexpr (VEC) {
-            Vec<T> v;
-            v.raw = make_uint4(0, 0, 0, 0);
-            if (id >= 0) {
-                v.raw = __ldg(reinterpret_cast<const uint4*>(w + id * ld_w + c));
-                float f[V];
-                v.unpack(f);
+    const int64_t total = tokens * pieces;
+    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * (kLookThreads * N) + threadIdx.x; i0 < total;
+         i0 += static_cast<int64_t>(gridDim.x) * (kLookThreads * N)) {
+        int64_t t[N], id[N];
+        uint32_t c[N];
 #pragma unroll
-                for (int j = 0; j < V; ++j) f[j] *= scale;
-                v.pack(f);
+        for (int q = 0; q < N; ++q) {
+            const int64_t i = min(i0 + q * kLookThreads, total - 1);
+            t[q] = total <= 0xffffffffll ? static_cast<int64_t>(static_cast<uint32_t>(i) / pieces) : i / pieces;
+            c[q] = static_cast<uint32_t>(i - t[q] * pieces) * V;
+            id[q] = token_at(ids, t[q], vocab);
+        }
+        if constexpr (VEC) {
+            Vec<T> v[N];
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                v[q].raw = make_uint4(0, 0, 0, 0);
+                if (id[q] >= 0) v[q].raw = __ldg(reinterpret_cast<const uint4*>(w + id[q] * ld_w + c[q]));
             }
-            *reinterpret_cast<uint4*>(y + t * ld_y + c) = v.raw;
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                if (i0 + q * kLookThreads >= total) break;
+                if (scale != 1.f && id[q] >= 0) {
+                    float f[V];
+                    v[q].unpack(f);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) f[j] *= scale;
+                    v[q].pack(f);
+                }
+                st_stream(y + t[q] * ld_y + c[q], v[q].raw);
+            }
         } else {
-            y[t * ld_y + c] = id >= 0 ? from_f32<T>(to_f32(w[id * ld_w + c]) * scale) : from_f32<T>(0.f);
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                if (i0 + q * kLookThreads >= total) break;
+                const T v = id[q] >= 0 ? w[id[q] * ld_w + c[q]] : from_f32<T>(0.f);
+                y[t[q] * ld_y + c[q]] = scale == 1.f || id[q] < 0 ? v : from_f32<T>(to_f32(v) * scale);
+            }
         }
     }
 }
@@ -74,7 +97,7 @@ __device__ __forceinline__ SortRange sort_range(int64_t n, uint32_t rank, int wa
 }
 
 template <class I>
-__device__ void sort_ids(SortSmem& sm, const I* ids, int64_t n, int64_t vocab, int bits, uint32_t* key[2], uint32_t* pos[2]) {
+__device__ __forceinline__ void sort_ids(SortSmem& sm, const I* ids, int64_t n, int64_t vocab, int bits, uint32_t* key[2], uint32_t* pos[2]) {
     const uint32_t rank = cluster_ctarank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const SortRange rg = sort_range(n, rank, warp);
@@ -162,10 +185,12 @@ __device__ void sort_ids(SortSmem& sm, const I* ids, int64_t n, int64_t vocab, i
 template <class I>
 __global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThreads)
     k_embed_sort(const I* ids, int64_t n, int64_t vocab, int bits, uint32_t* k0, uint32_t* k1, uint32_t* p0, uint32_t* p1,
-                 uint8_t* dw, int64_t row_bytes, int64_t ld_bytes) {
+                 uint32_t* nchains, uint8_t* dw, int64_t row_bytes, int64_t ld_bytes) {
     __shared__ SortSmem sm;
+    next_may_start();
     const int64_t cta = static_cast<int64_t>(blockIdx.x) - kSortCluster;
     if (cta < 0) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) *nchains = 0;
         uint32_t* key[2] = {k0, k1};
         uint32_t* pos[2] = {p0, p1};
         sort_ids(sm, ids, n, vocab, bits, key, pos);
@@ -187,132 +212,208 @@ __global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThre
 }
 
 // ------------------------------------------------------------------ sums
-constexpr int kSpan = 32;  // sorted positions of one CTA
+constexpr int kMaxSpan = 32;  // sorted positions of one CTA, at most (its last row's may be as many more)
+constexpr int kBatch = 8;     // rows of dy in flight per thread
 
-// part[span][0]: the sum of the span's first row, if that row began in an earlier span;
-// part[span][1]: of its last row, if that goes on in a later span (and began here).
+// chains: the spans in which a row begins that lies in three spans or more (in any order); part[span][1] is its
+// sum there, part[s][0] its sum in each of the later spans s.
 template <class T, class O, bool VEC>
 __global__ void __launch_bounds__(kRowThreads) k_embed_sum(const T* __restrict__ dy, int64_t ld_dy, int64_t vocab, int64_t width,
                                                            const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
-                                                           int64_t n, float scale, O* __restrict__ dw, int64_t ld_dw,
-                                                           float* __restrict__ part) {
+                                                           int64_t n, int len, float scale, O* __restrict__ dw, int64_t ld_dw,
+                                                           float* __restrict__ part, uint32_t* nchains,
+                                                           uint32_t* __restrict__ chains) {
     constexpr int V = VEC ? Vec<T>::kN : 1;
-    __shared__ uint32_t sk[kSpan + 2];  // keys from one before the span to one behind it
-    __shared__ uint32_t sp[kSpan];
-    const int64_t span = blockIdx.x;
-    const int64_t first = span * kSpan;
-    const int cnt = static_cast<int>(min(static_cast<int64_t>(kSpan), n - first));
-    for (int i = threadIdx.x; i < cnt + 2; i += kRowThreads) {
-        const int64_t j = first + i - 1;
-        sk[i] = (j >= 0 && j < n) ? key[j] : 0xffffffffu;
-    }
-    for (int i = threadIdx.x; i < cnt; i += kRowThreads) sp[i] = pos[first + i];
+    __shared__ uint32_t sk[2 * kMaxSpan + 2];  // keys from one before the span to one behind the next
+    __shared__ uint32_t sp[2 * kMaxSpan];
+    after_previous();
+    const int64_t span = blockIdx.x, first = span * len;
+    auto key_at = [&](int64_t j) { return j >= 0 && j < n ? key[j] : 0xffffffffu; };
+    for (int i = threadIdx.x; i < 2 * len + 2; i += kRowThreads) sk[i] = key_at(first + i - 1);
+    for (int i = threadIdx.x; i < 2 * len; i += kRowThreads) sp[i] = first + i < n ? pos[first + i] : 0u;
+    const uint32_t before = key_at(first - len - 1);
     __syncthreads();
     const int64_t c = (static_cast<int64_t>(blockIdx.y) * kRowThreads + threadIdx.x) * V;
     if (c >= width) return;
+    // positions [from, to) are added here: without the end of a row that the span before adds as a whole, with
+    // the rest of a row that begins here and ends in the next span
+    const int cnt = static_cast<int>(min(static_cast<int64_t>(len), n - first));
+    int from = 0, to = cnt;
+    bool shared = sk[0] == sk[1];  // the first row began in an earlier span, and its share here is one of many
+    if (shared && before != sk[1] && sk[len + 1] != sk[1]) {
+        shared = false;
+        while (from < cnt && sk[from + 1] == sk[1]) ++from;
+    }
+    const uint32_t end_key = sk[cnt];
+    if (sk[cnt + 1] == end_key && sk[0] != end_key && sk[2 * len + 1] != end_key)
+        while (sk[to + 1] == end_key) ++to;  // (ends by sk[2 len + 1])
     float acc[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[j] = 0.f;
-    int begin = 0;  // of the row being added
-    for (int i = 0; i < cnt; ++i) {
-        const uint32_t k = sk[i + 1];
-        if (k >= vocab) break;  // no token, nor are the later ones
-        const T* src = dy + static_cast<int64_t>(sp[i]) * ld_dy + c;
-        if constexpr (VEC) {
-            Vec<T> v;
-            v.raw = ld_stream(src);
-            float f[V];
-            v.unpack(f);
+    for (int i0 = from; i0 < to; i0 += kBatch) {
+        Vec<T> v[kBatch];
+        T one[kBatch];
 #pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] += f[j];
-        } else {
-            acc[0] += to_f32(src[0]);
-        }
-        const bool last = i + 1 == cnt;
-        if (!last && sk[i + 2] == k) continue;
-        const bool open_left = begin == 0 && sk[0] == k;
-        const bool open_right = last && sk[i + 2] == k;
-        if (open_left || open_right) {
-            float* d = part + (span * 2 + (open_left ? 0 : 1)) * width + c;
-#pragma unroll
-            for (int j = 0; j < V; ++j) d[j] = acc[j];
-        } else {
-            O* d = dw + static_cast<int64_t>(k) * ld_dw + c;
-#pragma unroll
-            for (int j = 0; j < V; ++j) d[j] = from_f32<O>(acc[j] * scale);
+        for (int q = 0; q < kBatch; ++q) {
+            if (i0 + q >= to || sk[i0 + q + 1] >= vocab) continue;  // (no token sorts last)
+            const T* src = dy + static_cast<int64_t>(sp[i0 + q]) * ld_dy + c;
+            if constexpr (VEC) v[q].raw = ld_stream(src);
+            else one[q] = src[0];
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] = 0.f;
-        begin = i + 1;
+        for (int q = 0; q < kBatch; ++q) {
+            const int i = i0 + q;
+            if (i >= to) break;
+            const uint32_t k = sk[i + 1];
+            if (k >= vocab) break;
+            if constexpr (VEC) {
+                float f[V];
+                v[q].unpack(f);
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] += f[j];
+            } else {
+                acc[0] += to_f32(one[q]);
+            }
+            const bool last = i + 1 == to, goes_on = sk[i + 2] == k;
+            if (!last && goes_on) continue;
+            if (shared || goes_on) {
+                if (!shared && blockIdx.y == 0 && threadIdx.x == 0) chains[atomicAdd(nchains, 1u)] = static_cast<uint32_t>(span);
+                float* d = part + (span * 2 + (shared ? 0 : 1)) * width + c;
+#pragma unroll
+                for (int j = 0; j < V; ++j) d[j] = acc[j];
+            } else {
+                O* d = dw + static_cast<int64_t>(k) * ld_dw + c;
+                bool whole = false;  // 16 bytes at once where the output's type and address allow
+                if constexpr (VEC && sizeof(O) == sizeof(T)) {
+                    whole = (reinterpret_cast<uintptr_t>(d) & 15u) == 0;
+                    if (whole) {
+                        float f[V];
+#pragma unroll
+                        for (int j = 0; j < V; ++j) f[j] = acc[j] * scale;
+                        Vec<O> w;
+                        w.pack(f);
+                        *reinterpret_cast<uint4*>(d) = w.raw;
+                    }
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) d[j] = from_f32<O>(acc[j] * scale);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] = 0.f;
+            shared = false;
+        }
     }
 }
 
-// Rows that begin in span blockIdx.x and go on in later ones.
+// Rows that lie in many spans (a frequent token's in hundreds): kJoinCols columns of one of them per CTA step,
+// its spans in kJoinParts runs, each added by a group of threads.
+constexpr int kJoinCols = 128, kJoinParts = 4, kJoinThreads = kJoinCols * kJoinParts;
+
 template <class O>
-__global__ void __launch_bounds__(kRowThreads) k_embed_join(int64_t vocab, int64_t width, const uint32_t* __restrict__ key, int64_t n,
-                                                            float scale, O* __restrict__ dw, int64_t ld_dw,
-                                                            const float* __restrict__ part) {
-    const int64_t span = blockIdx.x, first = span * kSpan, next = first + kSpan;
-    if (next >= n) return;
-    const uint32_t k = key[next - 1];
-    if (k >= vocab || key[next] != k) return;       // nothing goes on behind this span
-    if (first > 0 && key[first - 1] == k) return;   // it began earlier
-    const int64_t c = static_cast<int64_t>(blockIdx.y) * kRowThreads + threadIdx.x;
-    if (c >= width) return;
-    float acc = part[(span * 2 + 1) * width + c];
-    for (int64_t s = span + 1; s * kSpan < n && key[s * kSpan] == k; ++s) acc += part[s * 2 * width + c];
-    dw[static_cast<int64_t>(k) * ld_dw + c] = from_f32<O>(acc * scale);
+__global__ void __launch_bounds__(kJoinThreads) k_embed_join(int64_t width, const uint32_t* __restrict__ key, int64_t n, int len,
+                                                             float scale, O* __restrict__ dw, int64_t ld_dw,
+                                                             const float* __restrict__ part, const uint32_t* nchains,
+                                                             const uint32_t* __restrict__ chains) {
+    __shared__ float sum[kJoinParts][kJoinCols];
+    after_previous();
+    const uint32_t blocks = static_cast<uint32_t>((width + kJoinCols - 1) / kJoinCols);
+    const int64_t items = static_cast<int64_t>(*nchains) * blocks;
+    const int run = threadIdx.x / kJoinCols, col = threadIdx.x % kJoinCols;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t span = chains[item / blocks], c = item % blocks * kJoinCols + col;
+        const uint32_t k = key[(span + 1) * len];
+        // later spans that begin with this row's key
+        int64_t more = 0;
+        for (;;) {
+            const int64_t at = (span + 1 + more + threadIdx.x) * len;
+            const int got = __syncthreads_count(at < n && key[at] == k);
+            more += got;
+            if (got < kJoinThreads) break;
+        }
+        const int64_t each = (more + kJoinParts - 1) / kJoinParts;
+        const int64_t lo = span + 1 + min(more, run * each), hi = span + 1 + min(more, (run + 1) * each);
+        float acc = 0.f;
+        if (c < width) {
+            if (run == 0) acc = part[(span * 2 + 1) * width + c];
+#pragma unroll 8
+            for (int64_t s = lo; s < hi; ++s) acc += part[s * 2 * width + c];
+        }
+        sum[run][col] = acc;
+        __syncthreads();
+        if (run == 0 && c < width) {
+#pragma unroll
+            for (int q = 1; q < kJoinParts; ++q) acc += sum[q][col];
+            dw[static_cast<int64_t>(k) * ld_dw + c] = from_f32<O>(acc * scale);
+        }
+        __syncthreads();
+    }
 }
 
-inline unsigned rows_grid(int64_t rows) { return static_cast<unsigned>(std::min<int64_t>(rows, 65535)); }
+template <class T, class I, bool VEC, int N>
+cudaError_t embed_n(const void* w, int64_t ld_w, int64_t vocab, int64_t pieces, const void* ids, int64_t tokens, float scale, void* y,
+                    int64_t ld_y, cudaStream_t st) {
+    const int64_t blocks = (tokens * pieces + kLookThreads * N - 1) / (kLookThreads * N);
+    k_embed<T, I, VEC, N><<<static_cast<unsigned>(std::min<int64_t>(blocks, int64_t(1) << 30)), kLookThreads, 0, st>>>(
+        static_cast<const T*>(w), ld_w, vocab, static_cast<uint32_t>(pieces), static_cast<const I*>(ids), tokens, scale, static_cast<T*>(y),
+        ld_y);
+    return cudaGetLastError();
+}
 
 template <class T, class I>
 cudaError_t embed_t(const void* w, int64_t ld_w, int64_t vocab, int64_t width, const void* ids, int64_t tokens, float scale,
                     void* y, int64_t ld_y, cudaStream_t st) {
     constexpr int64_t V = Vec<T>::kN;
+    int sms = 0;
+    const cudaError_t e = device_sms(&sms);
+    if (e != cudaSuccess) return e;
     const bool vec = aligned16(w) && aligned16(y) && ld_w % V == 0 && ld_y % V == 0 && width % V == 0;
-    const int64_t cols = vec ? width / V : width;
-    const dim3 grid(static_cast<unsigned>((cols + kRowThreads - 1) / kRowThreads), rows_grid(tokens));
-    if (vec)
-        k_embed<T, I, true><<<grid, kRowThreads, 0, st>>>(static_cast<const T*>(w), ld_w, vocab, width,
-                                                          static_cast<const I*>(ids), tokens, scale, static_cast<T*>(y), ld_y);
-    else
-        k_embed<T, I, false><<<grid, kRowThreads, 0, st>>>(static_cast<const T*>(w), ld_w, vocab, width,
-                                                           static_cast<const I*>(ids), tokens, scale, static_cast<T*>(y), ld_y);
-    return cudaGetLastError();
+    const int64_t pieces = vec ? width / V : width;
+    // four pieces per thread once that still leaves every SM a few CTAs
+    const bool many = tokens * pieces >= int64_t(4) * 4 * kLookThreads * sms;
+#define LOOK(VEC, N) embed_n<T, I, VEC, N>(w, ld_w, vocab, pieces, ids, tokens, scale, y, ld_y, st)
+    return vec ? (many ? LOOK(true, 4) : LOOK(true, 1)) : (many ? LOOK(false, 4) : LOOK(false, 1));
+#undef LOOK
 }
 
+// Positions per CTA of k_embed_sum: a short batch is cut finer, so that every SM has a few CTAs; a long one
+// leaves less at the spans' ends.
+int span_of(int64_t tokens) { return tokens <= 16384 ? 16 : kMaxSpan; }
+
 struct EmbedWs {
-    uint32_t *k0, *k1, *p0, *p1;
+    uint32_t *k0, *k1, *p0, *p1, *nchains, *chains;
     float* part;
 };
 
 int64_t r16(int64_t b) { return (b + 15) / 16 * 16; }
 
 EmbedWs embed_ws(void* ws, int64_t tokens) {
-    uint8_t* p = static_cast<uint8_t*>(ws);
-    const int64_t s = r16(4 * tokens);
-    return {reinterpret_cast<uint32_t*>(p), reinterpret_cast<uint32_t*>(p + s), reinterpret_cast<uint32_t*>(p + 2 * s),
-            reinterpret_cast<uint32_t*>(p + 3 * s), reinterpret_cast<float*>(p + 4 * s)};
+    uint32_t* p = static_cast<uint32_t*>(ws);
+    const int64_t s = r16(4 * tokens) / 4, spans = (tokens + span_of(tokens) - 1) / span_of(tokens);
+    return {p, p + s, p + 2 * s, p + 3 * s, p + 4 * s, p + 4 * s + 4, reinterpret_cast<float*>(p + 4 * s + 4 + r16(4 * spans) / 4)};
 }
 
 template <class T, class O>
 cudaError_t embed_grad_t(const void* dy, int64_t ld_dy, int64_t vocab, int64_t width, const EmbedWs& w, int64_t n, float scale,
-                         void* dw, int64_t ld_dw, cudaStream_t st) {
+                         void* dw, int64_t ld_dw, int sms, cudaStream_t st) {
     constexpr int64_t V = Vec<T>::kN;
     const bool vec = aligned16(dy) && ld_dy % V == 0 && width % V == 0;
     const int64_t cols = vec ? width / V : width;
-    const unsigned spans = static_cast<unsigned>((n + kSpan - 1) / kSpan);
+    const int len = span_of(n);
+    const unsigned spans = static_cast<unsigned>((n + len - 1) / len);
     const dim3 grid(spans, static_cast<unsigned>((cols + kRowThreads - 1) / kRowThreads));
+    cudaError_t e;
     if (vec)
-        k_embed_sum<T, O, true><<<grid, kRowThreads, 0, st>>>(static_cast<const T*>(dy), ld_dy, vocab, width, w.k1, w.p1, n, scale,
-                                                              static_cast<O*>(dw), ld_dw, w.part);
+        e = launch_next(k_embed_sum<T, O, true>, grid, kRowThreads, st, static_cast<const T*>(dy), ld_dy, vocab, width,
+                        static_cast<const uint32_t*>(w.k1), static_cast<const uint32_t*>(w.p1), n, len, scale, static_cast<O*>(dw), ld_dw, w.part, w.nchains, w.chains);
     else
-        k_embed_sum<T, O, false><<<grid, kRowThreads, 0, st>>>(static_cast<const T*>(dy), ld_dy, vocab, width, w.k1, w.p1, n, scale,
-                                                               static_cast<O*>(dw), ld_dw, w.part);
-    const dim3 jgrid(spans, static_cast<unsigned>((width + kRowThreads - 1) / kRowThreads));
-    k_embed_join<O><<<jgrid, kRowThreads, 0, st>>>(vocab, width, w.k1, n, scale, static_cast<O*>(dw), ld_dw, w.part);
-    return cudaGetLastError();
+        e = launch_next(k_embed_sum<T, O, false>, grid, kRowThreads, st, static_cast<const T*>(dy), ld_dy, vocab, width,
+                        static_cast<const uint32_t*>(w.k1), static_cast<const uint32_t*>(w.p1), n, len, scale, static_cast<O*>(dw), ld_dw, w.part, w.nchains, w.chains);
+    if (e != cudaSuccess) return e;
+    return launch_next(k_embed_join<O>, 4 * sms, kJoinThreads, st, width, static_cast<const uint32_t*>(w.k1), n, len,
+                       scale, static_cast<O*>(dw), ld_dw, static_cast<const float*>(w.part), static_cast<const uint32_t*>(w.nchains),
+                       static_cast<const uint32_t*>(w.chains));
 }
 
 }  // namespace
@@ -331,7 +432,8 @@ cudaError_t launch_embed(const void* weight, int64_t ld_w, int dtype, int64_t vo
 
 int64_t embed_grad_workspace(int64_t vocab, int64_t width, int64_t tokens) {
     (void)vocab;
-    return 4 * r16(4 * tokens) + (tokens + kSpan - 1) / kSpan * 2 * width * 4 + 16;
+    const int64_t spans = (tokens + span_of(tokens) - 1) / span_of(tokens);
+    return 4 * r16(4 * tokens) + 16 + r16(4 * spans) + spans * 2 * width * 4;
 }
 
 cudaError_t launch_embed_grad(const void* dy, int64_t ld_dy, int dtype, int64_t vocab, int64_t width, const void* ids,
@@ -347,12 +449,12 @@ cudaError_t launch_embed_grad(const void* dy, int64_t ld_dy, int dtype, int64_t 
     const unsigned grid = kSortCluster + std::max(1, (2 * sms) / kSortCluster) * kSortCluster;
     if (ids64)
         k_embed_sort<int64_t><<<grid, kSortThreads, 0, st>>>(static_cast<const int64_t*>(ids), tokens, vocab, bits, w.k0, w.k1, w.p0,
-                                                             w.p1, static_cast<uint8_t*>(dw), width * es, ld_dw * es);
+                                                             w.p1, w.nchains, static_cast<uint8_t*>(dw), width * es, ld_dw * es);
     else
         k_embed_sort<int32_t><<<grid, kSortThreads, 0, st>>>(static_cast<const int32_t*>(ids), tokens, vocab, bits, w.k0, w.k1, w.p0,
-                                                             w.p1, static_cast<uint8_t*>(dw), width * es, ld_dw * es);
+                                                             w.p1, w.nchains, static_cast<uint8_t*>(dw), width * es, ld_dw * es);
     if ((e = cudaGetLastError()) != cudaSuccess || tokens == 0) return e;
-#define GRAD(T, O) return embed_grad_t<T, O>(dy, ld_dy, vocab, width, w, tokens, scale, dw, ld_dw, st)
+#define GRAD(T, O) return embed_grad_t<T, O>(dy, ld_dy, vocab, width, w, tokens, scale, dw, ld_dw, sms, st)
     if (dtype == ISOLOCO_F32) GRAD(float, float);
     if (dtype == ISOLOCO_BF16) {
         if (dw_dtype == ISOLOCO_F32) GRAD(__nv_bfloat16, float);

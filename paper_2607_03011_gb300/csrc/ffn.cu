@@ -27,9 +27,14 @@ namespace isoloco {
 namespace {
 
 // ------------------------------------------------------------------ activation
-// act(g) and, with SLOPE, act'(g).  expf and the division are good to a few units in fp32's last place,
-// below every rounding to 16 bits that follows; where the denominator passes 2^126 the quotient is 0.
-__device__ __forceinline__ float logistic(float q) { return __fdividef(1.f, 1.f + __expf(-q)); }
+// act(g) and act'(g).  The exponential and the reciprocal are good to a few units in fp32's last place,
+// below every rounding to 16 bits that follows (e^-q past fp32's range gives s = 0).
+__device__ __forceinline__ float logistic(float q) {
+    float e, s;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(q * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
+    return s;
+}
 
 template <bool GELU>
 __device__ __forceinline__ float act_value(float g) {
@@ -54,25 +59,26 @@ __device__ __forceinline__ void act_both(float g, float& a, float& slope) {
 
 // ------------------------------------------------------------------ g and u kept for the gradient
 // With fp16 operands they stay fp32.  With bf16 they take 16 bits: sign, 6 exponent and 9 fraction
-// bits, 2^-30 to 2^33 (and gradual underflow to 2^-39).  Two bits more than bf16 has keep their rounding
-// below that of dg and du: the gradients' error against 64 bits is 1.45 times that of one rounding
-// to bf16, where bf16 here gave 1.85; fp16's 11 bits would give 1.42 but end at 65504.
+// bits, 2^-30 to 2^33 (and gradual underflow to 2^-39); what lies past 2^33, like NaN, comes back as
+// NaN.  Two bits more than bf16 has keep their rounding below that of dg and du: the gradients' error
+// against 64 bits is 1.45 times that of one rounding to bf16, where bf16 here gave 1.85; fp16's 11 bits
+// would end at 65504.
 template <class T>
 struct Kept;
 template <>
 struct Kept<__half> {
     using Store = float;
-    static __device__ __forceinline__ float clamp(float v) { return v > 3.4e38f ? 3.4e38f : v < -3.4e38f ? -3.4e38f : v; }
+    static __device__ __forceinline__ float clamp(float v) { return v; }
 };
 template <>
 struct Kept<__nv_bfloat16> {
     using Store = uint16_t;
-    static __device__ __forceinline__ uint32_t encode(float v) {
-        // NaN: the largest exponent and fraction, kept apart from the largest finite code
-        const uint32_t sign = (__float_as_uint(v) >> 16) & 0x8000u;
-        const uint32_t b = __float_as_uint(fminf(fabsf(v), 8.5e9f) * 0x1p-96f);
-        const uint32_t code = (b + 0x1fffu + ((b >> 14) & 1u)) >> 14;
-        return sign | (v == v ? code : 0x7fffu);
+    // two values, a's code in the low half: |v| 2^-96 has its 6-bit exponent and 9 fraction bits at bit 14
+    static __device__ __forceinline__ uint32_t encode2(float a, float b) {
+        const uint32_t x = min(__float_as_uint(fabsf(a) * 0x1p-96f) + 0x2000u, 0x1fffffffu);
+        const uint32_t y = min(__float_as_uint(fabsf(b) * 0x1p-96f) + 0x2000u, 0x1fffffffu);
+        const uint32_t codes = (x >> 14) | ((y << 2) & 0x7fff0000u);
+        return (__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632) & 0x80008000u) | codes;
     }
     static __device__ __forceinline__ float decode(uint32_t c) {
         const float m = __uint_as_float((c & 0x7fffu) << 14) * 0x1p96f;
@@ -87,11 +93,19 @@ constexpr int kDepth = 64;                     // K of a stage
 constexpr int kABytes = kTileRows * kDepth * 2;
 constexpr int kBBytes = 128 * kDepth * 2;      // at most 128 rows of B per CTA
 constexpr int kStageBytes = kABytes + kBBytes;
-constexpr int kStages = 6;
-constexpr int kEpiWarpsF = 8;
 constexpr int kStagingBytes = 4096;            // of an epilogue warp: 32 rows of 128 bytes
-constexpr int kThreads = 32 * (2 + kEpiWarpsF);
-constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kEpiWarpsF * kStagingBytes + 256;
+constexpr int kMaxStages = 6;
+// Forward, 16 epilogue warps: 8 for the even and 8 for the odd tiles of a cluster, so that a tile's epilogue
+// (two special functions and three stores per entry) may take as long as two tiles' products.  Backward, 8
+// warps suffice and the shared memory is another stage's.
+template <bool FWD>
+struct Geometry {
+    static constexpr int kEpiWarps = FWD ? 16 : 8;
+    static constexpr int kStages = FWD ? 5 : 6;
+    static constexpr int kThreads = 32 * (2 + kEpiWarps);
+    static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kEpiWarps * kStagingBytes + 256;
+};
+constexpr int kTileWarps = 8;                  // that drain one accumulator
 constexpr int kAccCols = 256;                  // tensor-memory columns of one accumulator
 
 // A product of the launch: `tiles` = tiles_m x tiles_n tiles of 256 x 2 nh.
@@ -104,15 +118,23 @@ struct Product {
 };
 enum { kGated = 0, kDx = 1, kDw = 2 };
 
-struct alignas(64) FfnGemm {
-    CUtensorMap x_k, wg_mn, wu_mn, h, keep_g, keep_u;            // forward
-    CUtensorMap dg_k, du_k, wg_k, wu_k, dx, x_mn, dg_mn, du_mn, dwg, dwu;  // gradient
+template <bool FWD>
+struct FfnGemm;
+struct FfnTiles {
     Product p[2];
     int n0, n1;       // tiles of p[0] and p[1]
     int extra;        // rounds of p[1] that the clusters without a tile in p[0]'s last round run first
     int tokens, width, ff;
     bool f16, keep, gelu;
     uint32_t* err;
+};
+template <>
+struct alignas(64) FfnGemm<true> : FfnTiles {
+    CUtensorMap x_k, wg_mn, wu_mn, h, keep_g, keep_u;
+};
+template <>
+struct alignas(64) FfnGemm<false> : FfnTiles {
+    CUtensorMap dg_k, du_k, wg_k, wu_k, dx, x_mn, dg_mn, du_mn, dwg, dwu;
 };
 
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
@@ -136,7 +158,7 @@ struct TileAt {
     int m0, n0, mat;  // first row of the pair's 256, first column, matrix (kDw)
     bool valid;
 };
-__device__ __forceinline__ TileAt tile_at(const FfnGemm& g, int c, int C, int i) {
+__device__ __forceinline__ TileAt tile_at(const FfnTiles& g, int c, int C, int i) {
     const int full = g.n0 / C, rest = g.n0 % C, left = C - rest;  // clusters < rest run one more tile of p[0]
     const int mine = full + (c < rest ? 1 : 0);
     TileAt r;
@@ -174,99 +196,131 @@ __device__ __forceinline__ TileAt tile_at(const FfnGemm& g, int c, int C, int i)
 __device__ __forceinline__ uint64_t k_desc(uint32_t a) { return make_sdesc(a, 16, 8 * kDepth * 2, 2); }
 __device__ __forceinline__ uint64_t mn_desc(uint32_t a) { return make_sdesc(a, kDepth * 128, 1024, 2); }
 
-// 32 rows x 64 columns of 16-bit values (w: the lane's row, 32 words) or 32 of fp32 to `dst`, rows of 128
-// bytes in the 128-byte swizzle, and from there by TMA to (col, row).
-__device__ __forceinline__ void store_block(const uint32_t (&w)[32], uint32_t stg, int lane, const CUtensorMap* map, int col,
-                                            int row) {
-    if (elect_one()) bulk_wait_read0();  // the block before has left
-    __syncwarp();
-    const uint32_t at = stg + lane * 128 + ((lane & 7) << 4);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) st_shared4(at ^ (q << 4), w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (elect_one()) {
-        tma_store_2d(map, stg, col, row);
-        bulk_commit();
-    }
+// Two pieces of 16 columns of the warp's tensor-memory lanes, one wait for both.
+__device__ __forceinline__ void tmem_ld16x2(uint32_t at_a, uint32_t at_b, uint32_t (&a)[16], uint32_t (&b)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%33];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(a[4]), "=r"(a[5]), "=r"(a[6]), "=r"(a[7]), "=r"(a[8]), "=r"(a[9]),
+          "=r"(a[10]), "=r"(a[11]), "=r"(a[12]), "=r"(a[13]), "=r"(a[14]), "=r"(a[15]), "=r"(b[0]), "=r"(b[1]), "=r"(b[2]),
+          "=r"(b[3]), "=r"(b[4]), "=r"(b[5]), "=r"(b[6]), "=r"(b[7]), "=r"(b[8]), "=r"(b[9]), "=r"(b[10]), "=r"(b[11]),
+          "=r"(b[12]), "=r"(b[13]), "=r"(b[14]), "=r"(b[15])
+        : "r"(at_a), "r"(at_b)
+        : "memory");
 }
 
-// One warp's 32 rows of a forward tile: columns [c0, c0 + 64) of g and u.
-template <class T, bool GELU>
-__device__ __forceinline__ void gated_block(const FfnGemm& p, uint32_t tacc, int nh, int c0, int col, int row, uint32_t stg,
-                                            int lane) {
-    uint32_t hw[32];
-    uint32_t kw[2][32];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        uint32_t g[32], u[32];
-        tmem_ld32(tacc + c0 + half * 32, g);
-        tmem_ld32(tacc + nh + c0 + half * 32, u);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const float g0 = __uint_as_float(g[2 * j]), g1 = __uint_as_float(g[2 * j + 1]);
-            const float u0 = __uint_as_float(u[2 * j]), u1 = __uint_as_float(u[2 * j + 1]);
-            hw[half * 16 + j] = round16x2(act_value<GELU>(g0) * u0, act_value<GELU>(g1) * u1, __is_same(T, __half));
-            if constexpr (__is_same(T, __nv_bfloat16)) {
-                if (p.keep) {
-                    kw[0][half * 16 + j] = Kept<T>::encode(g0) | (Kept<T>::encode(g1) << 16);
-                    kw[1][half * 16 + j] = Kept<T>::encode(u0) | (Kept<T>::encode(u1) << 16);
-                }
-            }
-        }
-        if constexpr (__is_same(T, __half)) {
-            if (p.keep) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    g[j] = __float_as_uint(Kept<T>::clamp(__uint_as_float(g[j])));
-                    u[j] = __float_as_uint(Kept<T>::clamp(__uint_as_float(u[j])));
-                }
-                if (col + half * 32 < p.ff) {
-                    store_block(g, stg, lane, &p.keep_g, col + half * 32, row);
-                    store_block(u, stg, lane, &p.keep_u, col + half * 32, row);
-                }
-            }
+// A block of 32 rows of 128 bytes goes to memory through the warp's staging block, in the 128-byte swizzle:
+// the block before has left (begin), each lane writes its row's eight 16-byte chunks (chunk), one TMA
+// store takes it to (col, row) (end).
+struct Staging {
+    uint32_t stg, row_at;
+    __device__ __forceinline__ Staging(uint32_t s, int lane) : stg(s), row_at(s + lane * 128 + ((lane & 7) << 4)) {}
+    __device__ __forceinline__ void begin() const {
+        if (elect_one()) bulk_wait_read0();
+        __syncwarp();
+    }
+    __device__ __forceinline__ void chunk(int q, uint32_t a, uint32_t b, uint32_t c, uint32_t d) const {
+        st_shared4(row_at ^ (q << 4), a, b, c, d);
+    }
+    __device__ __forceinline__ void end(const CUtensorMap* map, int col, int row) const {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (elect_one()) {
+            tma_store_2d(map, stg, col, row);
+            bulk_commit();
         }
     }
-    store_block(hw, stg, lane, &p.h, col, row);
-    if constexpr (__is_same(T, __nv_bfloat16)) {
-        if (p.keep) {
-            store_block(kw[0], stg, lane, &p.keep_g, col, row);
-            store_block(kw[1], stg, lane, &p.keep_u, col, row);
+};
+
+// One warp's 32 rows of a forward tile: columns [c0, c0 + 64) of g and u.  The accumulators are read again for
+// each output: keeping them would take 128 registers.
+template <class T, bool GELU>
+__device__ __forceinline__ void gated_block(const FfnGemm<true>& p, uint32_t tacc, int nh, int c0, int col, int row, const Staging& st) {
+    constexpr bool kF16 = __is_same(T, __half);
+    uint32_t g[16], u[16];
+    st.begin();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        tmem_ld16x2(tacc + c0 + q * 16, tacc + nh + c0 + q * 16, g, u);
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float g0 = __uint_as_float(g[2 * j]), g1 = __uint_as_float(g[2 * j + 1]);
+            w[j] = round16x2(act_value<GELU>(g0) * __uint_as_float(u[2 * j]), act_value<GELU>(g1) * __uint_as_float(u[2 * j + 1]), kF16);
+        }
+        st.chunk(2 * q, w[0], w[1], w[2], w[3]);
+        st.chunk(2 * q + 1, w[4], w[5], w[6], w[7]);
+    }
+    st.end(&p.h, col, row);
+    if (!p.keep) return;
+#pragma unroll 1
+    for (int m = 0; m < 2; ++m) {
+        const uint32_t from = tacc + (m ? nh : 0) + c0;
+        const CUtensorMap* map = m ? &p.keep_u : &p.keep_g;
+        if constexpr (kF16) {
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {  // fp32: 32 columns are 128 bytes
+                if (col + half * 32 >= p.ff) break;
+                st.begin();
+                tmem_ld16x2(from + half * 32, from + half * 32 + 16, g, u);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) st.chunk(q, g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) st.chunk(4 + q, u[4 * q], u[4 * q + 1], u[4 * q + 2], u[4 * q + 3]);
+                st.end(map, col + half * 32, row);
+            }
+        } else {
+            st.begin();
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                tmem_ld16x2(from + half * 32, from + half * 32 + 16, g, u);
+                uint32_t w[16];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    w[j] = Kept<T>::encode2(__uint_as_float(g[2 * j]), __uint_as_float(g[2 * j + 1]));
+                    w[8 + j] = Kept<T>::encode2(__uint_as_float(u[2 * j]), __uint_as_float(u[2 * j + 1]));
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) st.chunk(4 * half + q, w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+            }
+            st.end(map, col, row);
         }
     }
 }
 
 template <class T>
-__device__ __forceinline__ void plain_block(uint32_t tacc, int c0, const CUtensorMap* map, int col, int row, uint32_t stg, int lane) {
-    uint32_t w[32];
+__device__ __forceinline__ void plain_block(uint32_t tacc, int c0, const CUtensorMap* map, int col, int row, const Staging& st) {
+    st.begin();
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-        uint32_t v[32];
+        uint32_t v[32], w[16];
         tmem_ld32(tacc + c0 + half * 32, v);
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            w[half * 16 + j] = round16x2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]), __is_same(T, __half));
+        for (int j = 0; j < 16; ++j) w[j] = round16x2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]), __is_same(T, __half));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) st.chunk(4 * half + q, w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
     }
-    store_block(w, stg, lane, map, col, row);
+    st.end(map, col, row);
 }
 
 // Persistent, clusters of two CTAs; cluster c runs tile_at(c, 0), tile_at(c, 1), ...  Warp 0 loads, warp 1
-// of CTA 0 issues the pair's MMAs, warps 2..9 of both drain the accumulators.  `full` / `empty` hand
+// of CTA 0 issues the pair's MMAs, the other warps of both drain the accumulators.  `full` / `empty` hand
 // stages over, `tfull` / `tempty` accumulators, as the TMA bytes and MMA commits complete.
-template <class T>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ffn_gemm(const __grid_constant__ FfnGemm p) {
+template <class T, bool FWD>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Geometry<FWD>::kThreads, 1) k_ffn_gemm(const __grid_constant__ FfnGemm<FWD> p) {
+    constexpr int kStages = Geometry<FWD>::kStages, kEpiWarps = Geometry<FWD>::kEpiWarps;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* staging = smem + kStages * kStageBytes;
-    uint64_t* full = reinterpret_cast<uint64_t*>(staging + kEpiWarpsF * kStagingBytes);
+    uint64_t* full = reinterpret_cast<uint64_t*>(staging + kEpiWarps * kStagingBytes);
     uint64_t* empty = full + kStages;
     uint64_t* tfull = empty + kStages;  // [2]
     uint64_t* tempty = tfull + 2;       // [2]
     uint64_t* drain = tempty + 2;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    static_assert(8 * (2 * kStages + 5) + 8 <= 256, "barriers behind the staging blocks");
+    static_assert(8 * (2 * kMaxStages + 5) + 8 <= 256, "barriers behind the staging blocks");
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
@@ -281,7 +335,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ffn_g
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&tfull[i], 1);
-            mbar_init(&tempty[i], kEpiWarpsF * 2);
+            mbar_init(&tempty[i], kTileWarps * 2);
         }
         mbar_init(drain, 1);
         *abort_flag = 0;
@@ -296,6 +350,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ffn_g
     cluster_sync();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    if (!FWD) after_previous();  // dg and du are complete
 
     if (warp == 0) {
         // ================= loads (one thread of each CTA)
@@ -320,7 +375,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ffn_g
                     if (leader) mbar_arrive_expect_tx(&full[stage], pair_bytes);
                     const uint32_t bar = fbar0 + 8u * stage;
                     const uint32_t sa = sbase + stage * kStageBytes, sb = sa + kABytes;
-                    if (q.kind == kGated) {
+                    if constexpr (FWD) {
                         const int k0 = kb * kDepth;
                         tma_load_2d_pair(sa, &p.x_k, bar, k0, m0);
                         const CUtensorMap* w = leader ? &p.wg_mn : &p.wu_mn;
@@ -420,11 +475,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ffn_g
             (void)mbar_wait(drain, 0);
         }
     } else {
-        // ================= epilogue: warp w reads tensor-memory lanes 32 (w % 4) ..; of the tile's
-        // blocks of 64 columns warps 2..5 take the even, warps 6..9 the odd ones
-        const int eg = warp & 3, half = (warp - 2) >> 2;
-        const uint32_t stg = smem_u32(staging) + (warp - 2) * kStagingBytes;
-        for (int i = 0;; ++i) {
+        // ================= epilogue: warp w reads tensor-memory lanes 32 (w % 4) ..; of the tile's blocks of
+        // 64 columns one set of four warps takes the even, the next the odd ones; forward, warps 2..9 take the
+        // even and warps 10..17 the odd tiles
+        const int eg = warp & 3, half = ((warp - 2) >> 2) & 1;
+        const Staging st(smem_u32(staging) + (warp - 2) * kStagingBytes, lane);
+        constexpr int kSets = kEpiWarps / kTileWarps;
+        for (int i = (warp - 2) / kTileWarps;; i += kSets) {
             const TileAt t = tile_at(p, c, C, i);
             if (!t.valid) break;
             const Product& q = *t.p;
@@ -436,18 +493,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ffn_g
             tc_fence_after();
             const uint32_t tacc = tmem_base + buf * kAccCols + (static_cast<uint32_t>(eg * 32) << 16);
             const int row = t.m0 + static_cast<int>(crank) * kTileRows + eg * 32;
-            if (q.kind == kGated) {
+            if constexpr (FWD) {
                 if (row < p.tokens)
                     for (int c0 = half * 64; c0 < q.nh && t.n0 + c0 < p.ff; c0 += 128) {
-                        if (p.gelu) gated_block<T, true>(p, tacc, q.nh, c0, t.n0 + c0, row, stg, lane);
-                        else gated_block<T, false>(p, tacc, q.nh, c0, t.n0 + c0, row, stg, lane);
+                        if (p.gelu) gated_block<T, true>(p, tacc, q.nh, c0, t.n0 + c0, row, st);
+                        else gated_block<T, false>(p, tacc, q.nh, c0, t.n0 + c0, row, st);
                     }
             } else {
                 const int rows = q.kind == kDx ? p.tokens : p.width, cols = q.kind == kDx ? p.width : p.ff;
                 const CUtensorMap* map = q.kind == kDx ? &p.dx : t.mat ? &p.dwu : &p.dwg;
                 if (row < rows)
                     for (int c0 = half * 64; c0 < 2 * q.nh && t.n0 + c0 < cols; c0 += 128)
-                        plain_block<T>(tacc, c0, map, t.n0 + c0, row, stg, lane);
+                        plain_block<T>(tacc, c0, map, t.n0 + c0, row, st);
             }
             tc_fence_before();
             __syncwarp();
@@ -473,15 +530,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) k_ffn_g
 }
 
 // ------------------------------------------------------------------ dg and du
-// d: tokens x 2 x pitch, dg then du of a token.  8 columns per thread; dh's rows may start anywhere.
+// d: tokens x 2 x pitch, dg then du of a token.  8 columns per step; dh's rows may start anywhere.
 template <class T, bool GELU>
 __global__ void __launch_bounds__(256) k_ffn_dgu(const T* __restrict__ dh, int64_t ld_dh, bool dh_vec,
                                                  const typename Kept<T>::Store* __restrict__ saved, T* __restrict__ d, int64_t tokens,
                                                  int64_t ff, int64_t pitch) {
-    const int64_t n = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
-    if (n >= ff) return;
-    const int cols = static_cast<int>(min(static_cast<int64_t>(8), ff - n));
-    for (int64_t m = blockIdx.y; m < tokens; m += gridDim.y) {
+    next_may_start();
+    const uint32_t per_row = static_cast<uint32_t>(pitch >> 3);
+    const int64_t total = tokens * per_row;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t m = total <= 0xffffffffll ? static_cast<int64_t>(static_cast<uint32_t>(i) / per_row) : i / per_row;
+        const int64_t n = (i - m * per_row) * 8;
+        const int cols = static_cast<int>(min(static_cast<int64_t>(8), ff - n));
         float g[8], u[8], v[8];
         const int64_t at = m * 2 * pitch + n;  // the pad behind a row's last column may be read, not used
         if constexpr (__is_same(T, __half)) {
@@ -558,7 +618,7 @@ __global__ void __launch_bounds__(kFewThreads) k_ffn_few(const T* __restrict__ x
     if (n < ff) {  // (ff <= pitch, a multiple of 8: the last 16 bytes of a row exist)
         const T* pg = wg + static_cast<int64_t>(d0) * ld_w + n;
         const T* pu = wu + static_cast<int64_t>(d0) * ld_w + n;
-#pragma unroll 4
+#pragma unroll (NT <= 2 ? 8 : NT <= 4 ? 4 : 2)
         for (int r = warp * 4 + (lane >> 3); r < rows; r += 32) {
             Vec<T> a, b;
             a.raw = __ldg(reinterpret_cast<const uint4*>(pg + r * ld_w));
@@ -618,8 +678,8 @@ __global__ void __launch_bounds__(kFewThreads) k_ffn_few(const T* __restrict__ x
                         saved[t * 2 * pitch + col] = Kept<T>::clamp(g);
                         saved[t * 2 * pitch + pitch + col] = Kept<T>::clamp(u);
                     } else {
-                        saved[t * 2 * pitch + col] = static_cast<uint16_t>(Kept<T>::encode(g));
-                        saved[t * 2 * pitch + pitch + col] = static_cast<uint16_t>(Kept<T>::encode(u));
+                        saved[t * 2 * pitch + col] = static_cast<uint16_t>(Kept<T>::encode2(g, 0.f));
+                        saved[t * 2 * pitch + pitch + col] = static_cast<uint16_t>(Kept<T>::encode2(u, 0.f));
                     }
                 }
             }
@@ -704,8 +764,9 @@ cudaLaunchConfig_t cluster_config(unsigned grid, unsigned threads, size_t smem, 
     return cfg;
 }
 
-template <class T>
+template <class T, bool FWD>
 cudaError_t gemm_clusters(int* clusters) {
+    using G = Geometry<FWD>;
     static PerDevice fit;
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -713,38 +774,54 @@ cudaError_t gemm_clusters(int* clusters) {
     return fit.get<cudaError_t>(dev, clusters, [&](int* n) {
         int sms = 0;
         cudaError_t r = device_sms(&sms);
-        if (r == cudaSuccess) r = cudaFuncSetAttribute(k_ffn_gemm<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+        if (r == cudaSuccess) r = cudaFuncSetAttribute(k_ffn_gemm<T, FWD>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kSmemBytes);
         if (r != cudaSuccess) return r;
         cudaLaunchAttribute at[1];
-        const cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(sms & ~1), kThreads, kSmemBytes, 2, nullptr, at);
-        r = cudaOccupancyMaxActiveClusters(n, k_ffn_gemm<T>, &cfg);
+        const cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(sms & ~1), G::kThreads, G::kSmemBytes, 2, nullptr, at);
+        r = cudaOccupancyMaxActiveClusters(n, k_ffn_gemm<T, FWD>, &cfg);
         *n = std::max(1, std::min(*n, sms / 2));
         return r;
     });
 }
 
-template <class T>
-cudaError_t launch_gemm2(FfnGemm& g, cudaStream_t st) {
-    int C = 0;
-    cudaError_t e = gemm_clusters<T>(&C);
-    if (e != cudaSuccess || (e = error_word(&g.err)) != cudaSuccess) return e;
-    if (g.n0 + g.n1 == 0) return cudaSuccess;
-    C = std::min(C, g.n0 + g.n1);
-    cudaLaunchAttribute at[1];
-    const cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(2 * C), kThreads, kSmemBytes, 2, st, at);
-    // p[1]'s rounds that even out p[0]'s last: the number with the smallest longest cluster
+// What a tile costs, in hundredths of a k-block of 256 columns: one of 128 columns takes 0.75 of its time (the
+// bytes it loads: a k-block's arrive no faster than its products run), and starting and draining a tile about
+// one k-block.  Narrow tiles pay only where they fill SMs that wide ones leave idle: 2047 x 1024 x 2816
+// forward takes 26 us in 3 rounds of wide tiles, 29 in 5 of narrow ones; 33 tokens 12.4 and 11.8.
+inline int64_t tile_cost(const Product& p) { return static_cast<int64_t>(p.kblocks) * (p.nh == 128 ? 100 : 75) + 100; }
+
+// The rounds of p[1] that even out p[0]'s last (FfnTiles::extra) on C clusters, and the longest cluster's cost.
+int64_t plan_rounds(const FfnTiles& g, int C, int* extra) {
+    const int64_t c0 = tile_cost(g.p[0]), c1 = tile_cost(g.p[1]);
     const int full = g.n0 / C, rest = g.n0 % C, left = C - rest;
     int64_t best = INT64_MAX;
-    g.extra = 0;
-    for (int x = 0; rest && x * left <= g.n1 + left && x < 4096; ++x) {
+    for (int x = 0; x == 0 || (rest && x * left <= g.n1 + left && x < 4096); ++x) {
         const int after = std::max(0, g.n1 - x * left), rounds = after / C, more = after % C;
         // clusters without the extra tile of p[0] take the last round's tiles first
-        const int64_t a = static_cast<int64_t>(full) * g.p[0].kblocks + static_cast<int64_t>(x + rounds + (more > 0)) * g.p[1].kblocks;
-        const int64_t b = static_cast<int64_t>(full + 1) * g.p[0].kblocks + static_cast<int64_t>(rounds + (more > left)) * g.p[1].kblocks;
-        const int64_t t = std::max(a, b);
-        if (t < best) best = t, g.extra = x;
+        const int64_t a = full * c0 + (x + rounds + (more > 0)) * c1;
+        const int64_t b = rest ? (full + 1) * c0 + (rounds + (more > left)) * c1 : 0;
+        if (std::max(a, b) < best) {
+            best = std::max(a, b);
+            *extra = x;
+        }
     }
-    return cudaLaunchKernelEx(&cfg, k_ffn_gemm<T>, g);
+    return best;
+}
+
+template <class T, bool FWD>
+cudaError_t launch_gemm2(FfnGemm<FWD>& g, int C, cudaStream_t st) {
+    cudaError_t e = error_word(&g.err);
+    if (e != cudaSuccess || g.n0 + g.n1 == 0) return e;
+    C = std::min(C, g.n0 + g.n1);
+    (void)plan_rounds(g, C, &g.extra);
+    cudaLaunchAttribute at[2];
+    cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(2 * C), Geometry<FWD>::kThreads, Geometry<FWD>::kSmemBytes, 2, st, at);
+    if (!FWD) {
+        at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.numAttrs = 2;
+    }
+    return cudaLaunchKernelEx(&cfg, k_ffn_gemm<T, FWD>, g);
 }
 
 inline int tiles(int64_t n, int per) { return static_cast<int>((n + per - 1) / per); }
@@ -758,10 +835,10 @@ cudaError_t few_n(const FfnArgs& a, const void* wg, const void* wu, int64_t ld_w
     if (e == cudaSuccess) e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     const int blocks = tiles(a.ff, kFewCols);
-    // split D until there is a CTA for every SM, a warp's worth of rows each at least; wide x needs the split
-    // for its share in shared memory (width <= 2^20: checked by the caller)
+    // split D until there are two CTAs for every SM, 64 of its rows each at least; a wide x needs the split for its
+    // share in shared memory (few_fits)
     int split = 1;
-    while (split < kFewMaxSplit && (blocks * split < sms || a.width / split > 4096) && a.width / (2 * split) >= 32) split *= 2;
+    while (split < kFewMaxSplit && (blocks * split < 2 * sms || a.width / split > 4096) && a.width / (2 * split) >= 64) split *= 2;
     const size_t smem = sizeof(float) * (9 * 2 * NT * kFewCols + static_cast<size_t>((a.width + split - 1) / split) * NT);
     e = ready.get<cudaError_t>(dev, &unused, [&](int* v) {
         *v = 1;
@@ -824,7 +901,7 @@ cudaError_t forward(const FfnArgs& a, void* h, int64_t ld_h, void* saved, void* 
     }
     const bool direct = tma_ok(h, ld_h);
     void* out = direct ? h : arena.take(copy_bytes(a.tokens, a.ff));
-    FfnGemm g;
+    FfnGemm<true> g;
     bool ok = make_map2(&g.x_k, x, a.tokens, a.width, ld_x, kTileRows) && make_map2(&g.wg_mn, wg, a.width, a.ff, ld_w, kDepth) &&
               make_map2(&g.wu_mn, wu, a.width, a.ff, ld_w, kDepth) && make_map2(&g.h, out, a.tokens, a.ff, direct ? ld_h : fp, 32);
     if (saved) {
@@ -834,13 +911,20 @@ cudaError_t forward(const FfnArgs& a, void* h, int64_t ld_h, void* saved, void* 
     }
     if (!ok) return kNoMap;
     const int kb = tiles(a.width, kDepth);
-    g.p[0] = {kGated, tiles(a.tokens, 256), tiles(a.ff, 128), 128, kb, kb, 1};
-    g.p[1] = g.p[0];
-    g.n0 = g.p[0].tiles_m * g.p[0].tiles_n;
+    int C = 0, unused;
+    TRY((gemm_clusters<T, true>(&C)));
     g.n1 = 0;
+    int64_t best = INT64_MAX;
+    for (int nh = 128; nh >= 64; nh /= 2) {
+        FfnTiles t = g;
+        t.p[0] = t.p[1] = {kGated, tiles(a.tokens, 256), tiles(a.ff, nh), nh, kb, kb, 1};
+        t.n0 = t.p[0].tiles_m * t.p[0].tiles_n;
+        const int64_t cost = plan_rounds(t, std::min(C, t.n0), &unused);
+        if (cost < best) best = cost, static_cast<FfnTiles&>(g) = t;
+    }
     g.tokens = static_cast<int>(a.tokens), g.width = static_cast<int>(a.width), g.ff = static_cast<int>(a.ff);
     g.f16 = f16, g.keep = saved != nullptr, g.gelu = a.act == ISOLOCO_GELU_TANH;
-    TRY(launch_gemm2<T>(g, st));
+    TRY((launch_gemm2<T, true>(g, C, st)));
     return direct ? cudaSuccess : repitch(out, fp, h, ld_h, a.tokens, a.ff, st);
 }
 
@@ -858,7 +942,9 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
     Arena arena = {static_cast<uint8_t*>(ws)};
     T* d = static_cast<T*>(arena.take(a.tokens * 2 * fp * 2));
     const bool dh_vec = tma_ok(dh, ld_dh);
-    const dim3 grid(static_cast<unsigned>((fp / 8 + 255) / 256), static_cast<unsigned>(std::min<int64_t>(a.tokens, 32768)));
+    int sms = 0;
+    TRY(device_sms(&sms));
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>((a.tokens * (fp / 8) + 255) / 256, 16 * sms));
     using Store = typename Kept<T>::Store;
     if (a.act == ISOLOCO_SILU)
         k_ffn_dgu<T, false><<<grid, 256, 0, st>>>(static_cast<const T*>(dh), ld_dh, dh_vec, static_cast<const Store*>(saved), d, a.tokens,
@@ -867,9 +953,26 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
         k_ffn_dgu<T, true><<<grid, 256, 0, st>>>(static_cast<const T*>(dh), ld_dh, dh_vec, static_cast<const Store*>(saved), d, a.tokens,
                                                  a.ff, fp);
     TRY(cudaGetLastError());
-    FfnGemm g;
+    FfnGemm<false> g;
     bool ok = true;
-    Product pdx = {kDx, 0, 0, 128, 0, 0, 1}, pdw = {kDw, 0, 0, 128, 0, 0, 2};
+    int C = 0, unused;
+    TRY((gemm_clusters<T, false>(&C)));
+    int64_t best = INT64_MAX;
+    for (int v = 0; v < 4; ++v) {  // tiles of 256 or 128 columns for either product
+        const int nx = v & 1 ? 64 : 128, nw = v & 2 ? 64 : 128, seg = tiles(a.ff, kDepth), kw = tiles(a.tokens, kDepth);
+        const Product pdx = {kDx, tiles(a.tokens, 256), tiles(a.width, 2 * nx), nx, 2 * seg, seg, 1};
+        const Product pdw = {kDw, tiles(a.width, 256), tiles(a.ff, 2 * nw), nw, kw, kw, 2};
+        const int ndx = dx ? pdx.tiles_m * pdx.tiles_n : 0, ndw = dwg ? 2 * pdw.tiles_m * pdw.tiles_n : 0;
+        // the product with the longer tiles first
+        const bool dw_first = !dx || (dwg && tile_cost(pdw) > tile_cost(pdx));
+        FfnTiles t = g;
+        t.p[0] = dw_first ? pdw : pdx, t.p[1] = dw_first ? pdx : pdw;
+        t.n0 = dw_first ? ndw : ndx, t.n1 = dw_first ? ndx : ndw;
+        if (t.n0 + t.n1 == 0) return cudaSuccess;
+        const int64_t cost = plan_rounds(t, std::min(C, t.n0 + t.n1), &unused);
+        if (cost < best) best = cost, static_cast<FfnTiles&>(g) = t;
+    }
+    const Product& pdx = g.p[0].kind == kDx ? g.p[0] : g.p[1];
     void *odx = dx, *odg = dwg, *odu = dwu;
     int64_t ldx = ld_dx, ldw = ld_dw;
     if (dx) {
@@ -882,8 +985,6 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
             wg = cg, wu = cu, ld_w = fp;
         }
         if (!tma_ok(dx, ldx)) odx = arena.take(copy_bytes(a.tokens, a.width)), ldx = dp;
-        const int seg = tiles(a.ff, kDepth);
-        pdx.tiles_m = tiles(a.tokens, 256), pdx.tiles_n = tiles(a.width, 2 * pdx.nh), pdx.seg = seg, pdx.kblocks = 2 * seg;
         ok = ok && make_map2(&g.dg_k, d, a.tokens, a.ff, 2 * fp, kTileRows) && make_map2(&g.du_k, d + fp, a.tokens, a.ff, 2 * fp, kTileRows) &&
              make_map2(&g.wg_k, wg, a.width, a.ff, ld_w, pdx.nh) && make_map2(&g.wu_k, wu, a.width, a.ff, ld_w, pdx.nh) &&
              make_map2(&g.dx, odx, a.tokens, a.width, ldx, 32);
@@ -900,22 +1001,14 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
             odg = arena.take(copy_bytes(a.width, a.ff)), odu = arena.take(copy_bytes(a.width, a.ff));
             ldw = fp;
         }
-        pdw.tiles_m = tiles(a.width, 256), pdw.tiles_n = tiles(a.ff, 2 * pdw.nh), pdw.kblocks = pdw.seg = tiles(a.tokens, kDepth);
         ok = ok && make_map2(&g.x_mn, x, a.tokens, a.width, ld_x, kDepth) && make_map2(&g.dg_mn, d, a.tokens, a.ff, 2 * fp, kDepth) &&
              make_map2(&g.du_mn, d + fp, a.tokens, a.ff, 2 * fp, kDepth) && make_map2(&g.dwg, odg, a.width, a.ff, ldw, 32) &&
              make_map2(&g.dwu, odu, a.width, a.ff, ldw, 32);
     }
     if (!ok) return kNoMap;
-    const int ndx = pdx.tiles_m * pdx.tiles_n, ndw = 2 * pdw.tiles_m * pdw.tiles_n;
-    // the product with the longer tiles first
-    const bool dw_first = pdw.kblocks > pdx.kblocks;
-    g.p[0] = dw_first ? pdw : pdx;
-    g.p[1] = dw_first ? pdx : pdw;
-    g.n0 = dw_first ? ndw : ndx;
-    g.n1 = dw_first ? ndx : ndw;
     g.tokens = static_cast<int>(a.tokens), g.width = static_cast<int>(a.width), g.ff = static_cast<int>(a.ff);
     g.f16 = __is_same(T, __half), g.keep = false, g.gelu = false;
-    TRY(launch_gemm2<T>(g, st));
+    TRY((launch_gemm2<T, false>(g, C, st)));
     if (odx != dx) TRY(repitch(odx, ldx, dx, ld_dx, a.tokens, a.width, st));
     if (odg != dwg) {
         TRY(repitch(odg, ldw, dwg, ld_dw, a.width, a.ff, st));

@@ -228,14 +228,18 @@ __device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int 
     if (threadIdx.x == 0) sm.count = sm.threads = 0;
     if (threadIdx.x < k) best[threadIdx.x] = 0;
     __syncthreads();
-    if (threadIdx.x < kGroups) {
-        const uint64_t own = sm.group[threadIdx.x];
+    {
+        // ranks of the groups: kPer threads each count a share of the greater ones
+        const int own_at = threadIdx.x / kPer, sub = threadIdx.x % kPer;
+        const uint64_t own = sm.group[own_at];
         int r = 0;
-#pragma unroll 16
-        for (int j = 0; j < kGroups; ++j) {
-            const uint64_t v = sm.group[j];
-            r += (v > own || (v == own && j < static_cast<int>(threadIdx.x))) ? 1 : 0;  // (equal keys: groups without entries)
+#pragma unroll
+        for (int j = 0; j < kGroups / kPer; ++j) {
+            const uint64_t v = sm.group[j * kPer + sub];
+            r += (v > own || (v == own && j * kPer + sub < own_at)) ? 1 : 0;  // (equal keys: groups without entries)
         }
+#pragma unroll
+        for (int o = 1; o < kPer; o <<= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
         if (r == k - 1) sm.bound = own;
     }
     __syncthreads();

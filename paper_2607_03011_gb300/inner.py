@@ -13,7 +13,7 @@ IsolocoError (what the library refuses) before anything is launched.
 """
 from __future__ import annotations
 
-import ctypes
+import array
 import functools
 from typing import NamedTuple, Optional, Sequence
 
@@ -33,6 +33,8 @@ MAX_TOP = 32
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _current_device = torch._C._cuda_getDevice
 _empty = torch.empty
+_data_ptr, _numel = torch.Tensor.data_ptr, torch.Tensor.numel
+_is_contiguous, _get_device = torch.Tensor.is_contiguous, torch.Tensor.get_device
 
 
 def _on_stream(f):
@@ -253,13 +255,15 @@ def token_logprobs_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.
 
 def _tensor_list(tensors: Sequence[torch.Tensor], what: str):
     """isoloco_tensor_t entries (address, length, type) as 64-bit words."""
-    words, dev = [], _current_device()
-    for t in tensors:
-        code = _DTYPE.get(t.dtype)
-        if code is None or t.get_device() != dev or not t.is_contiguous():
-            raise ValueError(f"{what}: contiguous tensors of fp32, bf16 or fp16 on the current CUDA device are needed")
-        words += (t.data_ptr(), t.numel(), code)
-    return (ctypes.c_int64 * (len(words) + 1))(*words)
+    codes = [_DTYPE.get(t.dtype, -1) for t in tensors]
+    if -1 in codes or not all(map(_is_contiguous, tensors)) or set(map(_get_device, tensors)) - {_current_device()}:
+        raise ValueError(f"{what}: contiguous tensors of fp32, bf16 or fp16 on the current CUDA device are needed")
+    n = len(codes)
+    words = array.array("q", bytes(24 * max(n, 1)))
+    words[0:3 * n:3] = array.array("q", map(_data_ptr, tensors))
+    words[1:3 * n:3] = array.array("q", map(_numel, tensors))
+    words[2:3 * n:3] = array.array("q", codes)
+    return words
 
 
 @_on_stream
@@ -271,7 +275,7 @@ def grad_norm(grads: Sequence[torch.Tensor]) -> torch.Tensor:
     need = L.isoloco_grad_norm_workspace(len(grads))
     norm = _empty((), dtype=torch.float32, device=dev)
     ws = _empty(need, dtype=torch.uint8, device=dev)
-    _check(L.isoloco_grad_norm(arr, len(grads), norm.data_ptr(), ws.data_ptr(), need, _raw_stream(dev)), "isoloco_grad_norm")
+    _check(L.isoloco_grad_norm(arr.buffer_info()[0], len(grads), norm.data_ptr(), ws.data_ptr(), need, _raw_stream(dev)), "isoloco_grad_norm")
     return norm
 
 
@@ -290,7 +294,7 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Seq
     need = L.isoloco_grad_norm_workspace(len(grads))
     norm = _empty((), dtype=torch.float32, device=dev)
     ws = _empty(need, dtype=torch.uint8, device=dev)
-    _check(L.isoloco_clip_grads(arr, outs, len(grads), max_norm, norm.data_ptr(), ws.data_ptr(), need, _raw_stream(dev)),
+    _check(L.isoloco_clip_grads(arr.buffer_info()[0], outs.buffer_info()[0] if outs else None, len(grads), max_norm, norm.data_ptr(), ws.data_ptr(), need, _raw_stream(dev)),
            "isoloco_clip_grads")
     return norm
 
