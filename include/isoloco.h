@@ -450,7 +450,7 @@ typedef struct {
 /* The gradient's global norm, sqrt(sum over all tensors and entries of g^2), to norm[0] (device
  * fp32).  Squares are taken in fp32: entries beyond 1.8e19 in magnitude give inf.
  *   tensors: HOST array of `count` entries, read during the call. */
-int64_t isoloco_grad_norm_workspace(int count);
+int64_t isoloco_grad_norm_workspace(const isoloco_tensor_t* tensors, int count);
 int isoloco_grad_norm(const isoloco_tensor_t* tensors, int count, float* norm, void* workspace,
                       int64_t workspace_bytes, void* stream);
 

@@ -2,14 +2,15 @@
 //
 //     n = sqrt(sum over all tensors and entries of g^2),   g' = g min(1, max_norm / n)
 //
-// Two launches whatever the number of tensors (up to kMaxTensors per table): the table of addresses
-// and lengths travels in the kernel's parameters, so no copy to the device precedes the call.  The
-// first sums squares over fixed chunks (fp32 within a thread, fp64 from there on) and leaves one
-// fp64 partial per CTA; the second adds the partials, every CTA in the same order, so that all have
-// the same bits, and scales.
+// The table of addresses and lengths travels in the kernel's parameters, so no copy to the device
+// precedes the call.  Two launches per table (kMaxTensors tensors): the first sums squares over fixed chunks
+// (fp32 within a thread, fp64 from there on) and leaves one fp64 partial per CTA; the second adds the
+// partials, every CTA in the same order, so that all have the same bits, and scales.  A short list of
+// small tensors takes one launch of one cluster (k_grad_small), whose CTAs exchange their sums in shared memory.
 #include <algorithm>
 #include <cmath>
 
+#include "common.cuh"
 #include "inner.cuh"
 #include "inner.h"
 
@@ -22,6 +23,8 @@ constexpr int kMaxTensors = 512;       // of one table: 512 x 32 bytes of kernel
 constexpr int kFewTensors = 32;        // a short list's parameters are a 16th of that (launch and first reads)
 constexpr int kChunkBytes = 32768;     // a CTA's unit of work: 8 16-byte loads per thread
 constexpr int kCtasPerSm = 8;
+constexpr int kSmallCluster = 8;       // CTAs of k_grad_small
+constexpr int kSmallChunks = 64;       // 2 MB: what that takes, 8 chunks per CTA
 constexpr int kKeepChunks = 2048;      // the last 64 MB stay in L2 for the scaling, which begins with them
 
 struct ClipTensor {
@@ -136,16 +139,33 @@ __device__ __forceinline__ double cta_sum(double v) {
 }
 
 template <int N>
+__device__ __forceinline__ float squares_of(const ClipTable<N>& tab, int c, bool keep) {
+    const ClipTensor& t = tab.t[find_tensor(tab, c)];
+    const int k = c - t.first;
+    return t.dtype == ISOLOCO_F32 ? chunk_squares<float>(t, k, keep)
+           : t.dtype == ISOLOCO_BF16 ? chunk_squares<__nv_bfloat16>(t, k, keep) : chunk_squares<__half>(t, k, keep);
+}
+template <int N>
+__device__ __forceinline__ void scale_by(const ClipTable<N>& tab, int c, float coef) {
+    const ClipTensor& t = tab.t[find_tensor(tab, c)];
+    const int k = c - t.first;
+    if (t.dtype == ISOLOCO_F32) chunk_scale<float>(t, k, coef);
+    else if (t.dtype == ISOLOCO_BF16) chunk_scale<__nv_bfloat16>(t, k, coef);
+    else chunk_scale<__half>(t, k, coef);
+}
+
+__device__ __forceinline__ float root_of(double s) {
+    return s > 1e30 ? sqrtf(static_cast<float>(s * 0x1p-64)) * 0x1p32f : sqrtf(static_cast<float>(s));
+}
+// A norm that is not finite, or zero, scales nothing.
+__device__ __forceinline__ float coef_of(float norm, float max_norm) { return norm > max_norm && norm < INFINITY ? max_norm / norm : 1.f; }
+
+template <int N>
 __global__ void __launch_bounds__(kClipThreads) k_grad_squares(const __grid_constant__ ClipTable<N> tab, double* part) {
     next_may_start();
     double acc = 0.0;
     for (int c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
-        const ClipTensor& t = tab.t[find_tensor(tab, c)];
-        const int k = c - t.first;
-        const bool keep = tab.chunks - c <= kKeepChunks;
-        const float s = t.dtype == ISOLOCO_F32 ? chunk_squares<float>(t, k, keep)
-                        : t.dtype == ISOLOCO_BF16 ? chunk_squares<__nv_bfloat16>(t, k, keep) : chunk_squares<__half>(t, k, keep);
-        acc += static_cast<double>(s);
+        acc += static_cast<double>(squares_of(tab, c, tab.chunks - c <= kKeepChunks));
     }
     const double s = cta_sum(acc);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -166,7 +186,7 @@ __device__ __forceinline__ float norm_of(const double* part, int nparts) {
     __syncthreads();
     double s = warps ? sum[0] : 0.0;
     for (int i = 1; i < warps; ++i) s += sum[i];
-    return s > 1e30 ? sqrtf(static_cast<float>(s * 0x1p-64)) * 0x1p32f : sqrtf(static_cast<float>(s));
+    return root_of(s);
 }
 
 // tab.chunks == 0: the norm only.
@@ -176,17 +196,32 @@ __global__ void __launch_bounds__(kClipThreads) k_grad_scale(const __grid_consta
     after_previous();
     const float n = norm_of(part, nparts);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = n;
-    // a norm that is not finite, or zero, scales nothing
-    const float coef = (n > max_norm && n < INFINITY) ? max_norm / n : 1.f;
+    const float coef = coef_of(n, max_norm);
     if (in_place && coef == 1.f) return;
     // from the last chunk down: what the first pass read last is still in L2
-    for (int c = tab.chunks - 1 - static_cast<int>(blockIdx.x); c >= 0; c -= gridDim.x) {
-        const ClipTensor& t = tab.t[find_tensor(tab, c)];
-        const int k = c - t.first;
-        if (t.dtype == ISOLOCO_F32) chunk_scale<float>(t, k, coef);
-        else if (t.dtype == ISOLOCO_BF16) chunk_scale<__nv_bfloat16>(t, k, coef);
-        else chunk_scale<__half>(t, k, coef);
-    }
+    for (int c = tab.chunks - 1 - static_cast<int>(blockIdx.x); c >= 0; c -= gridDim.x) scale_by(tab, c, coef);
+}
+
+// (max_norm: negative for the norm alone)
+__global__ void __cluster_dims__(kSmallCluster, 1, 1) __launch_bounds__(kClipThreads)
+    k_grad_small(const __grid_constant__ ClipTable<kFewTensors> tab, float max_norm, bool in_place, float* norm) {
+    __shared__ double sums[kSmallCluster];  // of every CTA, in every CTA
+    const uint32_t rank = cluster_ctarank();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    double acc = 0.0;
+    for (int c = rank; c < tab.chunks; c += kSmallCluster) acc += static_cast<double>(squares_of(tab, c, true));
+    acc = cta_sum(acc);
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // every CTA runs: its shared memory may be written
+    if (threadIdx.x < kSmallCluster)
+        asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(mapa_shared(smem_u32(sums + rank), threadIdx.x)), "d"(acc) : "memory");
+    cluster_sync();
+    double s = 0.0;
+    for (int i = 0; i < kSmallCluster; ++i) s += sums[i];
+    const float n = root_of(s);
+    if (rank == 0 && threadIdx.x == 0) norm[0] = n;
+    const float coef = coef_of(n, max_norm);
+    if (max_norm < 0.f || (in_place && coef == 1.f)) return;
+    for (int c = rank; c < tab.chunks; c += kSmallCluster) scale_by(tab, c, coef);
 }
 
 int chunks_of(const isoloco_tensor_t& t) {
@@ -199,9 +234,22 @@ int chunks_of(const isoloco_tensor_t& t) {
 
 }  // namespace
 
+namespace {
+
+bool is_small(const isoloco_tensor_t* in, int count) {
+    if (count > kFewTensors) return false;
+    int chunks = 0;
+    for (int i = 0; i < count && chunks <= kSmallChunks; ++i)
+        if (in[i].n) chunks += chunks_of(in[i]);
+    return chunks <= kSmallChunks;
+}
+
+}  // namespace
+
 // One table per kMaxTensors tensors, at most kCtasPerSm partials per SM each.
-int64_t grad_norm_workspace(int count) {
-    const int64_t tables = count > 0 ? (count + kMaxTensors - 1) / kMaxTensors : 1;
+int64_t grad_norm_workspace(const isoloco_tensor_t* in, int count) {
+    if (is_small(in, count)) return 0;
+    const int64_t tables = (count + kMaxTensors - 1) / kMaxTensors;
     return tables * 1024 * kCtasPerSm * static_cast<int64_t>(sizeof(double));
 }
 
@@ -257,6 +305,12 @@ cudaError_t clip_n(const isoloco_tensor_t* in, const isoloco_tensor_t* out, int 
 
 cudaError_t launch_clip(const isoloco_tensor_t* in, const isoloco_tensor_t* out, int count, bool clip, float max_norm,
                         float* norm, void* ws, cudaStream_t st) {
+    if (is_small(in, count)) {
+        ClipTable<kFewTensors> tab;
+        (void)fill_table(tab, in, out, 0, count);
+        k_grad_small<<<kSmallCluster, kClipThreads, 0, st>>>(tab, clip ? max_norm : -1.f, out == nullptr, norm);
+        return cudaGetLastError();
+    }
     int sms = 0;
     const cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;

@@ -55,7 +55,7 @@ cudaError_t launch_logprobs(const LogprobArgs& a, cudaStream_t st);
 // a.lse and a.entropy are read
 cudaError_t launch_logprobs_grad(const LogprobArgs& a, cudaStream_t st);
 
-int64_t grad_norm_workspace(int count);
+int64_t grad_norm_workspace(const isoloco_tensor_t* in, int count);
 // clip: false writes the norm only
 cudaError_t launch_clip(const isoloco_tensor_t* in, const isoloco_tensor_t* out, int count, bool clip, float max_norm,
                         float* norm, void* ws, cudaStream_t st);

@@ -206,13 +206,15 @@ int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_d
     return cuda_status(launch_logprobs_grad(a, stream_of(stream)));
 }
 
-int64_t isoloco_grad_norm_workspace(int count) { return count < 0 ? ISOLOCO_ERR_INVALID : grad_norm_workspace(count); }
+int64_t isoloco_grad_norm_workspace(const isoloco_tensor_t* tensors, int count) {
+    return tensors_problem(tensors, count) ? ISOLOCO_ERR_INVALID : grad_norm_workspace(tensors, count);
+}
 
 int isoloco_grad_norm(const isoloco_tensor_t* tensors, int count, float* norm, void* workspace,
                       int64_t workspace_bytes, void* stream) {
     if (const char* p = tensors_problem(tensors, count)) return invalid(p);
     if (!array_ok(norm, 1, 4)) return invalid("norm is NULL or misaligned");
-    const int rc = workspace_ok(workspace, workspace_bytes, grad_norm_workspace(count));
+    const int rc = workspace_ok(workspace, workspace_bytes, grad_norm_workspace(tensors, count));
     if (rc != ISOLOCO_OK) return rc;
     return cuda_status(launch_clip(tensors, nullptr, count, false, 0.f, norm, workspace, stream_of(stream)));
 }
@@ -227,7 +229,7 @@ int isoloco_clip_grads(const isoloco_tensor_t* tensors, const isoloco_tensor_t* 
     }
     if (!(max_norm > 0.f)) return invalid("max_norm must be positive");
     if (!array_ok(norm, 1, 4)) return invalid("norm is NULL or misaligned");
-    const int rc = workspace_ok(workspace, workspace_bytes, grad_norm_workspace(count));
+    const int rc = workspace_ok(workspace, workspace_bytes, grad_norm_workspace(tensors, count));
     if (rc != ISOLOCO_OK) return rc;
     return cuda_status(launch_clip(tensors, outs, count, true, max_norm, norm, workspace, stream_of(stream)));
 }

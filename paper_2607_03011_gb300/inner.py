@@ -156,7 +156,7 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: st
     L, dev, dt = lib(), x.device, x.dtype
     h = _empty((*x.shape[:-1], ff), dtype=dt, device=dev)
     saved = _empty(L.isoloco_gated_ffn_saved_bytes(n, ff, _HALF[dt]), dtype=torch.uint8, device=dev) if save else None
-    need = L.isoloco_gated_ffn_workspace(n, width, ff, aligned)
+    need = 0 if aligned else L.isoloco_gated_ffn_workspace(n, width, ff, 0)
     ws = _empty(need, dtype=torch.uint8, device=dev) if need else None
     _check(L.isoloco_gated_ffn(*args, h.data_ptr(), ff, _ptr(saved), _ptr(ws), need, _raw_stream(dev.index)),
            "isoloco_gated_ffn")
@@ -270,12 +270,12 @@ def _tensor_list(tensors: Sequence[torch.Tensor], what: str):
 def grad_norm(grads: Sequence[torch.Tensor]) -> torch.Tensor:
     """The norm over all entries of all tensors, a 0-d fp32 tensor on the device."""
     grads = list(grads)
-    arr = _tensor_list(grads, "grads")
-    L, dev = lib(), _current_device()
-    need = L.isoloco_grad_norm_workspace(len(grads))
+    words = _tensor_list(grads, "grads")
+    L, n, dev, arr = lib(), len(grads), _current_device(), words.buffer_info()[0]
+    need = L.isoloco_grad_norm_workspace(arr, n)
     norm = _empty((), dtype=torch.float32, device=dev)
-    ws = _empty(need, dtype=torch.uint8, device=dev)
-    _check(L.isoloco_grad_norm(arr.buffer_info()[0], len(grads), norm.data_ptr(), ws.data_ptr(), need, _raw_stream(dev)), "isoloco_grad_norm")
+    ws = _empty(need, dtype=torch.uint8, device=dev) if need else None
+    _check(L.isoloco_grad_norm(arr, n, norm.data_ptr(), _ptr(ws), need, _raw_stream(dev)), "isoloco_grad_norm")
     return norm
 
 
@@ -284,18 +284,18 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Seq
     """Scales the gradient by min(1, max_norm / norm), in place or into `out`, and returns the norm
     (0-d, fp32).  A NaN or infinite norm scales nothing."""
     grads = list(grads)
-    arr, outs = _tensor_list(grads, "grads"), None
+    words, outs = _tensor_list(grads, "grads"), None
     if out is not None:
         out = list(out)
         if len(out) != len(grads):
             raise ValueError("out: one tensor per gradient")
         outs = _tensor_list(out, "out")
-    L, dev = lib(), _current_device()
-    need = L.isoloco_grad_norm_workspace(len(grads))
+    L, n, dev, arr = lib(), len(grads), _current_device(), words.buffer_info()[0]
+    need = L.isoloco_grad_norm_workspace(arr, n)
     norm = _empty((), dtype=torch.float32, device=dev)
-    ws = _empty(need, dtype=torch.uint8, device=dev)
-    _check(L.isoloco_clip_grads(arr.buffer_info()[0], outs.buffer_info()[0] if outs else None, len(grads), max_norm, norm.data_ptr(), ws.data_ptr(), need, _raw_stream(dev)),
-           "isoloco_clip_grads")
+    ws = _empty(need, dtype=torch.uint8, device=dev) if need else None
+    _check(L.isoloco_clip_grads(arr, outs and outs.buffer_info()[0], n, max_norm, norm.data_ptr(), _ptr(ws), need,
+                                _raw_stream(dev)), "isoloco_clip_grads")
     return norm
 
 

@@ -114,7 +114,7 @@ def lib():
             for f in (L.isoloco_gated_ffn_workspace, L.isoloco_gated_ffn_grad_workspace):
                 f.argtypes, f.restype = [i64, i64, i64, ci], i64
             L.isoloco_gated_ffn_saved_bytes.argtypes, L.isoloco_gated_ffn_saved_bytes.restype = [i64, i64, ci], i64
-            L.isoloco_grad_norm_workspace.argtypes, L.isoloco_grad_norm_workspace.restype = [ci], i64
+            L.isoloco_grad_norm_workspace.argtypes, L.isoloco_grad_norm_workspace.restype = [_vp, ci], i64
             _lib = L
     return _lib
 

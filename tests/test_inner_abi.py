@@ -112,8 +112,11 @@ def test_clip_grads(iso, ptr):
         assert L.isoloco_clip_grads(a, None, 1, 1.0, p, p, BIG, None) == bad
         assert L.isoloco_clip_grads(good, a, 1, 1.0, p, p, BIG, None) == bad
     assert L.isoloco_grad_norm(None, 1, p, p, BIG, None) == bad and L.isoloco_grad_norm(good, -1, p, p, BIG, None) == bad
-    assert L.isoloco_grad_norm(good, 1, None, p, BIG, None) == bad and L.isoloco_grad_norm(good, 1, p, p, 8, None) == bad
-    assert L.isoloco_grad_norm(good, 1, p, odd(p, 8), BIG, None) == iso.ERR_ALIGN
+    assert L.isoloco_grad_norm(good, 1, None, p, BIG, None) == bad
+    large = arr((p.value, 1 << 24, 0))  # (a small gradient needs no workspace)
+    assert L.isoloco_grad_norm_workspace(good, 1) == 0 and L.isoloco_grad_norm_workspace(large, 1) > 8
+    assert L.isoloco_grad_norm(large, 1, p, p, 8, None) == bad and L.isoloco_grad_norm(large, 1, p, None, BIG, None) == bad
+    assert L.isoloco_grad_norm(large, 1, p, odd(p, 8), BIG, None) == iso.ERR_ALIGN
     for outs in (arr((p.value, 5, 0)), arr((p.value, 4, 1))):
         assert L.isoloco_clip_grads(good, outs, 1, 1.0, p, p, BIG, None) == bad
     for m in (0.0, -1.0, float("nan")):
