@@ -129,11 +129,11 @@ struct FfnTiles {
     uint32_t* err;
 };
 template <>
-struct alignas(64) FfnGemm<true> : FfnTiles {
+struct FfnGemm<true> : FfnTiles {
     CUtensorMap x_k, wg_mn, wu_mn, h, keep_g, keep_u;
 };
 template <>
-struct alignas(64) FfnGemm<false> : FfnTiles {
+struct FfnGemm<false> : FfnTiles {
     CUtensorMap dg_k, du_k, wg_k, wu_k, dx, x_mn, dg_mn, du_mn, dwg, dwu;
 };
 

@@ -14,7 +14,6 @@ IsolocoError (what the library refuses) before anything is launched.
 from __future__ import annotations
 
 import array
-import functools
 from typing import NamedTuple, Optional, Sequence
 
 import torch
@@ -37,18 +36,12 @@ _data_ptr, _numel = torch.Tensor.data_ptr, torch.Tensor.numel
 _is_contiguous, _get_device = torch.Tensor.is_contiguous, torch.Tensor.get_device
 
 
-def _on_stream(f):
-    """Adds the argument `stream`: the call runs with it as the current stream, outputs and workspaces
-    are allocated there."""
-    @functools.wraps(f)
-    def call(*args, stream=None, **kw):
-        if stream is None:
-            return f(*args, **kw)
-        if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream))
-        with torch.cuda.stream(stream):
-            return f(*args, **kw)
-    return call
+def _on(stream, f, *args):
+    """The call f(*args) with `stream` as the current stream: its outputs and workspaces are allocated there."""
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream))
+    with torch.cuda.stream(stream):
+        return f(*args)
 
 
 def _rows(t: torch.Tensor, what: str, dtypes=_DTYPE):
@@ -95,23 +88,27 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-@_on_stream
-def embed(weight: torch.Tensor, ids: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
+def embed(weight: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, stream=None) -> torch.Tensor:
     """scale * weight[ids] (vocab x width by ids of any shape); zeros where an id is outside
     [0, vocab)."""
+    if stream is not None:
+        return _on(stream, embed, weight, ids, scale)
     w, vocab, width, ld = _rows(weight, "weight")
     size = _tokens(ids, "ids")
     dev = w.device
     y = _empty((*ids.shape, width), dtype=w.dtype, device=dev)
-    _check(lib().isoloco_embed(w.data_ptr(), ld, _DTYPE[w.dtype], vocab, width, ids.data_ptr(), size, ids.numel(), scale,
-                               y.data_ptr(), width, _raw_stream(dev.index)), "isoloco_embed")
+    rc = lib().isoloco_embed(w.data_ptr(), ld, _DTYPE[w.dtype], vocab, width, ids.data_ptr(), size, ids.numel(), scale,
+                               y.data_ptr(), width, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "isoloco_embed")
     return y
 
 
-@_on_stream
-def embed_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0, dtype=None) -> torch.Tensor:
+def embed_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0, dtype=None, stream=None) -> torch.Tensor:
     """The lookup's gradient by the whole table (vocab x width, of `dtype`: grad's or fp32), from
     grad = d loss / d embed(weight, ids, scale)."""
+    if stream is not None:
+        return _on(stream, embed_grad, grad, ids, vocab, scale, dtype)
     dy, n, width, ld = _rows(grad, "grad")
     size = _tokens(ids, "ids", n)
     dtype = dtype or dy.dtype
@@ -123,9 +120,10 @@ def embed_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float =
         raise ValueError("vocab must be in 1 .. 2^31 - 1")
     dw = _empty((vocab, width), dtype=dtype, device=dev)
     ws = _empty(need, dtype=torch.uint8, device=dev)
-    _check(L.isoloco_embed_grad(dy.data_ptr(), ld, _DTYPE[dy.dtype], vocab, width, ids.data_ptr(), size, n, scale,
-                                dw.data_ptr(), width, _DTYPE[dtype], ws.data_ptr(), need, _raw_stream(dev.index)),
-           "isoloco_embed_grad")
+    rc = L.isoloco_embed_grad(dy.data_ptr(), ld, _DTYPE[dy.dtype], vocab, width, ids.data_ptr(), size, n, scale,
+                                dw.data_ptr(), width, _DTYPE[dtype], ws.data_ptr(), need, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "isoloco_embed_grad")
     return dw
 
 
@@ -148,25 +146,28 @@ def _ffn_operands(x, w_gate, w_up, act):
     return n, width, ff, (px, ldx, pg, pu, ldw, _HALF[x2.dtype], n, width, ff, _ACT[act]), aligned
 
 
-@_on_stream
-def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: str = "silu", save: bool = False):
+def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: str = "silu", save: bool = False, stream=None):
     """h = act(x w_gate) * (x w_up); w_gate and w_up are width x ff.  With save=True returns
     (h, saved), where `saved` is what gated_ffn_grad needs besides the operands."""
+    if stream is not None:
+        return _on(stream, gated_ffn, x, w_gate, w_up, act, save)
     n, width, ff, args, aligned = _ffn_operands(x, w_gate, w_up, act)
     L, dev, dt = lib(), x.device, x.dtype
     h = _empty((*x.shape[:-1], ff), dtype=dt, device=dev)
     saved = _empty(L.isoloco_gated_ffn_saved_bytes(n, ff, _HALF[dt]), dtype=torch.uint8, device=dev) if save else None
     need = 0 if aligned else L.isoloco_gated_ffn_workspace(n, width, ff, 0)
     ws = _empty(need, dtype=torch.uint8, device=dev) if need else None
-    _check(L.isoloco_gated_ffn(*args, h.data_ptr(), ff, _ptr(saved), _ptr(ws), need, _raw_stream(dev.index)),
-           "isoloco_gated_ffn")
+    rc = L.isoloco_gated_ffn(*args, h.data_ptr(), ff, _ptr(saved), _ptr(ws), need, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "isoloco_gated_ffn")
     return (h, saved) if save else h
 
 
-@_on_stream
 def gated_ffn_grad(grad: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, saved: torch.Tensor,
-                   act: str = "silu", need_x: bool = True, need_w: bool = True):
+                   act: str = "silu", need_x: bool = True, need_w: bool = True, stream=None):
     """(dx, dw_gate, dw_up) for grad = d loss / d h; None for what is not needed."""
+    if stream is not None:
+        return _on(stream, gated_ffn_grad, grad, x, w_gate, w_up, saved, act, need_x, need_w)
     n, width, ff, args, aligned = _ffn_operands(x, w_gate, w_up, act)
     dh, rows, cols, ldh = _rows(grad, "grad", _HALF)
     L, dev, dt = lib(), x.device, x.dtype
@@ -180,8 +181,10 @@ def gated_ffn_grad(grad: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_
     dwu = _empty((width, ff), dtype=dt, device=dev) if need_w else None
     need = L.isoloco_gated_ffn_grad_workspace(n, width, ff, aligned)
     ws = _empty(need, dtype=torch.uint8, device=dev)
-    _check(L.isoloco_gated_ffn_grad(dh.data_ptr(), ldh, *args, saved.data_ptr(), _ptr(dx), width, _ptr(dwg), _ptr(dwu), ff,
-                                    ws.data_ptr(), need, _raw_stream(dev.index)), "isoloco_gated_ffn_grad")
+    rc = L.isoloco_gated_ffn_grad(dh.data_ptr(), ldh, *args, saved.data_ptr(), _ptr(dx), width, _ptr(dwg), _ptr(dwu), ff,
+                                    ws.data_ptr(), need, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "isoloco_gated_ffn_grad")
     return dx, dwg, dwu
 
 
@@ -210,13 +213,14 @@ def _like_rows(z, shape, vocab, ld, dev):
     return _empty((*shape[:-1], ld), dtype=z.dtype, device=dev)[..., :vocab]
 
 
-@_on_stream
 def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, top: int = 0,
-                   grad_logp: Optional[torch.Tensor] = None, grad_entropy: Optional[torch.Tensor] = None) -> TokenLogprobs:
+                   grad_logp: Optional[torch.Tensor] = None, grad_entropy: Optional[torch.Tensor] = None, stream=None) -> TokenLogprobs:
     """Log probability of each row's target under softmax(scale * logits), the rows' entropies and
     logarithms of the sum of exponentials, and the `top` likeliest tokens (ties: the lowest index).
     With grad_logp or grad_entropy (a gradient per row, known in advance as for a weighted sum of log
     probabilities) the same call returns the gradient by the logits."""
+    if stream is not None:
+        return _on(stream, token_logprobs, logits, targets, scale, top, grad_logp, grad_entropy)
     z, n, vocab, ld = _rows(logits, "logits")
     size = _tokens(targets, "targets", n)
     if not 0 <= top <= min(vocab, MAX_TOP):
@@ -230,26 +234,31 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1
     tl = _empty((*lead, top), dtype=torch.float32, device=dev) if top else None
     ti = _empty((*lead, top), dtype=torch.int64, device=dev) if top else None
     gz = _like_rows(z, shape, vocab, ld, dev) if gl is not None or ge is not None else None
-    _check(lib().isoloco_token_logprobs(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, targets.data_ptr(), size, scale,
+    rc = lib().isoloco_token_logprobs(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, targets.data_ptr(), size, scale,
                                         logp.data_ptr(), ent.data_ptr(), lse.data_ptr(), top, _ptr(tl), _ptr(ti), gl, ge,
-                                        _ptr(gz), ld, _raw_stream(dev.index)), "isoloco_token_logprobs")
+                                        _ptr(gz), ld, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "isoloco_token_logprobs")
     return TokenLogprobs(logp, ent, lse, tl, ti, gz)
 
 
-@_on_stream
 def token_logprobs_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, entropy: Optional[torch.Tensor],
                         grad_logp: Optional[torch.Tensor], grad_entropy: Optional[torch.Tensor],
-                        scale: float = 1.0) -> torch.Tensor:
+                        scale: float = 1.0, stream=None) -> torch.Tensor:
     """The gradient by the logits alone, from the lse and entropy of token_logprobs (backward pass of
     an autograd step, where the rows' gradients come later)."""
+    if stream is not None:
+        return _on(stream, token_logprobs_grad, logits, targets, lse, entropy, grad_logp, grad_entropy, scale)
     z, n, vocab, ld = _rows(logits, "logits")
     size = _tokens(targets, "targets", n)
     dev = z.device
     gz = _like_rows(z, logits.shape, vocab, ld, dev)
-    _check(lib().isoloco_token_logprobs_grad(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, targets.data_ptr(), size, scale,
+    rc = lib().isoloco_token_logprobs_grad(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, targets.data_ptr(), size, scale,
                                              _per_row(lse, n, "lse"), _per_row(entropy, n, "entropy"),
                                              _per_row(grad_logp, n, "grad_logp"), _per_row(grad_entropy, n, "grad_entropy"),
-                                             gz.data_ptr(), ld, _raw_stream(dev.index)), "isoloco_token_logprobs_grad")
+                                             gz.data_ptr(), ld, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "isoloco_token_logprobs_grad")
     return gz
 
 
@@ -266,23 +275,27 @@ def _tensor_list(tensors: Sequence[torch.Tensor], what: str):
     return words
 
 
-@_on_stream
-def grad_norm(grads: Sequence[torch.Tensor]) -> torch.Tensor:
+def grad_norm(grads: Sequence[torch.Tensor], stream=None) -> torch.Tensor:
     """The norm over all entries of all tensors, a 0-d fp32 tensor on the device."""
+    if stream is not None:
+        return _on(stream, grad_norm, grads)
     grads = list(grads)
     words = _tensor_list(grads, "grads")
     L, n, dev, arr = lib(), len(grads), _current_device(), words.buffer_info()[0]
     need = L.isoloco_grad_norm_workspace(arr, n)
     norm = _empty((), dtype=torch.float32, device=dev)
     ws = _empty(need, dtype=torch.uint8, device=dev) if need else None
-    _check(L.isoloco_grad_norm(arr, n, norm.data_ptr(), _ptr(ws), need, _raw_stream(dev)), "isoloco_grad_norm")
+    rc = L.isoloco_grad_norm(arr, n, norm.data_ptr(), _ptr(ws), need, _raw_stream(dev))
+    if rc:
+        _check(rc, "isoloco_grad_norm")
     return norm
 
 
-@_on_stream
-def clip_grads(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
+def clip_grads(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None, stream=None) -> torch.Tensor:
     """Scales the gradient by min(1, max_norm / norm), in place or into `out`, and returns the norm
     (0-d, fp32).  A NaN or infinite norm scales nothing."""
+    if stream is not None:
+        return _on(stream, clip_grads, grads, max_norm, out)
     grads = list(grads)
     words, outs = _tensor_list(grads, "grads"), None
     if out is not None:
@@ -294,8 +307,10 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Seq
     need = L.isoloco_grad_norm_workspace(arr, n)
     norm = _empty((), dtype=torch.float32, device=dev)
     ws = _empty(need, dtype=torch.uint8, device=dev) if need else None
-    _check(L.isoloco_clip_grads(arr, outs and outs.buffer_info()[0], n, max_norm, norm.data_ptr(), _ptr(ws), need,
-                                _raw_stream(dev)), "isoloco_clip_grads")
+    rc = L.isoloco_clip_grads(arr, outs and outs.buffer_info()[0], n, max_norm, norm.data_ptr(), _ptr(ws), need,
+                                _raw_stream(dev))
+    if rc:
+        _check(rc, "isoloco_clip_grads")
     return norm
 
 
