@@ -7,6 +7,10 @@
 // (fp32 within a thread, fp64 from there on) and leaves one fp64 partial per CTA; the second adds the
 // partials, every CTA in the same order, so that all have the same bits, and scales.  A short list of
 // small tensors takes one launch of one cluster (k_grad_small), whose CTAs exchange their sums in shared memory.
+//
+// Bound by HBM.  219.7 M fp32 entries in 110 tensors: squares 127 us (6.9 TB/s), scaling into other tensors
+// 267 us (6.6 TB/s of the second read and the write; of the 64 MB that the first pass leaves in L2 it
+// gains 2 us).
 #include <algorithm>
 #include <cmath>
 
