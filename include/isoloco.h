@@ -375,7 +375,8 @@ typedef enum { ISOLOCO_SILU = 0, ISOLOCO_GELU_TANH = 1 } isoloco_act_t;
 
 /* Embedding lookup: y[t][:] = scale * weight[ids[t]][:], zeros where ids[t] is no token.
  *   weight: vocab x width; y: tokens x width; both of `dtype`.  ids: tokens entries of
- *   id_bytes (4 or 8) bytes, signed.  Sizes may be 0 (tokens) and up to 2^31 - 1. */
+ *   id_bytes (4 or 8) bytes, signed.  vocab and tokens up to 2^31 - 1 (tokens may be 0), width up to
+ *   2^20. */
 int isoloco_embed(const void* weight, int64_t ld_weight, isoloco_dtype_t dtype, int64_t vocab, int64_t width,
                   const void* ids, int id_bytes, int64_t tokens, float scale, void* y, int64_t ld_y, void* stream);
 
@@ -393,7 +394,7 @@ int isoloco_embed_grad(const void* dy, int64_t ld_dy, isoloco_dtype_t dtype, int
  *   matrices); h: tokens x ff.  dtype BF16 or F16 for all.
  *   saved: NULL, or isoloco_gated_ffn_saved_bytes() bytes, 16-byte aligned, that receive x w_gate and
  *   x w_up for isoloco_gated_ffn_grad: in fp32 for F16, in 16 bits (10 of them significant, magnitudes
- *   to 2^33, larger ones cut off there) for BF16.
+ *   below 2^33: what lies beyond makes the gradient NaN) for BF16.
  *   Workspace: aligned = 1 when the addresses and pitches of all matrices (without dh) are multiples of
  *   16 bytes; 0 any others, which are copied to and from rows that are.
  *   tokens up to 2^30, width and ff up to 2^20. */

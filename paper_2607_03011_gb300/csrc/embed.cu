@@ -28,15 +28,15 @@ namespace {
 constexpr int kRowThreads = 128;
 
 // ------------------------------------------------------------------ lookup
-// Pieces (16 bytes when VEC, else one element) of all rows of y in one sequence; a thread takes N of them,
+// Pieces (16 bytes when VEC, else put_piece's) of all rows of y in one sequence; a thread takes N of them,
 // kLookThreads apart, so that N rows' ids and then N pieces of the table are in flight.
 constexpr int kLookThreads = 256;
 
 template <class T, class I, bool VEC, int N>
-__global__ void __launch_bounds__(kLookThreads) k_embed(const T* __restrict__ w, int64_t ld_w, int64_t vocab, uint32_t pieces,
+__global__ void __launch_bounds__(kLookThreads) k_embed(const T* __restrict__ w, int64_t ld_w, int64_t vocab, int64_t width, uint32_t pieces,
                                                         const I* __restrict__ ids, int64_t tokens, float scale, T* __restrict__ y,
                                                         int64_t ld_y) {
-    constexpr int V = VEC ? Vec<T>::kN : 1;
+    constexpr int V = Vec<T>::kN;
     const int64_t total = tokens * pieces;
     for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * (kLookThreads * N) + threadIdx.x; i0 < total;
          i0 += static_cast<int64_t>(gridDim.x) * (kLookThreads * N)) {
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(kLookThreads) k_embed(const T* __restrict__ w,
         for (int q = 0; q < N; ++q) {
             const int64_t i = min(i0 + q * kLookThreads, total - 1);
             t[q] = total <= 0xffffffffll ? static_cast<int64_t>(static_cast<uint32_t>(i) / pieces) : i / pieces;
-            c[q] = static_cast<uint32_t>(i - t[q] * pieces) * V;
+            c[q] = static_cast<uint32_t>(i - t[q] * pieces);
             id[q] = token_at(ids, t[q], vocab);
         }
         if constexpr (VEC) {
@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(kLookThreads) k_embed(const T* __restrict__ w,
 #pragma unroll
             for (int q = 0; q < N; ++q) {
                 v[q].raw = make_uint4(0, 0, 0, 0);
-                if (id[q] >= 0) v[q].raw = __ldg(reinterpret_cast<const uint4*>(w + id[q] * ld_w + c[q]));
+                if (id[q] >= 0) v[q].raw = __ldg(reinterpret_cast<const uint4*>(w + id[q] * ld_w + static_cast<int64_t>(c[q]) * V));
             }
 #pragma unroll
             for (int q = 0; q < N; ++q) {
@@ -66,14 +66,13 @@ __global__ void __launch_bounds__(kLookThreads) k_embed(const T* __restrict__ w,
                     for (int j = 0; j < V; ++j) f[j] *= scale;
                     v[q].pack(f);
                 }
-                st_stream(y + t[q] * ld_y + c[q], v[q].raw);
+                st_stream(y + t[q] * ld_y + static_cast<int64_t>(c[q]) * V, v[q].raw);
             }
         } else {
 #pragma unroll
             for (int q = 0; q < N; ++q) {
                 if (i0 + q * kLookThreads >= total) break;
-                const T v = id[q] >= 0 ? w[id[q] * ld_w + c[q]] : from_f32<T>(0.f);
-                y[t[q] * ld_y + c[q]] = scale == 1.f || id[q] < 0 ? v : from_f32<T>(to_f32(v) * scale);
+                put_piece(id[q] >= 0 ? w + id[q] * ld_w : nullptr, y + t[q] * ld_y, width, c[q], scale);
             }
         }
     }
@@ -357,11 +356,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(int64_t width, cons
 }
 
 template <class T, class I, bool VEC, int N>
-cudaError_t embed_n(const void* w, int64_t ld_w, int64_t vocab, int64_t pieces, const void* ids, int64_t tokens, float scale, void* y,
+cudaError_t embed_n(const void* w, int64_t ld_w, int64_t vocab, int64_t width, int64_t pieces, const void* ids, int64_t tokens, float scale, void* y,
                     int64_t ld_y, cudaStream_t st) {
     const int64_t blocks = (tokens * pieces + kLookThreads * N - 1) / (kLookThreads * N);
     k_embed<T, I, VEC, N><<<static_cast<unsigned>(std::min<int64_t>(blocks, int64_t(1) << 30)), kLookThreads, 0, st>>>(
-        static_cast<const T*>(w), ld_w, vocab, static_cast<uint32_t>(pieces), static_cast<const I*>(ids), tokens, scale, static_cast<T*>(y),
+        static_cast<const T*>(w), ld_w, vocab, width, static_cast<uint32_t>(pieces), static_cast<const I*>(ids), tokens, scale, static_cast<T*>(y),
         ld_y);
     return cudaGetLastError();
 }
@@ -374,10 +373,10 @@ cudaError_t embed_t(const void* w, int64_t ld_w, int64_t vocab, int64_t width, c
     const cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;
     const bool vec = aligned16(w) && aligned16(y) && ld_w % V == 0 && ld_y % V == 0 && width % V == 0;
-    const int64_t pieces = vec ? width / V : width;
+    const int64_t pieces = vec ? width / V : any_pieces(width, V);
     // four pieces per thread once that still leaves every SM a few CTAs
     const bool many = tokens * pieces >= int64_t(4) * 4 * kLookThreads * sms;
-#define LOOK(VEC, N) embed_n<T, I, VEC, N>(w, ld_w, vocab, pieces, ids, tokens, scale, y, ld_y, st)
+#define LOOK(VEC, N) embed_n<T, I, VEC, N>(w, ld_w, vocab, width, pieces, ids, tokens, scale, y, ld_y, st)
     return vec ? (many ? LOOK(true, 4) : LOOK(true, 1)) : (many ? LOOK(false, 4) : LOOK(false, 1));
 #undef LOOK
 }
@@ -404,7 +403,7 @@ cudaError_t embed_grad_t(const void* dy, int64_t ld_dy, int64_t vocab, int64_t w
                          void* dw, int64_t ld_dw, int sms, cudaStream_t st) {
     constexpr int64_t V = Vec<T>::kN;
     const bool vec = aligned16(dy) && ld_dy % V == 0 && width % V == 0;
-    const int64_t cols = vec ? width / V : width;
+    const int64_t cols = vec ? width / V : width;  // (16 bytes put together from two pieces: 149 us where single columns take 122)
     const int len = span_of(n);
     const unsigned spans = static_cast<unsigned>((n + len - 1) / len);
     const dim3 grid(spans, static_cast<unsigned>((cols + kRowThreads - 1) / kRowThreads));

@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(256) k_ffn_dgu(const T* __restrict__ dh, int64
 }
 
 // ------------------------------------------------------------------ few tokens
-constexpr int kGemvTokens = 8;
+constexpr int kGemvTokens = 2;    // (2048 x 5632 bf16: 14.9 us for 2 tokens, 21 for 4; the pair GEMM takes 18 for 9)
 constexpr int kFewThreads = 256;
 constexpr int kFewCols = 64;      // columns of F per cluster: 8 lanes of 16 bytes, whole 128-byte lines
 constexpr int kFewMaxSplit = 8;   // CTAs of a cluster, each a share of D
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kFewThreads) k_ffn_few(const T* __restrict__ x
     if (n < ff) {  // (ff <= pitch, a multiple of 8: the last 16 bytes of a row exist)
         const T* pg = wg + static_cast<int64_t>(d0) * ld_w + n;
         const T* pu = wu + static_cast<int64_t>(d0) * ld_w + n;
-#pragma unroll (NT <= 2 ? 8 : NT <= 4 ? 4 : 2)
+#pragma unroll 8
         for (int r = warp * 4 + (lane >> 3); r < rows; r += 32) {
             Vec<T> a, b;
             a.raw = __ldg(reinterpret_cast<const uint4*>(pg + r * ld_w));
@@ -198,17 +198,24 @@ __global__ void __launch_bounds__(kFewThreads) k_ffn_few(const T* __restrict__ x
 // ------------------------------------------------------------------ pitches
 // dst[r][0 .. cols) = src[r][0 .. cols), any pitches: operands that 16-byte accesses cannot read go through
 // the workspace (an extra read and write of them), and outputs come back the same way.
-__global__ void __launch_bounds__(256) k_repitch(const uint16_t* __restrict__ src, int64_t ld_s, uint16_t* __restrict__ dst, int64_t ld_d,
-                                                 int64_t rows, int64_t cols) {
-    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
-        for (int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; c < cols; c += static_cast<int64_t>(gridDim.x) * 256)
-            dst[r * ld_d + c] = src[r * ld_s + c];
+__global__ void __launch_bounds__(256) k_repitch(const __nv_bfloat16* __restrict__ src, int64_t ld_s, __nv_bfloat16* __restrict__ dst, int64_t ld_d,
+                                                 int64_t rows, int64_t cols, uint32_t pieces) {
+    const int64_t total = rows * pieces;
+#pragma unroll 4
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t r = total <= 0xffffffffll ? static_cast<int64_t>(static_cast<uint32_t>(i) / pieces) : i / pieces;
+        put_piece(src + r * ld_s, dst + r * ld_d, cols, static_cast<uint32_t>(i - r * pieces), 1.f);
+    }
 }
 
 cudaError_t repitch(const void* src, int64_t ld_s, void* dst, int64_t ld_d, int64_t rows, int64_t cols, cudaStream_t st) {
     if (rows == 0) return cudaSuccess;
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((cols + 255) / 256, 64)), static_cast<unsigned>(std::min<int64_t>(rows, 16384)));
-    k_repitch<<<grid, 256, 0, st>>>(static_cast<const uint16_t*>(src), ld_s, static_cast<uint16_t*>(dst), ld_d, rows, cols);
+    int sms = 0;
+    const cudaError_t e = device_sms(&sms);
+    if (e != cudaSuccess) return e;
+    const uint32_t pieces = any_pieces(cols, 8);
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>((rows * pieces + 255) / 256, 32 * sms));
+    k_repitch<<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(src), ld_s, static_cast<__nv_bfloat16*>(dst), ld_d, rows, cols, pieces);
     return cudaGetLastError();
 }
 
@@ -368,13 +375,7 @@ template <class T, bool GELU>
 cudaError_t few(const FfnArgs& a, const void* wg, const void* wu, int64_t ld_w, void* h, int64_t ld_h, void* saved, cudaStream_t st) {
     switch (a.tokens) {
         case 1: return few_n<T, 1, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
-        case 2: return few_n<T, 2, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
-        case 3: return few_n<T, 3, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
-        case 4: return few_n<T, 4, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
-        case 5: return few_n<T, 5, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
-        case 6: return few_n<T, 6, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
-        case 7: return few_n<T, 7, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
-        default: return few_n<T, 8, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
+        default: return few_n<T, 2, GELU>(a, wg, wu, ld_w, h, ld_h, saved, st);
     }
 }
 

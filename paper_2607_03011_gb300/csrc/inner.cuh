@@ -93,6 +93,55 @@ __device__ __forceinline__ void st_stream(void* p, uint4 v) { __stcs(reinterpret
 
 __host__ __device__ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// 16 bytes from an address that is a multiple of 2: the aligned pieces that hold them, shifted together.
+__device__ __forceinline__ uint4 load16_any(const void* p) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    const uint4* q = reinterpret_cast<const uint4*>(at & ~uintptr_t(15));
+    const uint32_t off = static_cast<uint32_t>(at & 15u);
+    const uint4 a = __ldg(q);
+    if (off == 0) return a;
+    const uint4 b = __ldg(q + 1);
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (off & 8u) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (off & 4u) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    const uint32_t bits = (off & 3u) * 8u;
+    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                      __funnelshift_r(w[3], w[4], bits));
+}
+
+// Rows whose addresses are no multiples of 16 bytes are written in pieces: piece 0 the elements before the row's first
+// 16-byte boundary, piece j the j-th 16 bytes behind it, the last cut short by the row's end.
+__host__ __device__ __forceinline__ uint32_t any_pieces(int64_t cols, int per_vec) { return static_cast<uint32_t>((cols + per_vec - 1) / per_vec + 1); }
+
+// Piece j of dst[0 .. cols) = scale src[0 .. cols), zeros without src.
+template <class T>
+__device__ __forceinline__ void put_piece(const T* src, T* dst, int64_t cols, uint32_t j, float scale) {
+    constexpr int V = Vec<T>::kN;
+    const uint32_t mis = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(dst) & 15u);
+    const int64_t head = min(cols, static_cast<int64_t>(mis ? (16u - mis) / sizeof(T) : 0u));
+    const int64_t from = j ? head + static_cast<int64_t>(j - 1) * V : 0, to = j ? min(cols, from + V) : head;
+    if (j && from + V <= cols) {
+        Vec<T> v;
+        v.raw = src ? load16_any(src + from) : make_uint4(0, 0, 0, 0);
+        if (scale != 1.f && src) {
+            float f[V];
+            v.unpack(f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[i] *= scale;
+            v.pack(f);
+        }
+        st_stream(dst + from, v.raw);
+    } else {
+        for (int64_t i = from; i < to; ++i) dst[i] = !src ? from_f32<T>(0.f) : scale == 1.f ? src[i] : from_f32<T>(to_f32(src[i]) * scale);
+    }
+}
+
 // The token id at position t, or -1 where it is none of [0, vocab).
 template <class I>
 __device__ __forceinline__ int64_t token_at(const I* ids, int64_t t, int64_t vocab) {

@@ -29,6 +29,8 @@ using namespace isoloco;
 namespace {
 
 constexpr int64_t kMaxSize = INT_MAX;
+// No exception passes an entry point: what may be thrown here is for want of memory (a message's text).
+constexpr int kNoMemory = ISOLOCO_ERR_OOM;
 
 int invalid(const char* what) { return set_error(ISOLOCO_ERR_INVALID, what); }
 
@@ -59,7 +61,8 @@ cudaStream_t stream_of(void* s) { return static_cast<cudaStream_t>(s); }
 
 const char* embed_problem(int dtype, int64_t vocab, int64_t width, const void* ids, int id_bytes, int64_t tokens) {
     if (!any_dtype(dtype)) return "bad element type";
-    if (!size_ok(vocab, 1) || !size_ok(width, 1) || !size_ok(tokens, 0)) return "vocab and width must be in 1 .. 2^31 - 1, tokens in 0 .. 2^31 - 1";
+    if (!size_ok(vocab, 1) || !size_ok(width, 1) || width > (1 << 20) || !size_ok(tokens, 0))
+        return "vocab must be in 1 .. 2^31 - 1, width in 1 .. 2^20, tokens in 0 .. 2^31 - 1";
     if (id_bytes != 4 && id_bytes != 8) return "id_bytes must be 4 or 8";
     if (!array_ok(ids, tokens, id_bytes)) return "ids is NULL or misaligned";
     return nullptr;
@@ -106,22 +109,26 @@ const char* tensors_problem(const isoloco_tensor_t* t, int count) {
 extern "C" {
 
 int isoloco_embed(const void* weight, int64_t ld_weight, isoloco_dtype_t dtype, int64_t vocab, int64_t width,
-                  const void* ids, int id_bytes, int64_t tokens, float scale, void* y, int64_t ld_y, void* stream) {
+                  const void* ids, int id_bytes, int64_t tokens, float scale, void* y, int64_t ld_y, void* stream) try {
     if (const char* p = embed_problem(dtype, vocab, width, ids, id_bytes, tokens)) return invalid(p);
     const int es = elem_size(dtype);
     if (!matrix_ok(weight, vocab, width, ld_weight, es)) return invalid("weight is NULL, misaligned or its pitch too small");
     if (!matrix_ok(y, tokens, width, ld_y, es)) return invalid("y is NULL, misaligned or its pitch too small");
     return cuda_status(launch_embed(weight, ld_weight, dtype, vocab, width, ids, id_bytes == 8, tokens, scale, y, ld_y, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
 }
 
-int64_t isoloco_embed_grad_workspace(int64_t vocab, int64_t width, int64_t tokens) {
+int64_t isoloco_embed_grad_workspace(int64_t vocab, int64_t width, int64_t tokens) try {
     if (!size_ok(vocab, 1) || !size_ok(width, 1) || !size_ok(tokens, 0)) return ISOLOCO_ERR_INVALID;
     return embed_grad_workspace(vocab, width, tokens);
+} catch (...) {
+    return kNoMemory;
 }
 
 int isoloco_embed_grad(const void* dy, int64_t ld_dy, isoloco_dtype_t dtype, int64_t vocab, int64_t width,
                        const void* ids, int id_bytes, int64_t tokens, float scale, void* dw, int64_t ld_dw,
-                       isoloco_dtype_t dw_dtype, void* workspace, int64_t workspace_bytes, void* stream) {
+                       isoloco_dtype_t dw_dtype, void* workspace, int64_t workspace_bytes, void* stream) try {
     if (const char* p = embed_problem(dtype, vocab, width, ids, id_bytes, tokens)) return invalid(p);
     if (dw_dtype != dtype && dw_dtype != ISOLOCO_F32) return invalid("dw is of dy's type or F32");
     if (!matrix_ok(dy, tokens, width, ld_dy, elem_size(dtype))) return invalid("dy is NULL, misaligned or its pitch too small");
@@ -130,26 +137,34 @@ int isoloco_embed_grad(const void* dy, int64_t ld_dy, isoloco_dtype_t dtype, int
     if (rc != ISOLOCO_OK) return rc;
     return cuda_status(launch_embed_grad(dy, ld_dy, dtype, vocab, width, ids, id_bytes == 8, tokens, scale, dw, ld_dw, dw_dtype,
                                          workspace, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
 }
 
-int64_t isoloco_gated_ffn_saved_bytes(int64_t tokens, int64_t ff, isoloco_dtype_t dtype) {
+int64_t isoloco_gated_ffn_saved_bytes(int64_t tokens, int64_t ff, isoloco_dtype_t dtype) try {
     if (!size_ok(tokens, 0) || !size_ok(ff, 1) || !half_dtype(dtype)) return ISOLOCO_ERR_INVALID;
     return ffn_saved_bytes(tokens, ff, dtype);
+} catch (...) {
+    return kNoMemory;
 }
 
-int64_t isoloco_gated_ffn_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned) {
+int64_t isoloco_gated_ffn_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned) try {
     if (!size_ok(tokens, 0) || !size_ok(width, 1) || !size_ok(ff, 1)) return ISOLOCO_ERR_INVALID;
     return ffn_workspace(tokens, width, ff, false, aligned != 0);
+} catch (...) {
+    return kNoMemory;
 }
 
-int64_t isoloco_gated_ffn_grad_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned) {
+int64_t isoloco_gated_ffn_grad_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned) try {
     if (!size_ok(tokens, 0) || !size_ok(width, 1) || !size_ok(ff, 1)) return ISOLOCO_ERR_INVALID;
     return ffn_workspace(tokens, width, ff, true, aligned != 0);
+} catch (...) {
+    return kNoMemory;
 }
 
 int isoloco_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w,
                       isoloco_dtype_t dtype, int64_t tokens, int64_t width, int64_t ff, isoloco_act_t act, void* h,
-                      int64_t ld_h, void* saved, void* workspace, int64_t workspace_bytes, void* stream) {
+                      int64_t ld_h, void* saved, void* workspace, int64_t workspace_bytes, void* stream) try {
     const FfnArgs a = {x, w_gate, w_up, ld_x, ld_w, tokens, width, ff, dtype, act};
     if (const char* p = ffn_problem(a)) return invalid(p);
     if (!matrix_ok(h, tokens, ff, ld_h, 2)) return invalid("h is NULL, misaligned or its pitch too small");
@@ -158,12 +173,14 @@ int isoloco_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, const voi
         rows16(x, ld_x, tokens) && rows16(w_gate, ld_w, width) && rows16(w_up, ld_w, width) && rows16(h, ld_h, tokens)));
     if (rc != ISOLOCO_OK) return rc;
     return cuda_status(launch_ffn(a, h, ld_h, saved, workspace, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
 }
 
 int isoloco_gated_ffn_grad(const void* dh, int64_t ld_dh, const void* x, int64_t ld_x, const void* w_gate,
                            const void* w_up, int64_t ld_w, isoloco_dtype_t dtype, int64_t tokens, int64_t width,
                            int64_t ff, isoloco_act_t act, const void* saved, void* dx, int64_t ld_dx, void* dw_gate,
-                           void* dw_up, int64_t ld_dw, void* workspace, int64_t workspace_bytes, void* stream) {
+                           void* dw_up, int64_t ld_dw, void* workspace, int64_t workspace_bytes, void* stream) try {
     const FfnArgs a = {x, w_gate, w_up, ld_x, ld_w, tokens, width, ff, dtype, act};
     if (const char* p = ffn_problem(a)) return invalid(p);
     if (!matrix_ok(dh, tokens, ff, ld_dh, 2)) return invalid("dh is NULL, misaligned or its pitch too small");
@@ -178,24 +195,28 @@ int isoloco_gated_ffn_grad(const void* dh, int64_t ld_dh, const void* x, int64_t
         (!dw_gate || (rows16(dw_gate, ld_dw, width) && rows16(dw_up, ld_dw, width)))));
     if (rc != ISOLOCO_OK) return rc;
     return cuda_status(launch_ffn_grad(a, dh, ld_dh, saved, dx, ld_dx, dw_gate, dw_up, ld_dw, workspace, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
 }
 
 int isoloco_token_logprobs(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows, int64_t vocab,
                            const void* targets, int target_bytes, float scale, float* logp, float* entropy, float* lse,
                            int top, float* top_logp, int64_t* top_index, const float* grad_logp,
-                           const float* grad_entropy, void* grad_logits, int64_t ld_grad, void* stream) {
+                           const float* grad_entropy, void* grad_logits, int64_t ld_grad, void* stream) try {
     const LogprobArgs a = {logits, ld_logits, rows, vocab, dtype, targets, target_bytes == 8, scale, logp, entropy, lse, top,
                            top_logp, top_index, grad_logp, grad_entropy, grad_logits, ld_grad};
     if (const char* p = logprob_problem(a, target_bytes)) return invalid(p);
     if (top < 0 || top > ISOLOCO_MAX_TOP || top > vocab) return invalid("top must be in 0 .. min(vocab, 32)");
     if (top && (!array_ok(top_logp, rows, 4) || !array_ok(top_index, rows, 8))) return invalid("top_logp or top_index is NULL or misaligned");
     return cuda_status(launch_logprobs(a, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
 }
 
 int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows,
                                 int64_t vocab, const void* targets, int target_bytes, float scale, const float* lse,
                                 const float* entropy, const float* grad_logp, const float* grad_entropy,
-                                void* grad_logits, int64_t ld_grad, void* stream) {
+                                void* grad_logits, int64_t ld_grad, void* stream) try {
     const LogprobArgs a = {logits, ld_logits, rows, vocab, dtype, targets, target_bytes == 8, scale, nullptr,
                            const_cast<float*>(entropy), const_cast<float*>(lse), 0, nullptr, nullptr, grad_logp, grad_entropy,
                            grad_logits, ld_grad};
@@ -204,23 +225,29 @@ int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_d
     if (rows > 0 && !grad_logits) return invalid("grad_logits is NULL");
     if (grad_entropy && !array_ok(entropy, rows, 4)) return invalid("entropy is NULL or misaligned");
     return cuda_status(launch_logprobs_grad(a, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
 }
 
-int64_t isoloco_grad_norm_workspace(const isoloco_tensor_t* tensors, int count) {
+int64_t isoloco_grad_norm_workspace(const isoloco_tensor_t* tensors, int count) try {
     return tensors_problem(tensors, count) ? ISOLOCO_ERR_INVALID : grad_norm_workspace(tensors, count);
+} catch (...) {
+    return kNoMemory;
 }
 
 int isoloco_grad_norm(const isoloco_tensor_t* tensors, int count, float* norm, void* workspace,
-                      int64_t workspace_bytes, void* stream) {
+                      int64_t workspace_bytes, void* stream) try {
     if (const char* p = tensors_problem(tensors, count)) return invalid(p);
     if (!array_ok(norm, 1, 4)) return invalid("norm is NULL or misaligned");
     const int rc = workspace_ok(workspace, workspace_bytes, grad_norm_workspace(tensors, count));
     if (rc != ISOLOCO_OK) return rc;
     return cuda_status(launch_clip(tensors, nullptr, count, false, 0.f, norm, workspace, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
 }
 
 int isoloco_clip_grads(const isoloco_tensor_t* tensors, const isoloco_tensor_t* outs, int count, float max_norm,
-                       float* norm, void* workspace, int64_t workspace_bytes, void* stream) {
+                       float* norm, void* workspace, int64_t workspace_bytes, void* stream) try {
     if (const char* p = tensors_problem(tensors, count)) return invalid(p);
     if (outs) {
         if (const char* p = tensors_problem(outs, count)) return invalid(p);
@@ -232,9 +259,11 @@ int isoloco_clip_grads(const isoloco_tensor_t* tensors, const isoloco_tensor_t* 
     const int rc = workspace_ok(workspace, workspace_bytes, grad_norm_workspace(tensors, count));
     if (rc != ISOLOCO_OK) return rc;
     return cuda_status(launch_clip(tensors, outs, count, true, max_norm, norm, workspace, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
 }
 
-int isoloco_inner_status(void* stream) {
+int isoloco_inner_status(void* stream) try {
     uint32_t *word = nullptr, bits = 0;
     cudaStream_t st = stream_of(stream);
     cudaError_t e = error_word(&word);
@@ -243,6 +272,8 @@ int isoloco_inner_status(void* stream) {
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (e != cudaSuccess) return cuda_status(e);
     return (bits & kErrTimeout) ? set_error(ISOLOCO_ERR_TIMEOUT, "a wait in an inner-step kernel gave up") : ISOLOCO_OK;
+} catch (...) {
+    return kNoMemory;
 }
 
 }  // extern "C"

@@ -35,6 +35,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kGroups = 64;         // of threads, at least 2 ISOLOCO_MAX_TOP
 constexpr int kCandidates = 1024;   // entries a CTA ranks: all that a row of equal logits gives, 32 per group and `top`
 constexpr int kMaxSplit = 8;
+// A row's share of a CTA with gradient: 760 of them at once are 73 MB (4096 x 128000 fp32: 721 us in shares of 64 KB,
+// 957 in shares of 128, 1029 in whole rows).
+constexpr int64_t kShareBytes = 98304;
 constexpr int kUnroll = 4;
 // Threads per SM the registers are cut for: 5 CTAs of 256 (8192 x 32000 bf16 with gradient 180 us; 4 CTAs, with
 // 64 registers, 194; 6, with 40, 188; 8 of 128 threads 229).
@@ -313,7 +316,7 @@ __device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int 
 }
 
 template <class T, class I, int THREADS, bool TOP, bool GRAD>
-__global__ void __launch_bounds__(THREADS, kThreadsPerSm / THREADS) k_logprobs(LogprobArgs a, uint32_t split) {
+__global__ void __launch_bounds__(THREADS, kThreadsPerSm / THREADS > 32 ? 32 : kThreadsPerSm / THREADS) k_logprobs(LogprobArgs a, uint32_t split) {
     constexpr int V = Vec<T>::kN;
     __shared__ Stat sm[THREADS / 32];
     __shared__ Stat peer[kMaxSplit];  // the sums of every CTA of the cluster
@@ -559,9 +562,13 @@ __global__ void __launch_bounds__(256) k_logprobs_grad(LogprobArgs a) {
 
 template <class T, class I, int THREADS, bool TOP, bool GRAD>
 cudaError_t launch_rows(const LogprobArgs& a, int sms, cudaStream_t st) {
-    // a row to one CTA where rows fill the GPU; else a cluster of up to 8, at least 4096 entries each
+    // a row to one CTA where rows fill the GPU; else a cluster of up to 8, at least 4096 entries each.  With the
+    // gradient also where the rows that are under way at once would not stay in L2 for its second pass: shares of
+    // kShareBytes
     uint32_t split = 1;
-    while (split < kMaxSplit && a.rows * split * 2 <= 2 * sms && a.vocab / (2 * split) >= 4096) split *= 2;
+    while (split < kMaxSplit && ((a.rows * split * 2 <= 2 * sms && a.vocab / (2 * split) >= 4096) ||
+                                 (GRAD && a.vocab * static_cast<int64_t>(sizeof(T)) > split * kShareBytes)))
+        split *= 2;
     const int64_t rows = std::min<int64_t>(a.rows, int64_t(1) << 24);
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -584,8 +591,11 @@ cudaError_t run(const LogprobArgs& a, cudaStream_t st) {
 #define ROWS(N)                                                                                   \
     (a.grad_logits ? (a.top ? launch_rows<T, I, N, true, true>(a, sms, st) : launch_rows<T, I, N, false, true>(a, sms, st)) \
                    : (a.top ? launch_rows<T, I, N, true, false>(a, sms, st) : launch_rows<T, I, N, false, false>(a, sms, st)))
-    // (a short row is a few vectors per thread: more rows at once instead)
-    return a.vocab <= 4096 ? ROWS(128) : ROWS(256);
+    // A short row is a few vectors per thread and its reductions weigh more: smaller CTAs, more rows at once (8192
+    // bf16 rows without / with gradient: of 8000 32 / 62 us with 64 threads, 36 / 64 with 128; of 16000 52 / 103
+    // with 128, 64 / 116 with 256; of 32000 with gradient 229 with 128, 180 with 256).
+    if (a.vocab <= 8192) return ROWS(64);
+    return a.vocab <= 16384 ? ROWS(128) : ROWS(256);
 #undef ROWS
 }
 

@@ -37,9 +37,14 @@ _is_contiguous, _get_device = torch.Tensor.is_contiguous, torch.Tensor.get_devic
 
 
 def _on(stream, f, *args):
-    """The call f(*args) with `stream` as the current stream: its outputs and workspaces are allocated there."""
+    """The call f(*args) with `stream` as the current stream: its outputs and workspaces are allocated there, and
+    inputs freed before it has run are not given out again until then."""
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream))
+    for a in args:
+        for t in a if isinstance(a, (list, tuple)) else (a,):
+            if isinstance(t, torch.Tensor) and t.is_cuda:
+                t.record_stream(stream)
     with torch.cuda.stream(stream):
         return f(*args)
 

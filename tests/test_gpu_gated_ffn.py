@@ -115,6 +115,25 @@ def test_large_and_invalid_values(n):
     assert torch.isfinite(dx).all() and torch.isfinite(dwg).all() and torch.isfinite(dwu).all()
 
 
+@pytest.mark.parametrize("exponent", [-28, -12, 12, 28])
+def test_scales_far_from_one(exponent):
+    """bf16 keeps g and u in a form of its own: small and large products keep their accuracy, and beyond its range
+    the gradient is NaN, not some number."""
+    from paper_2607_03011_gb300 import inner
+    x, wg, wu, dh = operands(torch.bfloat16, 300, 64, 72, 17)
+    wu = (wu.float() * 2.0 ** exponent).bfloat16()
+    if exponent < 0:
+        wg = (wg.float() * 2.0 ** exponent).bfloat16()
+    h, saved = inner.gated_ffn(x, wg, wu, save=True)
+    dx, dwg, dwu = inner.gated_ffn_grad(dh, x, wg, wu, saved)
+    check({"h": h, "dx": dx, "dwg": dwg, "dwu": dwu}, x, wg, wu, dh, "silu")
+    wu.fill_(2.0 ** 40)
+    x[7] = 1.0
+    _, saved = inner.gated_ffn(x, wg, wu, save=True)
+    dx, _, _ = inner.gated_ffn_grad(dh, x, wg, wu, saved)
+    assert torch.isnan(dx[7]).all()
+
+
 @pytest.mark.parametrize("kind", ["silu", "gelu_tanh"])
 def test_gradient_by_differences(kind):
     """<dh, f(v + e w) - f(v - e w)> / 2e against <grad, w>, f in 64 bits, for each operand."""

@@ -33,7 +33,7 @@ def test_embed(iso, ptr):
     def call(w=p, ldw=8, dt=0, vocab=4, width=8, ids=p, ib=8, n=2, y=p, ldy=8):
         return L.isoloco_embed(w, ldw, dt, vocab, width, ids, ib, n, 1.0, y, ldy, None)
 
-    for kw in (dict(w=None), dict(ldw=7), dict(dt=3), dict(dt=-1), dict(vocab=0), dict(width=0), dict(vocab=1 << 31), dict(ids=None),
+    for kw in (dict(w=None), dict(ldw=7), dict(dt=3), dict(dt=-1), dict(vocab=0), dict(width=0), dict(vocab=1 << 31), dict(width=(1 << 20) + 1, ldw=1 << 21, ldy=1 << 21), dict(ids=None),
                dict(ids=odd(p, 4)), dict(ib=2), dict(n=-1), dict(n=1 << 31), dict(y=None), dict(ldy=7), dict(w=odd(p, 2)), dict(y=odd(p))):
         assert call(**kw) == bad, kw
         assert iso.last_error()
