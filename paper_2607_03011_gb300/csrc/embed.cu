@@ -11,10 +11,10 @@
 //   k_embed_join   adds those shares in the order of their spans and writes their rows.
 // Which terms are added in which order depends on the ids alone.
 //
-// Measured: the lookup of 65533 x 2048 fp32 rows 124 us (537 MB written, 165 MB of table rows read); its gradient
-// over 128000 rows 170 us for the zeros (6.2 TB/s; the sort's 41 us pass behind them), 98 us for the sums (537 MB
-// read) and 14 us to join.  8192 x 1024 bf16 over 32000 rows: 6.3 us, and 13.5 (the sort's own 12.7 us,
-// mostly its cluster barriers and trips to L2), 9 and 6 us.
+// Measured: the lookup of 65533 x 2048 fp32 rows 118 us (537 MB written, 165 MB of table rows read); its gradient
+// over 128000 rows 166 to 175 us for the zeros (6.2 TB/s; the sort's 31 us pass behind them), 98 us for the sums
+// (537 MB read) and 14 us to join.  8192 x 1024 bf16 over 32000 rows: 6.7 us, and 13.5 (the sort's own
+// 12.7 us, mostly its cluster barriers and trips to L2), 9.6 and 6.3 us.
 #include <algorithm>
 
 #include "common.cuh"
@@ -84,120 +84,158 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kDigits = 256;
 
-struct SortSmem {
-    uint32_t warp[kSortWarps][kDigits];  // counts, then the next place of each warp's digit
-    uint32_t total[kSortCluster][kDigits];  // every CTA's count of every digit
-    uint32_t scan[kDigits];
-};
-
-// Positions of a cluster's keys: CTA r, warp w owns [begin, end), in order.
-struct SortRange {
-    int64_t begin, end;
-};
-__device__ __forceinline__ SortRange sort_range(int64_t n, uint32_t rank, int warp) {
-    const int64_t per = (n + kSortCluster * kSortWarps - 1) / (kSortCluster * kSortWarps);
-    const int64_t b = min(n, per * (static_cast<int64_t>(rank) * kSortWarps + warp));
-    return {b, min(n, b + per)};
+// The warp's lanes with the same 8-bit digit (match.any in its place: 46.7 us for the gradient of 65533 narrow rows,
+// so 44.5).
+__device__ __forceinline__ uint32_t same_digit(uint32_t d) {
+    uint32_t same = 0xffffffffu;
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+        const uint32_t v = __ballot_sync(0xffffffffu, (d >> b) & 1u);
+        same &= (d >> b) & 1u ? v : ~v;
+    }
+    return same;
 }
 
+constexpr int kSortItems = 8;                     // keys of a lane in registers at once
+constexpr int kSortBatch = 32 * kSortItems;
+constexpr int kQuadWarps = kSortWarps / 4;
+
+struct SortSmem {
+    uint32_t warp[kSortWarps][kDigits + 1];  // counts, then the next place of each warp's digit (rows apart by a bank)
+    uint32_t total[kSortCluster][kDigits];   // every CTA's count of every digit
+    uint32_t before[kDigits];                // places before this CTA's first of each digit
+    uint32_t ends[kDigits / 32];
+};
+static_assert(kSortThreads == 4 * kDigits, "four threads per digit");
+
+// Sorts (id, position) into kp[1].  A pass over a digit: every warp counts the digits of its keys (a
+// contiguous run of them), the CTA and then the cluster add the counts up to the places where each warp's keys of
+// each digit begin, and every warp places its keys 32 at a time, in order.  Up to kSortBatch keys per warp (65536
+// in all) stay in registers over a pass.
 template <class I>
-__device__ __forceinline__ void sort_ids(SortSmem& sm, const I* ids, int64_t n, int64_t vocab, int bits, uint32_t* key[2], uint32_t* pos[2]) {
+__device__ __forceinline__ void sort_ids(SortSmem& sm, const I* ids, int64_t n, int64_t vocab, int bits, uint2* const (&kp)[2]) {
     const uint32_t rank = cluster_ctarank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const SortRange rg = sort_range(n, rank, warp);
+    const int64_t per = (n + kSortCluster * kSortWarps - 1) / (kSortCluster * kSortWarps);
+    const int64_t begin = min(n, per * (static_cast<int64_t>(rank) * kSortWarps + warp)), end = min(n, begin + per);
     const int passes = (bits + 7) / 8, dbits = (bits + passes - 1) / passes;
     const uint32_t dmask = (1u << dbits) - 1u;
+    const int d = threadIdx.x >> 2, q = threadIdx.x & 3;  // digit, and which quarter of the warps
+    const bool once = per <= kSortBatch;
     cluster_sync();  // every CTA runs before another writes its shared memory
     for (int pass = 0; pass < passes; ++pass) {
-        uint32_t* kdst = key[(passes - pass) & 1];  // key[1] in the last pass
-        uint32_t* pdst = pos[(passes - pass) & 1];
-        const uint32_t* ksrc = key[(passes - pass + 1) & 1];
-        const uint32_t* psrc = pos[(passes - pass + 1) & 1];
+        uint2* dst = kp[(passes - pass) & 1];  // kp[1] in the last pass
+        const uint2* src = kp[(passes - pass + 1) & 1];
         const int shift = pass * dbits;
-        // a key that is no token sorts behind all others
-        auto load = [&](int64_t i) -> uint32_t {
-            if (pass) return ksrc[i];
-            const int64_t v = token_at(ids, i, vocab);
-            return static_cast<uint32_t>(v < 0 ? vocab : v);
-        };
-        for (int d = lane; d < kDigits; d += 32) sm.warp[warp][d] = 0;
-        __syncwarp();
-        for (int64_t i = rg.begin + lane; i < rg.end; i += 32) atomicAdd(&sm.warp[warp][(load(i) >> shift) & dmask], 1u);
-        __syncthreads();
-        // this CTA's total of each digit, to every CTA of the cluster
-        if (threadIdx.x < kDigits) {
-            uint32_t s = 0;
-            for (int w = 0; w < kSortWarps; ++w) s += sm.warp[w][threadIdx.x];
-            for (uint32_t r = 0; r < kSortCluster; ++r) {
-                const uint32_t a = mapa_shared(smem_u32(&sm.total[rank][threadIdx.x]), r);
-                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(s) : "memory");
+        uint2 k[kSortItems];
+        auto load = [&](int64_t i0) {
+#pragma unroll
+            for (int j = 0; j < kSortItems; ++j) {
+                const int64_t i = i0 + j * 32 + lane;
+                if (i >= end) continue;
+                if (pass) {
+                    k[j] = src[i];
+                } else {
+                    const int64_t v = token_at(ids, i, vocab);
+                    k[j] = make_uint2(static_cast<uint32_t>(v < 0 ? vocab : v), static_cast<uint32_t>(i));  // no token: behind all others
+                }
             }
+        };
+        for (int i = lane; i < kDigits; i += 32) sm.warp[warp][i] = 0;
+        __syncwarp();
+        for (int64_t i0 = begin; i0 < end; i0 += kSortBatch) {
+            load(i0);
+#pragma unroll
+            for (int j = 0; j < kSortItems; ++j)
+                if (i0 + j * 32 + lane < end) atomicAdd(&sm.warp[warp][(k[j].x >> shift) & dmask], 1u);
         }
+        __syncthreads();
+        uint32_t c[kQuadWarps], mine = 0;
+#pragma unroll
+        for (int i = 0; i < kQuadWarps; ++i) {
+            c[i] = sm.warp[q * kQuadWarps + i][d];
+            mine += c[i];
+        }
+        uint32_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o, 4);
+            if (q >= o) upto += u;
+        }
+        // this CTA's total of the digit, to every CTA of the cluster
+        const uint32_t total = __shfl_sync(0xffffffffu, upto, 3, 4);
+#pragma unroll
+        for (uint32_t r = 0; r < kSortCluster / 4; ++r)
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapa_shared(smem_u32(&sm.total[rank][d]), q * (kSortCluster / 4) + r)),
+                         "r"(total)
+                         : "memory");
         cluster_sync();
-        // places before this CTA's first of each digit: smaller digits anywhere, and the same
-        // digit in earlier CTAs
-        uint32_t all = 0, before = 0;
+        // places before this CTA's first of each digit: smaller digits anywhere, and the same digit in earlier CTAs
+        uint32_t all = 0, before = 0, scan = 0;
         if (threadIdx.x < kDigits) {
+#pragma unroll
             for (uint32_t r = 0; r < kSortCluster; ++r) {
                 const uint32_t v = sm.total[r][threadIdx.x];
                 before += r < rank ? v : 0u;
                 all += v;
             }
-            // inclusive scan over the digits, warp by warp
-            uint32_t s = all;
+            scan = all;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t u = __shfl_up_sync(0xffffffffu, s, o);
-                if (lane >= o) s += u;
+                const uint32_t u = __shfl_up_sync(0xffffffffu, scan, o);
+                if (lane >= o) scan += u;
             }
-            sm.scan[threadIdx.x] = s;
+            if (lane == 31) sm.ends[warp] = scan;
         }
         __syncthreads();
         if (threadIdx.x < kDigits) {
-            uint32_t base = sm.scan[threadIdx.x] - all + before;
-            for (int w = 0; w < warp; ++w) base += sm.scan[w * 32 + 31];
-            for (int w = 0; w < kSortWarps; ++w) {
-                const uint32_t c = sm.warp[w][threadIdx.x];
-                sm.warp[w][threadIdx.x] = base;
-                base += c;
-            }
+            uint32_t base = scan - all + before;
+#pragma unroll
+            for (int w = 0; w < kDigits / 32; ++w) base += w < warp ? sm.ends[w] : 0u;
+            sm.before[threadIdx.x] = base;
         }
         __syncthreads();
-        // stable: a warp places its keys 32 at a time, in order
-        for (int64_t i0 = rg.begin; i0 < rg.end; i0 += 32) {
-            const int64_t i = i0 + lane;
-            const bool have = i < rg.end;
-            const uint32_t k = have ? load(i) : 0u;
-            const uint32_t d = have ? (k >> shift) & dmask : kDigits + lane;
-            const uint32_t same = __match_any_sync(0xffffffffu, d);
-            const uint32_t mine = __popc(same & ((1u << lane) - 1u));
-            if (have) {
-                const uint32_t at = sm.warp[warp][d] + mine;
-                kdst[at] = k;
-                pdst[at] = pass ? psrc[i] : static_cast<uint32_t>(i);
+        uint32_t place = sm.before[d] + upto - mine;
+#pragma unroll
+        for (int i = 0; i < kQuadWarps; ++i) {
+            sm.warp[q * kQuadWarps + i][d] = place;
+            place += c[i];
+        }
+        __syncthreads();
+        for (int64_t i0 = begin; i0 < end; i0 += kSortBatch) {
+            if (!once) load(i0);
+#pragma unroll
+            for (int j = 0; j < kSortItems; ++j) {
+                if (i0 + j * 32 >= end) break;  // (the whole warp)
+                const bool have = i0 + j * 32 + lane < end;
+                const uint32_t dg = (k[j].x >> shift) & dmask;
+                const uint32_t same = same_digit(dg) & __ballot_sync(0xffffffffu, have);
+                const uint32_t lower = __popc(same & ((1u << lane) - 1u));
+                uint32_t at = 0;
+                if (have) at = sm.warp[warp][dg] + lower;
+                __syncwarp();
+                if (have && lower == 0) sm.warp[warp][dg] = at + __popc(same);
+                __syncwarp();
+                if (have) dst[at] = k[j];
             }
-            __syncwarp();
-            if (have && mine == 0) sm.warp[warp][d] += __popc(same);
-            __syncwarp();
         }
         __threadfence();
         cluster_sync();  // the pass's output is complete, and the totals may be overwritten
     }
 }
 
-// Cluster 0 sorts the positions by id into key[1], pos[1]; the others fill dw with zeros.
+// Cluster 0 sorts (id, position) into kp1; the others fill dw with zeros.
 template <class I>
 __global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThreads)
-    k_embed_sort(const I* ids, int64_t n, int64_t vocab, int bits, uint32_t* k0, uint32_t* k1, uint32_t* p0, uint32_t* p1,
+    k_embed_sort(const I* ids, int64_t n, int64_t vocab, int bits, uint2* kp0, uint2* kp1,
                  uint32_t* nchains, uint8_t* dw, int64_t row_bytes, int64_t ld_bytes) {
     __shared__ SortSmem sm;
     next_may_start();
     const int64_t cta = static_cast<int64_t>(blockIdx.x) - kSortCluster;
     if (cta < 0) {
         if (blockIdx.x == 0 && threadIdx.x == 0) *nchains = 0;
-        uint32_t* key[2] = {k0, k1};
-        uint32_t* pos[2] = {p0, p1};
-        sort_ids(sm, ids, n, vocab, bits, key, pos);
+        uint2* const kp[2] = {kp0, kp1};
+        sort_ids(sm, ids, n, vocab, bits, kp);
         return;
     }
     const int64_t ctas = static_cast<int64_t>(gridDim.x) - kSortCluster;
@@ -223,8 +261,7 @@ constexpr int kBatch = 8;     // rows of dy in flight per thread
 // sum there, part[s][0] its sum in each of the later spans s.
 template <class T, class O, bool VEC>
 __global__ void __launch_bounds__(kRowThreads) k_embed_sum(const T* __restrict__ dy, int64_t ld_dy, int64_t vocab, int64_t width,
-                                                           const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
-                                                           int64_t n, int len, float scale, O* __restrict__ dw, int64_t ld_dw,
+                                                           const uint2* __restrict__ kp, int64_t n, int len, float scale, O* __restrict__ dw, int64_t ld_dw,
                                                            float* __restrict__ part, uint32_t* nchains,
                                                            uint32_t* __restrict__ chains) {
     constexpr int V = VEC ? Vec<T>::kN : 1;
@@ -232,9 +269,9 @@ __global__ void __launch_bounds__(kRowThreads) k_embed_sum(const T* __restrict__
     __shared__ uint32_t sp[2 * kMaxSpan];
     after_previous();
     const int64_t span = blockIdx.x, first = span * len;
-    auto key_at = [&](int64_t j) { return j >= 0 && j < n ? key[j] : 0xffffffffu; };
+    auto key_at = [&](int64_t j) { return j >= 0 && j < n ? kp[j].x : 0xffffffffu; };
     for (int i = threadIdx.x; i < 2 * len + 2; i += kRowThreads) sk[i] = key_at(first + i - 1);
-    for (int i = threadIdx.x; i < 2 * len; i += kRowThreads) sp[i] = first + i < n ? pos[first + i] : 0u;
+    for (int i = threadIdx.x; i < 2 * len; i += kRowThreads) sp[i] = first + i < n ? kp[first + i].y : 0u;
     const uint32_t before = key_at(first - len - 1);
     __syncthreads();
     const int64_t c = (static_cast<int64_t>(blockIdx.y) * kRowThreads + threadIdx.x) * V;
@@ -316,7 +353,7 @@ __global__ void __launch_bounds__(kRowThreads) k_embed_sum(const T* __restrict__
 constexpr int kJoinCols = 128, kJoinParts = 4, kJoinThreads = kJoinCols * kJoinParts;
 
 template <class O>
-__global__ void __launch_bounds__(kJoinThreads) k_embed_join(int64_t width, const uint32_t* __restrict__ key, int64_t n, int len,
+__global__ void __launch_bounds__(kJoinThreads) k_embed_join(int64_t width, const uint2* __restrict__ kp, int64_t n, int len,
                                                              float scale, O* __restrict__ dw, int64_t ld_dw,
                                                              const float* __restrict__ part, const uint32_t* nchains,
                                                              const uint32_t* __restrict__ chains) {
@@ -327,12 +364,12 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(int64_t width, cons
     const int run = threadIdx.x / kJoinCols, col = threadIdx.x % kJoinCols;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t span = chains[item / blocks], c = item % blocks * kJoinCols + col;
-        const uint32_t k = key[(span + 1) * len];
+        const uint32_t k = kp[(span + 1) * len].x;
         // later spans that begin with this row's key
         int64_t more = 0;
         for (;;) {
             const int64_t at = (span + 1 + more + threadIdx.x) * len;
-            const int got = __syncthreads_count(at < n && key[at] == k);
+            const int got = __syncthreads_count(at < n && kp[at].x == k);
             more += got;
             if (got < kJoinThreads) break;
         }
@@ -386,16 +423,18 @@ cudaError_t embed_t(const void* w, int64_t ld_w, int64_t vocab, int64_t width, c
 int span_of(int64_t tokens) { return tokens <= 16384 ? 16 : kMaxSpan; }
 
 struct EmbedWs {
-    uint32_t *k0, *k1, *p0, *p1, *nchains, *chains;
+    uint2 *kp0, *kp1;
+    uint32_t *nchains, *chains;
     float* part;
 };
 
 int64_t r16(int64_t b) { return (b + 15) / 16 * 16; }
 
 EmbedWs embed_ws(void* ws, int64_t tokens) {
-    uint32_t* p = static_cast<uint32_t*>(ws);
-    const int64_t s = r16(4 * tokens) / 4, spans = (tokens + span_of(tokens) - 1) / span_of(tokens);
-    return {p, p + s, p + 2 * s, p + 3 * s, p + 4 * s, p + 4 * s + 4, reinterpret_cast<float*>(p + 4 * s + 4 + r16(4 * spans) / 4)};
+    uint8_t* p = static_cast<uint8_t*>(ws);
+    const int64_t s = r16(8 * tokens), spans = (tokens + span_of(tokens) - 1) / span_of(tokens);
+    return {reinterpret_cast<uint2*>(p), reinterpret_cast<uint2*>(p + s), reinterpret_cast<uint32_t*>(p + 2 * s),
+            reinterpret_cast<uint32_t*>(p + 2 * s + 16), reinterpret_cast<float*>(p + 2 * s + 16 + r16(4 * spans))};
 }
 
 template <class T, class O>
@@ -410,12 +449,12 @@ cudaError_t embed_grad_t(const void* dy, int64_t ld_dy, int64_t vocab, int64_t w
     cudaError_t e;
     if (vec)
         e = launch_next(k_embed_sum<T, O, true>, grid, kRowThreads, st, static_cast<const T*>(dy), ld_dy, vocab, width,
-                        static_cast<const uint32_t*>(w.k1), static_cast<const uint32_t*>(w.p1), n, len, scale, static_cast<O*>(dw), ld_dw, w.part, w.nchains, w.chains);
+                        static_cast<const uint2*>(w.kp1), n, len, scale, static_cast<O*>(dw), ld_dw, w.part, w.nchains, w.chains);
     else
         e = launch_next(k_embed_sum<T, O, false>, grid, kRowThreads, st, static_cast<const T*>(dy), ld_dy, vocab, width,
-                        static_cast<const uint32_t*>(w.k1), static_cast<const uint32_t*>(w.p1), n, len, scale, static_cast<O*>(dw), ld_dw, w.part, w.nchains, w.chains);
+                        static_cast<const uint2*>(w.kp1), n, len, scale, static_cast<O*>(dw), ld_dw, w.part, w.nchains, w.chains);
     if (e != cudaSuccess) return e;
-    return launch_next(k_embed_join<O>, 4 * sms, kJoinThreads, st, width, static_cast<const uint32_t*>(w.k1), n, len,
+    return launch_next(k_embed_join<O>, 4 * sms, kJoinThreads, st, width, static_cast<const uint2*>(w.kp1), n, len,
                        scale, static_cast<O*>(dw), ld_dw, static_cast<const float*>(w.part), static_cast<const uint32_t*>(w.nchains),
                        static_cast<const uint32_t*>(w.chains));
 }
@@ -437,7 +476,7 @@ cudaError_t launch_embed(const void* weight, int64_t ld_w, int dtype, int64_t vo
 int64_t embed_grad_workspace(int64_t vocab, int64_t width, int64_t tokens) {
     (void)vocab;
     const int64_t spans = (tokens + span_of(tokens) - 1) / span_of(tokens);
-    return 4 * r16(4 * tokens) + 16 + r16(4 * spans) + spans * 2 * width * 4;
+    return 2 * r16(8 * tokens) + 16 + r16(4 * spans) + spans * 2 * width * 4;
 }
 
 cudaError_t launch_embed_grad(const void* dy, int64_t ld_dy, int dtype, int64_t vocab, int64_t width, const void* ids,
@@ -452,11 +491,11 @@ cudaError_t launch_embed_grad(const void* dy, int64_t ld_dy, int dtype, int64_t 
     const int es = dw_dtype == ISOLOCO_F32 ? 4 : 2;
     const unsigned grid = kSortCluster + std::max(1, (2 * sms) / kSortCluster) * kSortCluster;
     if (ids64)
-        k_embed_sort<int64_t><<<grid, kSortThreads, 0, st>>>(static_cast<const int64_t*>(ids), tokens, vocab, bits, w.k0, w.k1, w.p0,
-                                                             w.p1, w.nchains, static_cast<uint8_t*>(dw), width * es, ld_dw * es);
+        k_embed_sort<int64_t><<<grid, kSortThreads, 0, st>>>(static_cast<const int64_t*>(ids), tokens, vocab, bits, w.kp0, w.kp1,
+                                                             w.nchains, static_cast<uint8_t*>(dw), width * es, ld_dw * es);
     else
-        k_embed_sort<int32_t><<<grid, kSortThreads, 0, st>>>(static_cast<const int32_t*>(ids), tokens, vocab, bits, w.k0, w.k1, w.p0,
-                                                             w.p1, w.nchains, static_cast<uint8_t*>(dw), width * es, ld_dw * es);
+        k_embed_sort<int32_t><<<grid, kSortThreads, 0, st>>>(static_cast<const int32_t*>(ids), tokens, vocab, bits, w.kp0, w.kp1,
+                                                             w.nchains, static_cast<uint8_t*>(dw), width * es, ld_dw * es);
     if ((e = cudaGetLastError()) != cudaSuccess || tokens == 0) return e;
 #define GRAD(T, O) return embed_grad_t<T, O>(dy, ld_dy, vocab, width, w, tokens, scale, dw, ld_dw, sms, st)
     if (dtype == ISOLOCO_F32) GRAD(float, float);
