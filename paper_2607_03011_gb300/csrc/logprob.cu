@@ -13,12 +13,13 @@
 //
 // Measured: 8192 x 32000 bf16 with gradient 176 us (6.0 TB/s of logits read once and gradient written; about 8
 // instructions per 32 entries and pass at 2.4 per cycle and SM: loads' latency and issue share the bound); 2049 x
-// 50021 bf16 with 5 alternatives 51 us (4.1 TB/s: a row's reductions and alternatives, ~900 instructions per
-// warp, weigh against its 195 entries per thread); 4 x 32000 fp32 with 20 alternatives 12.4 us.
+// 50021 bf16 with 5 alternatives 48 us (4.3 TB/s: a row's reductions and alternatives weigh against its few
+// hundred entries per thread); 4 x 32000 fp32 with 20 alternatives 11.9 us.
 //
 // The `top` largest: the threads' own maxima, taken by groups, bound the top-th largest from below
-// (the top-th largest of kGroups group maxima); only threads whose maximum reaches the bound look
-// at their entries again, and the few entries found are ranked by counting.
+// (the top-th largest of kGroups group maxima); only threads whose maximum reaches the bound look again,
+// at the vector that holds it and, if another of theirs reaches the bound, at all of them, and the few
+// entries found are ranked by counting.
 #include <algorithm>
 #include <type_traits>
 
@@ -39,9 +40,11 @@ constexpr int kMaxSplit = 8;
 // 957 in shares of 128, 1029 in whole rows).
 constexpr int64_t kShareBytes = 98304;
 constexpr int kUnroll = 4;
-// Threads per SM the registers are cut for: 5 CTAs of 256 (8192 x 32000 bf16 with gradient 180 us; 4 CTAs, with
-// 64 registers, 194; 6, with 40, 188; 8 of 128 threads 229).
-constexpr int kThreadsPerSm = 1280;
+// Threads per SM the registers are cut for.  5 CTAs of 256 (8192 x 32000 bf16 with gradient 180 us; 4 CTAs, with 64
+// registers, 194; 6, with 40, 188; 8 of 128 threads 229); with alternatives 9 of 128 threads (8192 x 40000 bf16,
+// 20 alternatives: 142 us; 10 CTAs 151, 8 148, 5 of 256 threads 160).
+constexpr int threads_per_sm(bool top) { return top ? 1152 : 1280; }
+constexpr int ctas_per_sm(int threads, bool top) { return threads_per_sm(top) / threads > 32 ? 32 : threads_per_sm(top) / threads; }
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -221,7 +224,7 @@ __device__ __forceinline__ void merge_cta(Stat& st, float c, Stat* sm) {
 // The CTA's k largest entries, in order, to best[0 .. k) (keys; 0 where there are fewer).  bv, bi: this
 // thread's largest value and an index not below its first place.
 template <class T, int THREADS>
-__device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int k, float bv, uint32_t bi, uint64_t* best) {
+__device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int k, float bv, uint32_t bi, float second, uint64_t* best) {
     constexpr int kPer = THREADS / kGroups, V = Vec<T>::kN;
     // keys not above and not below that of the thread's largest entry, which lies within a vector of bi
     const bool any = bi != 0xffffffffu;
@@ -260,21 +263,26 @@ __device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int 
             if (at < kCandidates) sm.cand[at] = key;
         }
     };
+    auto look_at = [&](uint32_t i) {
+        Vec<T> v;
+        v.raw = *sh.vec(i);
+        float f[V];
+        v.unpack(f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) look(f[j], sh.head + i * V + j);
+    };
     static_assert(THREADS <= 256, "TopSmem::thread");
-    if (any && most >= bound) sm.thread[atomicAdd(&sm.threads, 1)] = static_cast<uint16_t>(threadIdx.x);
+    if (any && most >= bound) {
+        // the vector with the thread's largest entry, or, where another of its vectors may reach the bound, all of them
+        if (rank_key(second, 0) >= bound) sm.thread[atomicAdd(&sm.threads, 1)] = static_cast<uint16_t>(threadIdx.x);
+        else if (bi >= sh.head && bi < sh.tail()) look_at((bi - sh.head) / V);
+    }
     __syncthreads();
-    // their vectors, dealt to all threads
+    // those threads' vectors, dealt to all
     const uint32_t found = sm.threads, each = (sh.nvec + THREADS - 1) / THREADS;
     for (uint32_t e = threadIdx.x; e < found * each; e += THREADS) {
         const uint32_t i = sm.thread[e / each] + (e % each) * THREADS;
-        if (i < sh.nvec) {
-            Vec<T> v;
-            v.raw = *sh.vec(i);
-            float f[V];
-            v.unpack(f);
-#pragma unroll
-            for (int j = 0; j < V; ++j) look(f[j], sh.head + i * V + j);
-        }
+        if (i < sh.nvec) look_at(i);
     }
     if (threadIdx.x < sh.head) look(to_f32(sh.x[threadIdx.x]), threadIdx.x);
     if (threadIdx.x < sh.n - sh.tail()) look(to_f32(sh.x[sh.tail() + threadIdx.x]), sh.tail() + threadIdx.x);
@@ -316,7 +324,7 @@ __device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int 
 }
 
 template <class T, class I, int THREADS, bool TOP, bool GRAD>
-__global__ void __launch_bounds__(THREADS, kThreadsPerSm / THREADS > 32 ? 32 : kThreadsPerSm / THREADS) k_logprobs(LogprobArgs a, uint32_t split) {
+__global__ void __launch_bounds__(THREADS, ctas_per_sm(THREADS, TOP)) k_logprobs(LogprobArgs a, uint32_t split) {
     constexpr int V = Vec<T>::kN;
     __shared__ Stat sm[THREADS / 32];
     __shared__ Stat peer[kMaxSplit];  // the sums of every CTA of the cluster
@@ -333,7 +341,7 @@ __global__ void __launch_bounds__(THREADS, kThreadsPerSm / THREADS > 32 ? 32 : k
         const float xt = t >= 0 ? to_f32(row[t]) : 0.f;  // (early: its latency passes behind the row's)
         Stat st;
         st.clear();
-        float bv = -INFINITY;
+        float bv = -INFINITY, second = -INFINITY;  // the largest entry, and of the other vectors (and single entries)
         uint32_t bi = 0xffffffffu;
         if (threadIdx.x < sh.head) {
             const float v = to_f32(sh.x[threadIdx.x]);
@@ -384,6 +392,7 @@ __global__ void __launch_bounds__(THREADS, kThreadsPerSm / THREADS > 32 ? 32 : k
                     v[q].unpack(f);
 #pragma unroll
                     for (int j = 0; j < V; j += 2) two.add(f[j], f[j + 1], minus_m, c2);
+                    if (TOP) second = fmaxf(second, fminf(vm[q], bv));
                     if (TOP && (vm[q] > bv || bi == 0xffffffffu)) {
                         bv = fmaxf(vm[q], bv);
                         bi = sh.head + (i + q * THREADS) * V + V - 1;
@@ -403,6 +412,7 @@ __global__ void __launch_bounds__(THREADS, kThreadsPerSm / THREADS > 32 ? 32 : k
             const float v = to_f32(sh.x[sh.tail() + threadIdx.x]);
             if (v > st.m) st.raise(v, c);
             st.add(v, c);
+            if (TOP) second = fmaxf(second, fminf(v, bv));
             if (TOP && (v > bv || bi == 0xffffffffu)) bv = fmaxf(v, bv), bi = sh.tail() + threadIdx.x;
         }
         merge_cta<THREADS>(st, c, sm);
@@ -418,7 +428,7 @@ __global__ void __launch_bounds__(THREADS, kThreadsPerSm / THREADS > 32 ? 32 : k
         }
         if constexpr (TOP) {
             // every CTA's largest go to the first CTA's shared memory
-            top_of_cta<T, THREADS>(top_sm, sh, a.top, bv, bi, top_sm.best[rank]);
+            top_of_cta<T, THREADS>(top_sm, sh, a.top, bv, bi, second, top_sm.best[rank]);
             if (split > 1 && rank > 0 && threadIdx.x < a.top) {
                 const uint32_t at = mapa_shared(smem_u32(&top_sm.best[rank][threadIdx.x]), 0);
                 asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(at), "l"(top_sm.best[rank][threadIdx.x]) : "memory");
@@ -594,8 +604,9 @@ cudaError_t run(const LogprobArgs& a, cudaStream_t st) {
     // A short row is a few vectors per thread and its reductions weigh more: smaller CTAs, more rows at once (8192
     // bf16 rows without / with gradient: of 8000 32 / 62 us with 64 threads, 36 / 64 with 128; of 16000 52 / 103
     // with 128, 64 / 116 with 256; of 32000 with gradient 229 with 128, 180 with 256).
+    // With alternatives, whose search weighs as much, 128 threads wherever rows fill the GPU.
     if (a.vocab <= 8192) return ROWS(64);
-    return a.vocab <= 16384 ? ROWS(128) : ROWS(256);
+    return a.vocab <= 16384 || (a.top && a.rows > sms) ? ROWS(128) : ROWS(256);
 #undef ROWS
 }
 
