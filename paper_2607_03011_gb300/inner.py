@@ -103,13 +103,14 @@ def embed(weight: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, stream=No
     dev = w.device
     y = _empty((*ids.shape, width), dtype=w.dtype, device=dev)
     rc = lib().isoloco_embed(w.data_ptr(), ld, _DTYPE[w.dtype], vocab, width, ids.data_ptr(), size, ids.numel(), scale,
-                               y.data_ptr(), width, _raw_stream(dev.index))
+                             y.data_ptr(), width, _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_embed")
     return y
 
 
-def embed_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0, dtype=None, stream=None) -> torch.Tensor:
+def embed_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0, dtype=None,
+               stream=None) -> torch.Tensor:
     """The lookup's gradient by the whole table (vocab x width, of `dtype`: grad's or fp32), from
     grad = d loss / d embed(weight, ids, scale)."""
     if stream is not None:
@@ -126,7 +127,7 @@ def embed_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float =
     dw = _empty((vocab, width), dtype=dtype, device=dev)
     ws = _empty(need, dtype=torch.uint8, device=dev)
     rc = L.isoloco_embed_grad(dy.data_ptr(), ld, _DTYPE[dy.dtype], vocab, width, ids.data_ptr(), size, n, scale,
-                                dw.data_ptr(), width, _DTYPE[dtype], ws.data_ptr(), need, _raw_stream(dev.index))
+                              dw.data_ptr(), width, _DTYPE[dtype], ws.data_ptr(), need, _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_embed_grad")
     return dw
@@ -151,7 +152,8 @@ def _ffn_operands(x, w_gate, w_up, act):
     return n, width, ff, (px, ldx, pg, pu, ldw, _HALF[x2.dtype], n, width, ff, _ACT[act]), aligned
 
 
-def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: str = "silu", save: bool = False, stream=None):
+def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: str = "silu", save: bool = False,
+              stream=None):
     """h = act(x w_gate) * (x w_up); w_gate and w_up are width x ff.  With save=True returns
     (h, saved), where `saved` is what gated_ffn_grad needs besides the operands."""
     if stream is not None:
@@ -186,8 +188,8 @@ def gated_ffn_grad(grad: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_
     dwu = _empty((width, ff), dtype=dt, device=dev) if need_w else None
     need = L.isoloco_gated_ffn_grad_workspace(n, width, ff, aligned)
     ws = _empty(need, dtype=torch.uint8, device=dev)
-    rc = L.isoloco_gated_ffn_grad(dh.data_ptr(), ldh, *args, saved.data_ptr(), _ptr(dx), width, _ptr(dwg), _ptr(dwu), ff,
-                                    ws.data_ptr(), need, _raw_stream(dev.index))
+    rc = L.isoloco_gated_ffn_grad(dh.data_ptr(), ldh, *args, saved.data_ptr(), _ptr(dx), width, _ptr(dwg), _ptr(dwu),
+                                  ff, ws.data_ptr(), need, _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_gated_ffn_grad")
     return dx, dwg, dwu
@@ -219,7 +221,8 @@ def _like_rows(z, shape, vocab, ld, dev):
 
 
 def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, top: int = 0,
-                   grad_logp: Optional[torch.Tensor] = None, grad_entropy: Optional[torch.Tensor] = None, stream=None) -> TokenLogprobs:
+                   grad_logp: Optional[torch.Tensor] = None, grad_entropy: Optional[torch.Tensor] = None,
+                   stream=None) -> TokenLogprobs:
     """Log probability of each row's target under softmax(scale * logits), the rows' entropies and
     logarithms of the sum of exponentials, and the `top` likeliest tokens (ties: the lowest index).
     With grad_logp or grad_entropy (a gradient per row, known in advance as for a weighted sum of log
@@ -240,8 +243,8 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1
     ti = _empty((*lead, top), dtype=torch.int64, device=dev) if top else None
     gz = _like_rows(z, shape, vocab, ld, dev) if gl is not None or ge is not None else None
     rc = lib().isoloco_token_logprobs(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, targets.data_ptr(), size, scale,
-                                        logp.data_ptr(), ent.data_ptr(), lse.data_ptr(), top, _ptr(tl), _ptr(ti), gl, ge,
-                                        _ptr(gz), ld, _raw_stream(dev.index))
+                                      logp.data_ptr(), ent.data_ptr(), lse.data_ptr(), top, _ptr(tl), _ptr(ti), gl, ge,
+                                      _ptr(gz), ld, _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_token_logprobs")
     return TokenLogprobs(logp, ent, lse, tl, ti, gz)
@@ -259,9 +262,10 @@ def token_logprobs_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.
     dev = z.device
     gz = _like_rows(z, logits.shape, vocab, ld, dev)
     rc = lib().isoloco_token_logprobs_grad(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, targets.data_ptr(), size, scale,
-                                             _per_row(lse, n, "lse"), _per_row(entropy, n, "entropy"),
-                                             _per_row(grad_logp, n, "grad_logp"), _per_row(grad_entropy, n, "grad_entropy"),
-                                             gz.data_ptr(), ld, _raw_stream(dev.index))
+                                           _per_row(lse, n, "lse"), _per_row(entropy, n, "entropy"),
+                                           _per_row(grad_logp, n, "grad_logp"),
+                                           _per_row(grad_entropy, n, "grad_entropy"), gz.data_ptr(), ld,
+                                           _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_token_logprobs_grad")
     return gz
@@ -296,7 +300,8 @@ def grad_norm(grads: Sequence[torch.Tensor], stream=None) -> torch.Tensor:
     return norm
 
 
-def clip_grads(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None, stream=None) -> torch.Tensor:
+def clip_grads(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
+               stream=None) -> torch.Tensor:
     """Scales the gradient by min(1, max_norm / norm), in place or into `out`, and returns the norm
     (0-d, fp32).  A NaN or infinite norm scales nothing."""
     if stream is not None:
@@ -313,7 +318,7 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Seq
     norm = _empty((), dtype=torch.float32, device=dev)
     ws = _empty(need, dtype=torch.uint8, device=dev) if need else None
     rc = L.isoloco_clip_grads(arr, outs and outs.buffer_info()[0], n, max_norm, norm.data_ptr(), _ptr(ws), need,
-                                _raw_stream(dev))
+                              _raw_stream(dev))
     if rc:
         _check(rc, "isoloco_clip_grads")
     return norm
