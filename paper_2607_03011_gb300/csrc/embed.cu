@@ -454,6 +454,7 @@ cudaError_t embed_grad_t(const void* dy, int64_t ld_dy, int64_t vocab, int64_t w
         e = launch_next(k_embed_sum<T, O, false>, grid, kRowThreads, st, static_cast<const T*>(dy), ld_dy, vocab, width,
                         static_cast<const uint2*>(w.kp1), n, len, scale, static_cast<O*>(dw), ld_dw, w.part, w.nchains, w.chains);
     if (e != cudaSuccess) return e;
+    if (spans < 3) return cudaSuccess;  // no row lies in three
     return launch_next(k_embed_join<O>, 4 * sms, kJoinThreads, st, width, static_cast<const uint2*>(w.kp1), n, len,
                        scale, static_cast<O*>(dw), ld_dw, static_cast<const float*>(w.part), static_cast<const uint32_t*>(w.nchains),
                        static_cast<const uint32_t*>(w.chains));
