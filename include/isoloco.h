@@ -393,8 +393,8 @@ int isoloco_embed_grad(const void* dy, int64_t ld_dy, isoloco_dtype_t dtype, int
  *   x: tokens x width; w_gate, w_up: width x ff (pitch ld_w, the layout of the parameter table's
  *   matrices); h: tokens x ff.  dtype BF16 or F16 for all.
  *   saved: NULL, or isoloco_gated_ffn_saved_bytes() bytes, 16-byte aligned, that receive x w_gate and
- *   x w_up for isoloco_gated_ffn_grad: in fp32 for F16, in 16 bits (10 of them significant, magnitudes
- *   below 2^33: what lies beyond makes the gradient NaN) for BF16.
+ *   x w_up for isoloco_gated_ffn_grad: in fp32 for F16, in 16 bits for BF16: 10 significant bits for magnitudes
+ *   from 2^-22 to 2^10, 8 (bf16's own) below and above; what lies beyond 2^33 makes the gradient NaN.
  *   Workspace: aligned = 1 when the addresses and pitches of all matrices (without dh) are multiples of
  *   16 bytes; 0 any others, which are copied to and from rows that are.
  *   tokens up to 2^30, width and ff up to 2^20. */

@@ -182,8 +182,8 @@ __global__ void __launch_bounds__(kFewThreads) k_ffn_few(const T* __restrict__ x
                 h[t * ld_h + col] = from_f32<T>(act_value<GELU>(g) * u);
                 if (saved) {
                     if constexpr (__is_same(T, __half)) {
-                        saved[t * 2 * pitch + col] = Kept<T>::clamp(g);
-                        saved[t * 2 * pitch + pitch + col] = Kept<T>::clamp(u);
+                        saved[t * 2 * pitch + col] = g;
+                        saved[t * 2 * pitch + pitch + col] = u;
                     } else {
                         saved[t * 2 * pitch + col] = static_cast<uint16_t>(Kept<T>::encode2(g, 0.f));
                         saved[t * 2 * pitch + pitch + col] = static_cast<uint16_t>(Kept<T>::encode2(u, 0.f));
