@@ -45,7 +45,9 @@ bool matrix_ok(const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes)
     if (rows == 0) return true;
     return p && reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld >= cols && ld <= (int64_t(1) << 40);
 }
-bool array_ok(const void* p, int64_t n, int bytes) { return n == 0 || (p && reinterpret_cast<uintptr_t>(p) % bytes == 0); }
+// (NULL is)
+bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+bool array_ok(const void* p, int64_t n, int bytes) { return n == 0 || (p && aligned_to(p, bytes)); }
 
 int workspace_ok(const void* ws, int64_t have, int64_t need) {
     if (need == 0) return ISOLOCO_OK;
@@ -88,6 +90,8 @@ const char* logprob_problem(const LogprobArgs& a, int target_bytes) {
     if (!array_ok(a.targets, a.rows, target_bytes)) return "targets is NULL or misaligned";
     if (!(a.scale > 0.f) || a.scale > 1e30f) return "scale must be positive and finite";
     if (a.grad_logits && !matrix_ok(a.grad_logits, a.rows, a.vocab, a.ld_grad, es)) return "grad_logits is misaligned or its pitch too small";
+    if (!aligned_to(a.logp, 4) || !aligned_to(a.entropy, 4) || !aligned_to(a.lse, 4)) return "logp, entropy or lse is misaligned";
+    if (!aligned_to(a.grad_logp, 4) || !aligned_to(a.grad_entropy, 4)) return "grad_logp or grad_entropy is misaligned";
     return nullptr;
 }
 
