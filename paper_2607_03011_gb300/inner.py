@@ -201,7 +201,7 @@ class TokenLogprobs(NamedTuple):
     lse: torch.Tensor                      # fp32, one per row
     top_logp: Optional[torch.Tensor]       # fp32, rows x top
     top_index: Optional[torch.Tensor]      # int64, rows x top
-    grad_logits: Optional[torch.Tensor]    # of the logits' type and shape (and pitch)
+    grad_logits: Optional[torch.Tensor]    # of the logits' type and shape; rows a little apart where the logits' are
 
 
 def _per_row(t: Optional[torch.Tensor], n: int, what: str):
@@ -213,11 +213,12 @@ def _per_row(t: Optional[torch.Tensor], n: int, what: str):
 
 
 def _like_rows(z, shape, vocab, ld, dev):
-    """An empty tensor of the logits' shape and pitch (rows then start as far from a 16-byte boundary as
-    the logits' do, and both are read and written 16 bytes at a time)."""
-    if ld == vocab:
-        return _empty(shape, dtype=z.dtype, device=dev)
-    return _empty((*shape[:-1], ld), dtype=z.dtype, device=dev)[..., :vocab]
+    """(an empty tensor of the logits' shape, its pitch): the smallest pitch with which rows start as far from a
+    16-byte boundary as the logits' do (both are then read and written 16 bytes at a time)."""
+    pitch = vocab + (ld - vocab) % (16 // z.element_size())
+    if pitch == vocab:
+        return _empty(shape, dtype=z.dtype, device=dev), vocab
+    return _empty((*shape[:-1], pitch), dtype=z.dtype, device=dev)[..., :vocab], pitch
 
 
 def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, top: int = 0,
@@ -241,10 +242,10 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1
     lse = _empty(lead, dtype=torch.float32, device=dev)
     tl = _empty((*lead, top), dtype=torch.float32, device=dev) if top else None
     ti = _empty((*lead, top), dtype=torch.int64, device=dev) if top else None
-    gz = _like_rows(z, shape, vocab, ld, dev) if gl is not None or ge is not None else None
+    gz, ldg = _like_rows(z, shape, vocab, ld, dev) if gl is not None or ge is not None else (None, ld)
     rc = lib().isoloco_token_logprobs(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, targets.data_ptr(), size, scale,
                                       logp.data_ptr(), ent.data_ptr(), lse.data_ptr(), top, _ptr(tl), _ptr(ti), gl, ge,
-                                      _ptr(gz), ld, _raw_stream(dev.index))
+                                      _ptr(gz), ldg, _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_token_logprobs")
     return TokenLogprobs(logp, ent, lse, tl, ti, gz)
@@ -260,11 +261,11 @@ def token_logprobs_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.
     z, n, vocab, ld = _rows(logits, "logits")
     size = _tokens(targets, "targets", n)
     dev = z.device
-    gz = _like_rows(z, logits.shape, vocab, ld, dev)
+    gz, ldg = _like_rows(z, logits.shape, vocab, ld, dev)
     rc = lib().isoloco_token_logprobs_grad(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, targets.data_ptr(), size, scale,
                                            _per_row(lse, n, "lse"), _per_row(entropy, n, "entropy"),
                                            _per_row(grad_logp, n, "grad_logp"),
-                                           _per_row(grad_entropy, n, "grad_entropy"), gz.data_ptr(), ld,
+                                           _per_row(grad_entropy, n, "grad_entropy"), gz.data_ptr(), ldg,
                                            _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_token_logprobs_grad")
