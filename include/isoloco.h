@@ -462,9 +462,12 @@ int isoloco_clip_grads(const isoloco_tensor_t* tensors, const isoloco_tensor_t* 
                        float* norm, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Synchronizes `stream` and returns the device status of the inner step's operators on the current
- * device since the last such call: OK, or TIMEOUT when a kernel's wait gave up (its outputs are
- * then undefined). */
+ * device since the last such call: OK, or TIMEOUT when a kernel's wait gave up, on any of the device's
+ * streams (its outputs are then undefined).  Every such error is reported to one caller at least. */
 int isoloco_inner_status(void* stream);
+
+/* Testing hook: enqueues a kernel on `stream` that raises the same status as a wait that gave up. */
+int isoloco_debug_raise_inner(void* stream);
 
 /* Thread-local message describing the last error returned on this thread. */
 const char* isoloco_last_error(void);

@@ -18,6 +18,9 @@ cudaError_t device_sms(int* sms) {
 
 static __device__ uint32_t g_error_word;
 
+static __global__ void k_raise(uint32_t* word, uint32_t bits) { atomicOr(word, bits); }
+static __global__ void k_clear(uint32_t* word, uint32_t bits) { atomicAnd(word, ~bits); }
+
 cudaError_t error_word(uint32_t** word) {
     return cudaGetSymbolAddress(reinterpret_cast<void**>(word), g_error_word);
 }
@@ -272,10 +275,25 @@ int isoloco_inner_status(void* stream) try {
     cudaStream_t st = stream_of(stream);
     cudaError_t e = error_word(&word);
     if (e == cudaSuccess) e = cudaMemcpyAsync(&bits, word, sizeof(bits), cudaMemcpyDeviceToHost, st);
-    if (e == cudaSuccess) e = cudaMemsetAsync(word, 0, sizeof(bits), st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e == cudaSuccess && bits) {
+        // only what this call reports: a kernel on another stream may have raised an error since
+        k_clear<<<1, 1, 0, st>>>(word, bits);
+        e = cudaGetLastError();
+        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    }
     if (e != cudaSuccess) return cuda_status(e);
     return (bits & kErrTimeout) ? set_error(ISOLOCO_ERR_TIMEOUT, "a wait in an inner-step kernel gave up") : ISOLOCO_OK;
+} catch (...) {
+    return kNoMemory;
+}
+
+int isoloco_debug_raise_inner(void* stream) try {
+    uint32_t* word = nullptr;
+    cudaError_t e = error_word(&word);
+    if (e != cudaSuccess) return cuda_status(e);
+    k_raise<<<1, 1, 0, stream_of(stream)>>>(word, kErrTimeout);
+    return cuda_status(cudaGetLastError());
 } catch (...) {
     return kNoMemory;
 }

@@ -110,6 +110,7 @@ def lib():
             L.isoloco_grad_norm.argtypes = [_vp, ci, _vp, _vp, i64, _vp]
             L.isoloco_clip_grads.argtypes = [_vp, _vp, ci, cf, _vp, _vp, i64, _vp]
             L.isoloco_inner_status.argtypes = [_vp]
+            L.isoloco_debug_raise_inner.argtypes = [_vp]
             L.isoloco_embed_grad_workspace.argtypes, L.isoloco_embed_grad_workspace.restype = [i64, i64, i64], i64
             for f in (L.isoloco_gated_ffn_workspace, L.isoloco_gated_ffn_grad_workspace):
                 f.argtypes, f.restype = [i64, i64, i64, ci], i64
