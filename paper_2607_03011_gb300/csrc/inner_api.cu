@@ -64,20 +64,28 @@ bool rows16(const void* p, int64_t ld, int64_t rows) { return rows == 0 || ((rei
 
 cudaStream_t stream_of(void* s) { return static_cast<cudaStream_t>(s); }
 
+const char* embed_sizes_problem(int64_t vocab, int64_t width, int64_t tokens) {
+    return size_ok(vocab, 1) && size_ok(width, 1) && width <= (1 << 20) && size_ok(tokens, 0)
+               ? nullptr : "vocab must be in 1 .. 2^31 - 1, width in 1 .. 2^20, tokens in 0 .. 2^31 - 1";
+}
+
 const char* embed_problem(int dtype, int64_t vocab, int64_t width, const void* ids, int id_bytes, int64_t tokens) {
     if (!any_dtype(dtype)) return "bad element type";
-    if (!size_ok(vocab, 1) || !size_ok(width, 1) || width > (1 << 20) || !size_ok(tokens, 0))
-        return "vocab must be in 1 .. 2^31 - 1, width in 1 .. 2^20, tokens in 0 .. 2^31 - 1";
+    if (const char* p = embed_sizes_problem(vocab, width, tokens)) return p;
     if (id_bytes != 4 && id_bytes != 8) return "id_bytes must be 4 or 8";
     if (!array_ok(ids, tokens, id_bytes)) return "ids is NULL or misaligned";
     return nullptr;
 }
 
+const char* ffn_sizes_problem(int64_t tokens, int64_t width, int64_t ff) {
+    return tokens >= 0 && tokens <= (1 << 30) && width >= 1 && ff >= 1 && width <= (1 << 20) && ff <= (1 << 20)
+               ? nullptr : "tokens must be in 0 .. 2^30, width and ff in 1 .. 2^20";
+}
+
 const char* ffn_problem(const FfnArgs& a) {
     if (!half_dtype(a.dtype)) return "the gated block takes BF16 or F16";
     if (a.act != ISOLOCO_SILU && a.act != ISOLOCO_GELU_TANH) return "bad activation";
-    if (a.tokens < 0 || a.tokens > (1 << 30) || a.width < 1 || a.ff < 1 || a.width > (1 << 20) || a.ff > (1 << 20))
-        return "tokens must be in 0 .. 2^30, width and ff in 1 .. 2^20";
+    if (const char* p = ffn_sizes_problem(a.tokens, a.width, a.ff)) return p;
     if (!matrix_ok(a.x, a.tokens, a.width, a.ld_x, 2)) return "x is NULL, misaligned or its pitch too small";
     if (!matrix_ok(a.wg, a.width, a.ff, a.ld_w, 2) || !matrix_ok(a.wu, a.width, a.ff, a.ld_w, 2))
         return "w_gate or w_up is NULL, misaligned or its pitch too small";
@@ -127,7 +135,7 @@ int isoloco_embed(const void* weight, int64_t ld_weight, isoloco_dtype_t dtype, 
 }
 
 int64_t isoloco_embed_grad_workspace(int64_t vocab, int64_t width, int64_t tokens) try {
-    if (!size_ok(vocab, 1) || !size_ok(width, 1) || !size_ok(tokens, 0)) return ISOLOCO_ERR_INVALID;
+    if (const char* p = embed_sizes_problem(vocab, width, tokens)) return invalid(p);
     return embed_grad_workspace(vocab, width, tokens);
 } catch (...) {
     return kNoMemory;
@@ -149,21 +157,22 @@ int isoloco_embed_grad(const void* dy, int64_t ld_dy, isoloco_dtype_t dtype, int
 }
 
 int64_t isoloco_gated_ffn_saved_bytes(int64_t tokens, int64_t ff, isoloco_dtype_t dtype) try {
-    if (!size_ok(tokens, 0) || !size_ok(ff, 1) || !half_dtype(dtype)) return ISOLOCO_ERR_INVALID;
+    if (!half_dtype(dtype)) return invalid("the gated block takes BF16 or F16");
+    if (const char* p = ffn_sizes_problem(tokens, 1, ff)) return invalid(p);
     return ffn_saved_bytes(tokens, ff, dtype);
 } catch (...) {
     return kNoMemory;
 }
 
 int64_t isoloco_gated_ffn_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned) try {
-    if (!size_ok(tokens, 0) || !size_ok(width, 1) || !size_ok(ff, 1)) return ISOLOCO_ERR_INVALID;
+    if (const char* p = ffn_sizes_problem(tokens, width, ff)) return invalid(p);
     return ffn_workspace(tokens, width, ff, false, aligned != 0);
 } catch (...) {
     return kNoMemory;
 }
 
 int64_t isoloco_gated_ffn_grad_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned) try {
-    if (!size_ok(tokens, 0) || !size_ok(width, 1) || !size_ok(ff, 1)) return ISOLOCO_ERR_INVALID;
+    if (const char* p = ffn_sizes_problem(tokens, width, ff)) return invalid(p);
     return ffn_workspace(tokens, width, ff, true, aligned != 0);
 } catch (...) {
     return kNoMemory;
@@ -237,7 +246,8 @@ int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_d
 }
 
 int64_t isoloco_grad_norm_workspace(const isoloco_tensor_t* tensors, int count) try {
-    return tensors_problem(tensors, count) ? ISOLOCO_ERR_INVALID : grad_norm_workspace(tensors, count);
+    if (const char* p = tensors_problem(tensors, count)) return invalid(p);
+    return grad_norm_workspace(tensors, count);
 } catch (...) {
     return kNoMemory;
 }

@@ -93,6 +93,13 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+def _buffer(need: int, what: str, dev):
+    """Uninitialised bytes, as many as `what` asked for (none: None); what it refuses raises."""
+    if need < 0:
+        _check(need, what)
+    return _empty(need, dtype=torch.uint8, device=dev) if need else None
+
+
 def embed(weight: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, stream=None) -> torch.Tensor:
     """scale * weight[ids] (vocab x width by ids of any shape); zeros where an id is outside
     [0, vocab)."""
@@ -122,10 +129,8 @@ def embed_grad(grad: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float =
         raise ValueError("dtype: grad's type or fp32")
     L, dev = lib(), dy.device
     need = L.isoloco_embed_grad_workspace(vocab, width, n)
-    if need < 0:
-        raise ValueError("vocab must be in 1 .. 2^31 - 1")
+    ws = _buffer(need, "isoloco_embed_grad_workspace", dev)
     dw = _empty((vocab, width), dtype=dtype, device=dev)
-    ws = _empty(need, dtype=torch.uint8, device=dev)
     rc = L.isoloco_embed_grad(dy.data_ptr(), ld, _DTYPE[dy.dtype], vocab, width, ids.data_ptr(), size, n, scale,
                               dw.data_ptr(), width, _DTYPE[dtype], ws.data_ptr(), need, _raw_stream(dev.index))
     if rc:
@@ -160,10 +165,10 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: st
         return _on(stream, gated_ffn, x, w_gate, w_up, act, save)
     n, width, ff, args, aligned = _ffn_operands(x, w_gate, w_up, act)
     L, dev, dt = lib(), x.device, x.dtype
-    h = _empty((*x.shape[:-1], ff), dtype=dt, device=dev)
-    saved = _empty(L.isoloco_gated_ffn_saved_bytes(n, ff, _HALF[dt]), dtype=torch.uint8, device=dev) if save else None
+    saved = _buffer(L.isoloco_gated_ffn_saved_bytes(n, ff, _HALF[dt]), "isoloco_gated_ffn_saved_bytes", dev) if save else None
     need = 0 if aligned else L.isoloco_gated_ffn_workspace(n, width, ff, 0)
-    ws = _empty(need, dtype=torch.uint8, device=dev) if need else None
+    ws = _buffer(need, "isoloco_gated_ffn_workspace", dev)
+    h = _empty((*x.shape[:-1], ff), dtype=dt, device=dev)
     rc = L.isoloco_gated_ffn(*args, h.data_ptr(), ff, _ptr(saved), _ptr(ws), need, _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_gated_ffn")
@@ -180,16 +185,17 @@ def gated_ffn_grad(grad: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_
     L, dev, dt = lib(), x.device, x.dtype
     if dh.dtype != dt or rows != n or cols != ff:
         raise ValueError(f"grad: {n} rows of {ff} of x's type expected")
+    need = L.isoloco_gated_ffn_grad_workspace(n, width, ff, aligned)
+    _check(need, "isoloco_gated_ffn_grad_workspace")
     if saved.dtype != torch.uint8 or not saved.is_contiguous() or saved.device != dev or \
             saved.numel() != L.isoloco_gated_ffn_saved_bytes(n, ff, _HALF[dt]):
         raise ValueError("saved: not what gated_ffn(save=True) returned for these sizes")
     dx = _empty(x.shape, dtype=dt, device=dev) if need_x else None
     dwg = _empty((width, ff), dtype=dt, device=dev) if need_w else None
     dwu = _empty((width, ff), dtype=dt, device=dev) if need_w else None
-    need = L.isoloco_gated_ffn_grad_workspace(n, width, ff, aligned)
-    ws = _empty(need, dtype=torch.uint8, device=dev)
+    ws = _buffer(need, "isoloco_gated_ffn_grad_workspace", dev)
     rc = L.isoloco_gated_ffn_grad(dh.data_ptr(), ldh, *args, saved.data_ptr(), _ptr(dx), width, _ptr(dwg), _ptr(dwu),
-                                  ff, ws.data_ptr(), need, _raw_stream(dev.index))
+                                  ff, _ptr(ws), need, _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_gated_ffn_grad")
     return dx, dwg, dwu
@@ -293,8 +299,8 @@ def grad_norm(grads: Sequence[torch.Tensor], stream=None) -> torch.Tensor:
     words = _tensor_list(grads, "grads")
     L, n, dev, arr = lib(), len(grads), _current_device(), words.buffer_info()[0]
     need = L.isoloco_grad_norm_workspace(arr, n)
+    ws = _buffer(need, "isoloco_grad_norm_workspace", dev)
     norm = _empty((), dtype=torch.float32, device=dev)
-    ws = _empty(need, dtype=torch.uint8, device=dev) if need else None
     rc = L.isoloco_grad_norm(arr, n, norm.data_ptr(), _ptr(ws), need, _raw_stream(dev))
     if rc:
         _check(rc, "isoloco_grad_norm")
@@ -316,8 +322,8 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Seq
         outs = _tensor_list(out, "out")
     L, n, dev, arr = lib(), len(grads), _current_device(), words.buffer_info()[0]
     need = L.isoloco_grad_norm_workspace(arr, n)
+    ws = _buffer(need, "isoloco_grad_norm_workspace", dev)
     norm = _empty((), dtype=torch.float32, device=dev)
-    ws = _empty(need, dtype=torch.uint8, device=dev) if need else None
     rc = L.isoloco_clip_grads(arr, outs and outs.buffer_info()[0], n, max_norm, norm.data_ptr(), _ptr(ws), need,
                               _raw_stream(dev))
     if rc:
