@@ -14,7 +14,7 @@ IsolocoError (what the library refuses) before anything is launched.
 from __future__ import annotations
 
 import array
-from typing import NamedTuple, Optional, Sequence
+from typing import Iterable, List, NamedTuple, Optional
 
 import torch
 
@@ -278,7 +278,7 @@ def token_logprobs_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.
     return gz
 
 
-def _tensor_list(tensors: Sequence[torch.Tensor], what: str):
+def _tensor_list(tensors: List[torch.Tensor], what: str):
     """isoloco_tensor_t entries (address, length, type) as 64-bit words."""
     codes = [_DTYPE.get(t.dtype, -1) for t in tensors]
     if -1 in codes or not all(map(_is_contiguous, tensors)) or set(map(_get_device, tensors)) - {_current_device()}:
@@ -291,11 +291,11 @@ def _tensor_list(tensors: Sequence[torch.Tensor], what: str):
     return words
 
 
-def grad_norm(grads: Sequence[torch.Tensor], stream=None) -> torch.Tensor:
+def grad_norm(grads: Iterable[torch.Tensor], stream=None) -> torch.Tensor:
     """The norm over all entries of all tensors, a 0-d fp32 tensor on the device."""
+    grads = list(grads)
     if stream is not None:
         return _on(stream, grad_norm, grads)
-    grads = list(grads)
     words = _tensor_list(grads, "grads")
     L, n, dev, arr = lib(), len(grads), _current_device(), words.buffer_info()[0]
     need = L.isoloco_grad_norm_workspace(arr, n)
@@ -307,16 +307,15 @@ def grad_norm(grads: Sequence[torch.Tensor], stream=None) -> torch.Tensor:
     return norm
 
 
-def clip_grads(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
+def clip_grads(grads: Iterable[torch.Tensor], max_norm: float, out: Optional[Iterable[torch.Tensor]] = None,
                stream=None) -> torch.Tensor:
     """Scales the gradient by min(1, max_norm / norm), in place or into `out`, and returns the norm
     (0-d, fp32).  A NaN or infinite norm scales nothing."""
+    grads, out = list(grads), None if out is None else list(out)
     if stream is not None:
         return _on(stream, clip_grads, grads, max_norm, out)
-    grads = list(grads)
     words, outs = _tensor_list(grads, "grads"), None
     if out is not None:
-        out = list(out)
         if len(out) != len(grads):
             raise ValueError("out: one tensor per gradient")
         outs = _tensor_list(out, "out")
