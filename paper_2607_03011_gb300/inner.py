@@ -28,9 +28,9 @@ _INT = {torch.int32: 4, torch.int64: 8}
 MAX_TOP = 32
 
 # The smallest of these calls take a few microseconds on the GPU, so the way there is kept short: the
-# current stream's handle and the device's number without objects made for them.
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_current_device = torch._C._cuda_getDevice
+# current stream's handle and the device's number without objects made for them, where torch has these names.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _empty = torch.empty
 _data_ptr, _numel = torch.Tensor.data_ptr, torch.Tensor.numel
 _is_contiguous, _get_device = torch.Tensor.is_contiguous, torch.Tensor.get_device
