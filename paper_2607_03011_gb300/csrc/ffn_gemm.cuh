@@ -385,18 +385,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Geometry<FWD>::kThre
                 }
             }
             if (*abort_flag) {
-                // copies in flight land before the CTA exits (rank 0's barriers count both CTAs'
-                // copies; rank 1 leaves its own a generous margin)
+                // copies in flight land before the CTA exits: rank 0's barriers count both CTAs' copies, and rank 1
+                // gives up only here, by a wait of kWaitTimeoutNs behind its last copy, which has landed by then
                 if (leader) {
                     drain_barriers(kStages, [&](int s, uint64_t*& bar, uint32_t& parity) {
                         bar = &full[s];
                         parity = s < stage ? phase : phase ^ 1u;
                         return s < stage || wrapped;
                     });
-                } else {
-                    const uint64_t t0 = globaltimer_ns();
-                    while (globaltimer_ns() - t0 < 100000ull) {
-                    }
                 }
             }
         }
@@ -472,7 +468,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Geometry<FWD>::kThre
             if (!t.valid) break;
             const Product& q = *t.p;
             const uint32_t buf = i & 1;
-            if (!__all_sync(0xffffffffu, mbar_wait(&tfull[buf], (i >> 1) & 1))) {
+            // (a k-block takes 0.2 to 0.8 us; kDw's sum over all tokens may be of 2^24)
+            if (!__all_sync(0xffffffffu, mbar_wait(&tfull[buf], (i >> 1) & 1, kWaitTimeoutNs * (1u + (q.kblocks >> 20))))) {
                 if (lane == 0) atomicOr(p.err, kErrTimeout);
                 break;
             }
