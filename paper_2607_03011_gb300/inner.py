@@ -10,6 +10,11 @@ are free as long as the leading dimensions fold into one.  Every function takes 
 current stream): work is enqueued and outputs and workspaces are allocated there.  Inputs made on another stream have to be
 ordered before the call by the caller.  Bad arguments raise ValueError (shapes and types) or
 IsolocoError (what the library refuses) before anything is launched.
+
+Nothing here is recorded by autograd, as nothing in `isoloco` is: tensors that require a gradient are taken as they
+are, outputs never require one, and a loss.backward() through them reaches no operand.  Gradients come from the
+`*_grad` functions (and grad_logits of `token_logprobs`) alone, called by the training step itself as `inner_demo`
+does, or by a torch.autograd.Function around them.
 """
 from __future__ import annotations
 
