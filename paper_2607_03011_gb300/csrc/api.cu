@@ -26,6 +26,7 @@
 #include "isoloco.h"
 #include "per_device.h"
 #include "polar_loop.h"
+#include "tensor_map.h"
 #include "types.h"
 
 namespace isoloco {
@@ -301,20 +302,17 @@ int isoloco::set_error(int code, const char* msg) { return fail(code, msg); }
     } while (0)
 
 // ------------------------------------------------------------------ tensor maps
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_fn() {
+isoloco::EncodeTiledFn isoloco::tensor_map_encoder() {
+    static std::once_flag once;
     static EncodeTiledFn fn = nullptr;
-    if (!fn) {
+    std::call_once(once, [] {
         void* p = nullptr;
         cudaDriverEntryPointQueryResult q;
         if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) ==
                 cudaSuccess &&
             q == cudaDriverEntryPointSuccess)
             fn = reinterpret_cast<EncodeTiledFn>(p);
-    }
+    });
     return fn;
 }
 
@@ -322,7 +320,7 @@ static EncodeTiledFn encode_fn() {
 // gives a batch stride other than rows * ld (an n x n matrix in the first rows of a taller slot).
 static bool make_map(CUtensorMap* m, const void* base, int cols, int rows, int count, int ld, int role,
                      int64_t batch_elems = -1) {
-    EncodeTiledFn fn = encode_fn();
+    EncodeTiledFn fn = tensor_map_encoder();
     if (!fn) return false;
     cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)count};
     cuuint64_t strides[2] = {(cuuint64_t)ld * 2,

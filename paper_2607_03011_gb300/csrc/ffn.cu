@@ -21,13 +21,13 @@
 // starting and draining the pipeline weigh.  One stage's 32 KB per SM arrive in about the time that its products take,
 // so that a tile of half the columns takes 0.75 of the time, not 0.5.
 #include <algorithm>
-#include <mutex>
 
 #include "common.cuh"
 #include "ffn_gemm.cuh"
 #include "inner.cuh"
 #include "inner.h"
 #include "per_device.h"
+#include "tensor_map.h"
 
 namespace isoloco {
 
@@ -235,26 +235,9 @@ struct Arena {
 };
 
 // ------------------------------------------------------------------ tensor maps and launch
-typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                             CUtensorMapFloatOOBfill);
-
-EncodeFn encode_fn() {
-    static std::once_flag once;
-    static EncodeFn fn = nullptr;
-    std::call_once(once, [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeFn>(p);
-    });
-    return fn;
-}
-
 // rows x cols matrix of 2- or 4-byte elements, pitch in elements; boxes of 128 bytes x box_rows.
 bool make_map2(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t pitch, int box_rows, int es = 2) {
-    const EncodeFn fn = encode_fn();
+    const EncodeTiledFn fn = tensor_map_encoder();
     if (!fn) return false;
     cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
     cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch * es)};

@@ -1,0 +1,14 @@
+// tensor_map.h -- the driver's encoder of tensor maps, looked up once (defined in api.cu).
+#pragma once
+#include <cuda.h>
+
+namespace isoloco {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// cuTensorMapEncodeTiled; nullptr where the driver has none.
+EncodeTiledFn tensor_map_encoder();
+
+}  // namespace isoloco
