@@ -405,7 +405,8 @@ int isoloco_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, const voi
                       int64_t ld_h, void* saved, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Its gradient for dh (tokens x ff): with g = x w_gate, u = x w_up as saved,
- *   dg = dh u act'(g), du = dh act(g), each rounded to `dtype` (operands of the tensor cores);
+ *   dg = dh u act'(g), du = dh act(g), each rounded to `dtype` (operands of the tensor cores; up to 128 tokens the
+ *   rounded rest goes there too);
  *   dx = dg w_gate^T + du w_up^T, dw_gate = x^T dg, dw_up = x^T du.
  *   dx (pitch ld_dx) may be NULL; dw_gate and dw_up (pitch ld_dw) may be NULL together. */
 int64_t isoloco_gated_ffn_grad_workspace(int64_t tokens, int64_t width, int64_t ff, int aligned);

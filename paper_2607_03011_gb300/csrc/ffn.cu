@@ -34,8 +34,18 @@ namespace isoloco {
 namespace {
 
 // ------------------------------------------------------------------ dg and du
-// d: tokens x 2 x pitch, dg then du of a token.  8 columns per step; dh's rows may start anywhere.
-template <class T, bool GELU>
+// The rests of rounded values, rounded (none where the value has no finite form).
+template <class T>
+__device__ __forceinline__ void rests(const Vec<T>& rounded, float (&v)[8]) {
+    float r[8];
+    rounded.unpack(r);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = r[j] - r[j] == 0.f ? v[j] - r[j] : 0.f;
+}
+
+// d: tokens x 2 x pitch, dg then du of a token (SPLIT: x 4, their rests behind them).  8 columns per step; dh's rows may
+// start anywhere.
+template <class T, bool GELU, bool SPLIT>
 __global__ void __launch_bounds__(256) k_ffn_dgu(const T* __restrict__ dh, int64_t ld_dh, bool dh_vec,
                                                  const typename Kept<T>::Store* __restrict__ saved, T* __restrict__ d, int64_t tokens,
                                                  int64_t ff, int64_t pitch) {
@@ -82,12 +92,40 @@ __global__ void __launch_bounds__(256) k_ffn_dgu(const T* __restrict__ dh, int64
             dg[j] = v[j] * u[j] * s;
             du[j] = v[j] * a;
         }
+        T* out = d + (SPLIT ? at + m * 2 * pitch : at);
         Vec<T> w;
         w.pack(dg);
-        *reinterpret_cast<uint4*>(d + at) = w.raw;
+        *reinterpret_cast<uint4*>(out) = w.raw;
+        if constexpr (SPLIT) {
+            rests(w, dg);
+            w.pack(dg);
+            *reinterpret_cast<uint4*>(out + 2 * pitch) = w.raw;
+        }
         w.pack(du);
-        *reinterpret_cast<uint4*>(d + at + pitch) = w.raw;
+        *reinterpret_cast<uint4*>(out + pitch) = w.raw;
+        if constexpr (SPLIT) {
+            rests(w, du);
+            w.pack(du);
+            *reinterpret_cast<uint4*>(out + 3 * pitch) = w.raw;
+        }
     }
+}
+
+// dx of a split product: the sums over rounded values and over rests, kSplitTokens rows apart, added and rounded.
+template <class T>
+__global__ void __launch_bounds__(256) k_ffn_dx_join(const float* __restrict__ sums, int64_t pitch, T* __restrict__ dx, int64_t ld_dx,
+                                                     int tokens, int width) {
+    after_previous();
+    const uint32_t per_row = static_cast<uint32_t>(pitch >> 2), i = blockIdx.x * 256u + threadIdx.x;
+    const uint32_t t = i / per_row, c = (i - t * per_row) * 4u;
+    if (t >= static_cast<uint32_t>(tokens)) return;
+    const float4 a = *reinterpret_cast<const float4*>(sums + t * pitch + c);
+    const float4 b = *reinterpret_cast<const float4*>(sums + (kSplitTokens + t) * pitch + c);
+    const float v[4] = {a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w};
+    T* out = dx + t * ld_dx + c;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (c + j < static_cast<uint32_t>(width)) out[j] = from_f32<T>(v[j]);
 }
 
 // ------------------------------------------------------------------ few tokens
@@ -223,6 +261,8 @@ inline int64_t pitch_of(int64_t n) { return (n + 7) / 8 * 8; }
 inline bool tma_ok(const void* p, int64_t ld) { return aligned16(p) && ld % 8 == 0; }
 inline int64_t r256(int64_t b) { return (b + 255) / 256 * 256; }
 inline int64_t copy_bytes(int64_t rows, int64_t cols) { return r256(rows * pitch_of(cols) * 2); }
+inline bool splits(int64_t tokens) { return tokens > 0 && tokens <= kSplitTokens; }
+inline int64_t split_bytes(int64_t width) { return r256(2 * kSplitTokens * pitch_of(width) * 4); }  // dx's sums
 
 // Pieces of the workspace, taken one after the other.
 struct Arena {
@@ -414,7 +454,7 @@ cudaError_t forward(const FfnArgs& a, void* h, int64_t ld_h, void* saved, void* 
         if (cost < best) best = cost, static_cast<FfnTiles&>(g) = t;
     }
     g.tokens = static_cast<int>(a.tokens), g.width = static_cast<int>(a.width), g.ff = static_cast<int>(a.ff);
-    g.f16 = f16, g.keep = saved != nullptr, g.gelu = a.act == ISOLOCO_GELU_TANH;
+    g.f16 = f16, g.keep = saved != nullptr, g.gelu = a.act == ISOLOCO_GELU_TANH, g.split = false;
     TRY((launch_gemm2<T, true>(g, C, st)));
     return direct ? cudaSuccess : repitch(out, fp, h, ld_h, a.tokens, a.ff, st);
 }
@@ -431,14 +471,18 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
         return cudaSuccess;
     }
     Arena arena = {static_cast<uint8_t*>(ws)};
-    T* d = static_cast<T*>(arena.take(a.tokens * 2 * fp * 2));
+    const bool split = splits(a.tokens);
+    const int planes = split ? 2 : 1;
+    const int64_t dpitch = 2 * planes * fp;
+    T* d = static_cast<T*>(arena.take(a.tokens * dpitch * 2));
     const bool dh_vec = tma_ok(dh, ld_dh);
     int sms = 0;
     TRY(device_sms(&sms));
     const unsigned grid = static_cast<unsigned>(std::min<int64_t>((a.tokens * (fp / 8) + 255) / 256, 16 * sms));
     using Store = typename Kept<T>::Store;
-    TRY(launch_next(a.act == ISOLOCO_SILU ? k_ffn_dgu<T, false> : k_ffn_dgu<T, true>, grid, 256, st, static_cast<const T*>(dh), ld_dh, dh_vec,
-                    static_cast<const Store*>(saved), d, a.tokens, a.ff, fp));
+    const auto dgu = a.act == ISOLOCO_SILU ? (split ? k_ffn_dgu<T, false, true> : k_ffn_dgu<T, false, false>)
+                                           : (split ? k_ffn_dgu<T, true, true> : k_ffn_dgu<T, true, false>);
+    TRY(launch_next(dgu, grid, 256, st, static_cast<const T*>(dh), ld_dh, dh_vec, static_cast<const Store*>(saved), d, a.tokens, a.ff, fp));
     FfnGemm<false> g;
     bool ok = true;
     int C = 0, unused;
@@ -447,7 +491,7 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
     for (int v = 0; v < 4; ++v) {  // tiles of 256 or 128 columns for either product
         const int nx = v & 1 ? 64 : 128, nw = v & 2 ? 64 : 128, seg = tiles(a.ff, kDepth), kw = tiles(a.tokens, kDepth);
         const Product pdx = {kDx, tiles(a.tokens, 256), tiles(a.width, 2 * nx), nx, 2 * seg, seg, 1};
-        const Product pdw = {kDw, tiles(a.width, 256), tiles(a.ff, 2 * nw), nw, kw, kw, 2};
+        const Product pdw = {kDw, tiles(a.width, 256), tiles(a.ff, 2 * nw), nw, planes * kw, kw, 2};
         const int ndx = dx ? pdx.tiles_m * pdx.tiles_n : 0, ndw = dwg ? 2 * pdw.tiles_m * pdw.tiles_n : 0;
         // the product with the longer tiles first
         const bool dw_first = !dx || (dwg && tile_cost(pdw) > tile_cost(pdx));
@@ -470,10 +514,14 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
             TRY(repitch(wu, ld_w, cu, fp, a.width, a.ff, st));
             wg = cg, wu = cu, ld_w = fp;
         }
-        if (!tma_ok(dx, ldx)) odx = arena.take(copy_bytes(a.tokens, a.width)), ldx = dp;
-        ok = ok && make_map2(&g.dg_k, d, a.tokens, a.ff, 2 * fp, kTileRows) && make_map2(&g.du_k, d + fp, a.tokens, a.ff, 2 * fp, kTileRows) &&
+        if (split) odx = arena.take(split_bytes(a.width)), ldx = dp;
+        else if (!tma_ok(dx, ldx)) odx = arena.take(copy_bytes(a.tokens, a.width)), ldx = dp;
+        ok = ok && make_map2(&g.dg_k, d, a.tokens, a.ff, dpitch, kTileRows) && make_map2(&g.du_k, d + fp, a.tokens, a.ff, dpitch, kTileRows) &&
              make_map2(&g.wg_k, wg, a.width, a.ff, ld_w, pdx.nh) && make_map2(&g.wu_k, wu, a.width, a.ff, ld_w, pdx.nh) &&
-             make_map2(&g.dx, odx, a.tokens, a.width, ldx, 32);
+             make_map2(&g.dx, odx, split ? 2 * kSplitTokens : a.tokens, a.width, ldx, 32, split ? 4 : 2);
+        if (split)
+            ok = ok && make_map2(&g.dg_lo_k, d + 2 * fp, a.tokens, a.ff, dpitch, kTileRows) &&
+                 make_map2(&g.du_lo_k, d + 3 * fp, a.tokens, a.ff, dpitch, kTileRows);
     }
     if (dwg) {
         const void* x = a.x;
@@ -487,15 +535,21 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
             odg = arena.take(copy_bytes(a.width, a.ff)), odu = arena.take(copy_bytes(a.width, a.ff));
             ldw = fp;
         }
-        ok = ok && make_map2(&g.x_mn, x, a.tokens, a.width, ld_x, kDepth) && make_map2(&g.dg_mn, d, a.tokens, a.ff, 2 * fp, kDepth) &&
-             make_map2(&g.du_mn, d + fp, a.tokens, a.ff, 2 * fp, kDepth) && make_map2(&g.dwg, odg, a.width, a.ff, ldw, 32) &&
+        ok = ok && make_map2(&g.x_mn, x, a.tokens, a.width, ld_x, kDepth) && make_map2(&g.dg_mn, d, a.tokens, a.ff, dpitch, kDepth) &&
+             make_map2(&g.du_mn, d + fp, a.tokens, a.ff, dpitch, kDepth) && make_map2(&g.dwg, odg, a.width, a.ff, ldw, 32) &&
              make_map2(&g.dwu, odu, a.width, a.ff, ldw, 32);
+        if (split)
+            ok = ok && make_map2(&g.dg_lo_mn, d + 2 * fp, a.tokens, a.ff, dpitch, kDepth) &&
+                 make_map2(&g.du_lo_mn, d + 3 * fp, a.tokens, a.ff, dpitch, kDepth);
     }
     if (!ok) return kNoMap;
     g.tokens = static_cast<int>(a.tokens), g.width = static_cast<int>(a.width), g.ff = static_cast<int>(a.ff);
-    g.f16 = __is_same(T, __half), g.keep = false, g.gelu = false;
+    g.f16 = __is_same(T, __half), g.keep = false, g.gelu = false, g.split = split;
     TRY((launch_gemm2<T, false>(g, C, st)));
-    if (odx != dx) TRY(repitch(odx, ldx, dx, ld_dx, a.tokens, a.width, st));
+    if (dx && split)
+        TRY(launch_next(k_ffn_dx_join<T>, static_cast<unsigned>((a.tokens * (dp / 4) + 255) / 256), 256, st, static_cast<const float*>(odx), dp,
+                        static_cast<T*>(dx), ld_dx, static_cast<int>(a.tokens), static_cast<int>(a.width)));
+    else if (odx != dx) TRY(repitch(odx, ldx, dx, ld_dx, a.tokens, a.width, st));
     if (odg != dwg) {
         TRY(repitch(odg, ldw, dwg, ld_dw, a.width, a.ff, st));
         TRY(repitch(odu, ldw, dwu, ld_dw, a.width, a.ff, st));
@@ -512,7 +566,7 @@ int64_t ffn_saved_bytes(int64_t tokens, int64_t ff, int dtype) {
 // `aligned`: no operand needs a copy with another pitch.
 int64_t ffn_workspace(int64_t tokens, int64_t width, int64_t ff, bool backward, bool aligned) {
     int64_t n = 0;
-    if (backward) n += r256(tokens * 2 * pitch_of(ff) * 2);
+    if (backward) n += r256(tokens * (splits(tokens) ? 4 : 2) * pitch_of(ff) * 2) + (splits(tokens) ? split_bytes(width) : 0);
     // the weights and x; h, or dx and the weights' gradients
     if (!aligned) n += (backward ? 4 : 2) * copy_bytes(width, ff) + (backward ? 2 : 1) * copy_bytes(tokens, width) +
                        (backward ? 0 : copy_bytes(tokens, ff));

@@ -98,7 +98,7 @@ struct Product {
     int kind;       // kGated, kDx or kDw
     int tiles_m, tiles_n, nh;
     int kblocks;    // of one tile, over all segments
-    int seg;        // k-blocks of one segment (kDx: F's, then F's again)
+    int seg;        // k-blocks of one segment (kDx: dg's F, then du's; kDw: the tokens, with `split` once more)
     int mats;       // kDw: 2 (dWg's tiles, then dWu's), else 1
 };
 enum { kGated = 0, kDx = 1, kDw = 2 };
@@ -111,6 +111,7 @@ struct FfnTiles {
     int extra;        // rounds of p[1] that the clusters without a tile in p[0]'s last round run first
     int tokens, width, ff;
     bool f16, keep, gelu;
+    bool split;       // dg and du come as sums of two 16-bit values (kDx, kDw; see kSplitTokens)
     uint32_t* err;
 };
 template <>
@@ -120,7 +121,15 @@ struct FfnGemm<true> : FfnTiles {
 template <>
 struct FfnGemm<false> : FfnTiles {
     CUtensorMap dg_k, du_k, wg_k, wu_k, dx, x_mn, dg_mn, du_mn, dwg, dwu;
+    CUtensorMap dg_lo_k, du_lo_k, dg_lo_mn, du_lo_mn;  // with `split`: the lower values
 };
+
+// Up to so many tokens dg and du go to the tensor cores as the sum of two 16-bit values, the rounded one and the rounded
+// rest: dx and the weights' gradients of few tokens are sums of few roundings, and came out up to 1.6 times as far
+// from 64 bits as one rounding of the output is (1.05 times with the rest; 1.45 where many tokens' roundings average
+// out).  It costs few tokens little: dx's 128 rows of lower values are the second CTA's, which has no tokens of
+// its own, and the weights' gradients sum over one or two k-blocks more.
+constexpr int kSplitTokens = kTileRows;
 
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
     asm volatile(
@@ -289,6 +298,19 @@ __device__ __forceinline__ void plain_block(uint32_t tacc, int c0, const CUtenso
     st.end(map, col, row);
 }
 
+// The same of fp32 sums (128 bytes are 32 columns).
+__device__ __forceinline__ void sums_block(uint32_t tacc, int c0, const CUtensorMap* map, int col, int cols, int row, const Staging& st) {
+#pragma unroll 1
+    for (int half = 0; half < 2 && col + half * 32 < cols; ++half) {
+        uint32_t v[32];
+        st.begin();
+        tmem_ld32(tacc + c0 + half * 32, v);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) st.chunk(q, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        st.end(map, col + half * 32, row);
+    }
+}
+
 // Persistent, clusters of two CTAs; cluster c runs tile_at(c, 0), tile_at(c, 1), ...  Warp 0 loads, warp 1
 // of CTA 0 issues the pair's MMAs, the other warps of both drain the accumulators.  `full` / `empty` hand
 // stages over, `tfull` / `tempty` accumulators, as the TMA bytes and MMA commits complete.
@@ -367,14 +389,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Geometry<FWD>::kThre
                         const CUtensorMap* w = leader ? &p.wg_mn : &p.wu_mn;
                         for (int n = 0; n < q.nh; n += 64) tma_load_2d_pair(sb + n * kDepth * 2, w, bar, t.n0 + n, k0);
                     } else if (q.kind == kDx) {
-                        const bool up = kb >= q.seg;
+                        const bool up = kb >= q.seg, lo = p.split && !leader;
                         const int k0 = (up ? kb - q.seg : kb) * kDepth;
-                        tma_load_2d_pair(sa, up ? &p.du_k : &p.dg_k, bar, k0, m0);
+                        const CUtensorMap* d = lo ? (up ? &p.du_lo_k : &p.dg_lo_k) : (up ? &p.du_k : &p.dg_k);
+                        tma_load_2d_pair(sa, d, bar, k0, p.split ? t.m0 : m0);
                         tma_load_2d_pair(sb, up ? &p.wu_k : &p.wg_k, bar, k0, t.n0 + static_cast<int>(crank) * q.nh);
                     } else {
-                        const int k0 = kb * kDepth, n0 = t.n0 + static_cast<int>(crank) * q.nh;
+                        const bool lo = kb >= q.seg;
+                        const int k0 = (lo ? kb - q.seg : kb) * kDepth, n0 = t.n0 + static_cast<int>(crank) * q.nh;
                         for (int m = 0; m < kTileRows; m += 64) tma_load_2d_pair(sa + m * kDepth * 2, &p.x_mn, bar, m0 + m, k0);
-                        const CUtensorMap* d = t.mat ? &p.du_mn : &p.dg_mn;
+                        const CUtensorMap* d = lo ? (t.mat ? &p.du_lo_mn : &p.dg_lo_mn) : (t.mat ? &p.du_mn : &p.dg_mn);
                         for (int n = 0; n < q.nh; n += 64) tma_load_2d_pair(sb + n * kDepth * 2, d, bar, n0 + n, k0);
                     }
                     if (++stage == kStages) {
@@ -485,7 +509,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Geometry<FWD>::kThre
             } else {
                 const int rows = q.kind == kDx ? p.tokens : p.width, cols = q.kind == kDx ? p.width : p.ff;
                 const CUtensorMap* map = q.kind == kDx ? &p.dx : t.mat ? &p.dwu : &p.dwg;
-                if (row < rows)
+                if (q.kind == kDx && p.split) {
+                    // one tile of rows: either CTA's are the same tokens
+                    if (eg * 32 < rows)
+                        for (int c0 = half * 64; c0 < 2 * q.nh && t.n0 + c0 < cols; c0 += 128)
+                            sums_block(tacc, c0, map, t.n0 + c0, cols, row, st);
+                } else if (row < rows)
                     for (int c0 = half * 64; c0 < 2 * q.nh && t.n0 + c0 < cols; c0 += 128)
                         plain_block<T>(tacc, c0, map, t.n0 + c0, row, st);
             }
