@@ -382,7 +382,8 @@ int isoloco_embed(const void* weight, int64_t ld_weight, isoloco_dtype_t dtype, 
 
 /* The lookup's gradient: dw[v][:] = scale * sum over t with ids[t] == v of dy[t][:], every row of
  * dw written (zeros for tokens that do not occur).  The tokens are sorted by id, and a row's terms
- * are added in fp32 in an order that depends on the ids alone.
+ * are added in fp32 in an order that depends on the ids alone.  The sort runs on 8 SMs: beyond some 10^5 tokens of
+ * narrow rows its time, 0.35 ns per token, is the call's.
  *   dy: tokens x width of `dtype`; dw: vocab x width of dw_dtype (`dtype` or F32). */
 int64_t isoloco_embed_grad_workspace(int64_t vocab, int64_t width, int64_t tokens);
 int isoloco_embed_grad(const void* dy, int64_t ld_dy, isoloco_dtype_t dtype, int64_t vocab, int64_t width,
@@ -450,7 +451,8 @@ typedef struct {
 } isoloco_tensor_t;
 
 /* The gradient's global norm, sqrt(sum over all tensors and entries of g^2), to norm[0] (device
- * fp32).  Squares are taken in fp32: entries beyond 1.8e19 in magnitude give inf.
+ * fp32).  Squares are taken in fp32: entries beyond 1.8e19 in magnitude give inf, entries below 1.1e-19 lose bits
+ * and below 2.6e-23 count as zero.
  *   tensors: HOST array of `count` entries, read during the call. */
 int64_t isoloco_grad_norm_workspace(const isoloco_tensor_t* tensors, int count);
 int isoloco_grad_norm(const isoloco_tensor_t* tensors, int count, float* norm, void* workspace,

@@ -15,11 +15,12 @@
 // is a sum over 2F, theirs over T, and tiles of one fill the SMs that the other's last wave leaves idle.
 // Up to kGemvTokens tokens the block is bound by reading the weights and runs on k_ffn_few instead.
 //
-// Measured (bf16, 16384 tokens, 2048 x 5632; alone on the GPU): forward 421 us, 1.80 PFLOP/s; dg and du 145 us,
-// 6.4 TB/s; the gradient's products 790 us, 1.91 PFLOP/s (cuBLAS's burst rate on 8192^3: 1.89; in a long run the power
-// cap takes both to about nine tenths).  2047 x 1024 x 2816: 26, 12 and 33 us, where the last round of tiles and
+// Measured (bf16, 16384 tokens, 2048 x 5632; alone on the GPU): forward 418 us, 1.81 PFLOP/s; dg and du 151 us,
+// 6.1 TB/s; the gradient's products 787 us, 1.92 PFLOP/s (cuBLAS's burst rate on 8192^3: 1.89; in a long run the power
+// cap takes both to about nine tenths).  2047 x 1024 x 2816: 26, 13 and 33 us, where the last round of tiles and
 // starting and draining the pipeline weigh.  One stage's 32 KB per SM arrive in about the time that its products take,
-// so that a tile of half the columns takes 0.75 of the time, not 0.5.
+// so that a tile of half the columns takes 0.75 of the time, not 0.5.  The gradient of 33 tokens, whose dg and du go
+// to the products as two values each (kSplitTokens): 34 us for 1024 x 2816, 58 for 2048 x 5632 (31 and 55 with one value).
 #include <algorithm>
 
 #include "common.cuh"
@@ -134,8 +135,10 @@ constexpr int kFewThreads = 256;
 constexpr int kFewCols = 64;      // columns of F per cluster: 8 lanes of 16 bytes, whole 128-byte lines
 constexpr int kFewMaxSplit = 8;   // CTAs of a cluster, each a share of D
 
-// NT tokens.  One token through 2048 x 5632 bf16 takes 13.9 us, 3.3 TB/s: a CTA's loads, the sums over its warps and
-// the cluster's barriers follow one another, and the 46 MB pass in two of its CTAs' turns per SM.
+// NT tokens.  One token through 2048 x 5632 bf16 takes 13.7 us, 3.4 TB/s.  All 352 CTAs are resident at once (42
+// registers: 5 per SM fit) and wait for their loads (13.6 of the 21 cycles between a warp's instructions): a thread
+// reads 16 rows of either matrix with a few loads in flight beside its 16 sums, and x's share, the sums over the
+// warps and the cluster's barriers come before and behind.
 // A cluster of `split` CTAs owns kFewCols columns; its CTAs share D's rows, a warp reads 4
 // rows at a time (8 lanes each), and every thread keeps its 8 columns' sums for all tokens.  The sums meet by
 // shuffles, shared memory and, for the cluster's first CTA, distributed shared memory, in fixed order.

@@ -10,8 +10,9 @@ namespace isoloco {
 namespace {
 
 // ------------------------------------------------------------------ activation
-// act(g) and act'(g).  The exponential and the reciprocal are good to a few units in fp32's last place,
-// below every rounding to 16 bits that follows (e^-q past fp32's range gives s = 0).
+// act(g) and act'(g).  The reciprocal is good to a unit in fp32's last place, e^-q to about 1 + |q| units (its
+// argument q log2 e is rounded): 2^-17 at |q| = 80, far below every rounding to 16 bits that follows (e^-q
+// past fp32's range gives s = 0).
 __device__ __forceinline__ float logistic(float q) {
     float e, s;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(q * -1.4426950408889634f));

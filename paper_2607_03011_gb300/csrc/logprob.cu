@@ -12,9 +12,12 @@
 // rows, up to 8 where few would leave SMs idle.  The gradient's second pass finds its row in L2.
 //
 // Measured: 8192 x 32000 bf16 with gradient 176 us (6.0 TB/s of logits read once and gradient written; about 8
-// instructions per 32 entries and pass at 2.4 per cycle and SM: loads' latency and issue share the bound); 2049 x
+// instructions per 32 entries and pass at 2.5 per cycle and SM: loads' latency and issue share the bound); 2049 x
 // 50021 bf16 with 5 alternatives 48 us (4.3 TB/s: a row's reductions and alternatives weigh against its few
-// hundred entries per thread); 4 x 32000 fp32 with 20 alternatives 11.9 us.
+// hundred entries per thread, and 2049 rows are 1.5 rounds of the 1368 that the SMs hold); 4 x 32000 fp32 with 20
+// alternatives 11.9 us on 16 CTAs.  The gradient alone (k_logprobs_grad): 184 us for 8192 x 32000 bf16, 703 for
+// 8192 x 50021, whose rows off 16-byte boundaries it reads and writes one entry at a time (with the
+// statistics, from scalar heads and tails, 330).
 //
 // The `top` largest: the threads' own maxima, taken by groups, bound the top-th largest from below
 // (the top-th largest of kGroups group maxima); only threads whose maximum reaches the bound look again,
