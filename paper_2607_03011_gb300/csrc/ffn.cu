@@ -266,6 +266,9 @@ inline int64_t r256(int64_t b) { return (b + 255) / 256 * 256; }
 inline int64_t copy_bytes(int64_t rows, int64_t cols) { return r256(rows * pitch_of(cols) * 2); }
 inline bool splits(int64_t tokens) { return tokens > 0 && tokens <= kSplitTokens; }
 inline int64_t split_bytes(int64_t width) { return r256(2 * kSplitTokens * pitch_of(width) * 4); }  // dx's sums
+inline int slices_of(int64_t tokens) { return std::max(1, static_cast<int>((tokens + kSliceBlocks * kDepth - 1) / (kSliceBlocks * kDepth))); }
+inline int64_t slice_rows(int64_t width) { return (width + 31) / 32 * 32; }  // (stores are of 32 rows)
+inline int64_t slice_bytes(int64_t slices, int64_t width, int64_t ff) { return r256(2 * slices * slice_rows(width) * pitch_of(ff) * 4); }
 
 // Pieces of the workspace, taken one after the other.
 struct Arena {
@@ -302,6 +305,29 @@ cudaLaunchConfig_t cluster_config(unsigned grid, unsigned threads, size_t smem, 
     cfg.attrs = at;
     cfg.numAttrs = 1;
     return cfg;
+}
+
+// dw of sliced tokens: the slices' sums, in order, rounded.  blockIdx.y: which of the two matrices.
+template <class T>
+__global__ void __launch_bounds__(256) k_ffn_dw_join(const float* __restrict__ sums, int64_t pitch, int64_t slice_rows, int slices, T* __restrict__ dwg,
+                                                     T* __restrict__ dwu, int64_t ld_dw, int64_t width, int64_t ff) {
+    after_previous();
+    const int64_t per_row = pitch >> 2, total = width * per_row, stride = 2 * slice_rows * pitch;
+    T* dw = blockIdx.y ? dwu : dwg;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t r = i / per_row, c = (i - r * per_row) * 4;
+        const float* from = sums + (blockIdx.y * slice_rows + r) * pitch + c;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int s = 0; s < slices; ++s) {
+            const float4 a = __ldcs(reinterpret_cast<const float4*>(from + s * stride));
+            v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
+        }
+        T* out = dw + r * ld_dw + c;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c + j < ff) out[j] = from_f32<T>(v[j]);
+    }
 }
 
 template <class T, bool FWD>
@@ -451,13 +477,14 @@ cudaError_t forward(const FfnArgs& a, void* h, int64_t ld_h, void* saved, void* 
     int64_t best = INT64_MAX;
     for (int nh = 128; nh >= 64; nh /= 2) {
         FfnTiles t = g;
-        t.p[0] = t.p[1] = {kGated, tiles(a.tokens, 256), tiles(a.ff, nh), nh, kb, kb, 1};
+        t.p[0] = t.p[1] = {kGated, tiles(a.tokens, 256), tiles(a.ff, nh), nh, kb, kb, 1, kb};
         t.n0 = t.p[0].tiles_m * t.p[0].tiles_n;
         const int64_t cost = plan_rounds(t, std::min(C, t.n0), &unused);
         if (cost < best) best = cost, static_cast<FfnTiles&>(g) = t;
     }
     g.tokens = static_cast<int>(a.tokens), g.width = static_cast<int>(a.width), g.ff = static_cast<int>(a.ff);
     g.f16 = f16, g.keep = saved != nullptr, g.gelu = a.act == ISOLOCO_GELU_TANH, g.split = false;
+    g.slice_rows = 0;
     TRY((launch_gemm2<T, true>(g, C, st)));
     return direct ? cudaSuccess : repitch(out, fp, h, ld_h, a.tokens, a.ff, st);
 }
@@ -475,7 +502,7 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
     }
     Arena arena = {static_cast<uint8_t*>(ws)};
     const bool split = splits(a.tokens);
-    const int planes = split ? 2 : 1;
+    const int planes = split ? 2 : 1, slices = slices_of(a.tokens);
     const int64_t dpitch = 2 * planes * fp;
     T* d = static_cast<T*>(arena.take(a.tokens * dpitch * 2));
     const bool dh_vec = tma_ok(dh, ld_dh);
@@ -493,9 +520,9 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
     int64_t best = INT64_MAX;
     for (int v = 0; v < 4; ++v) {  // tiles of 256 or 128 columns for either product
         const int nx = v & 1 ? 64 : 128, nw = v & 2 ? 64 : 128, seg = tiles(a.ff, kDepth), kw = tiles(a.tokens, kDepth);
-        const Product pdx = {kDx, tiles(a.tokens, 256), tiles(a.width, 2 * nx), nx, 2 * seg, seg, 1};
-        const Product pdw = {kDw, tiles(a.width, 256), tiles(a.ff, 2 * nw), nw, planes * kw, kw, 2};
-        const int ndx = dx ? pdx.tiles_m * pdx.tiles_n : 0, ndw = dwg ? 2 * pdw.tiles_m * pdw.tiles_n : 0;
+        const Product pdx = {kDx, tiles(a.tokens, 256), tiles(a.width, 2 * nx), nx, 2 * seg, seg, 1, 2 * seg};
+        const Product pdw = {kDw, tiles(a.width, 256), tiles(a.ff, 2 * nw), nw, std::min(planes * kw, kSliceBlocks), kw, 2 * slices, planes * kw};
+        const int ndx = dx ? pdx.tiles_m * pdx.tiles_n : 0, ndw = dwg ? pdw.mats * pdw.tiles_m * pdw.tiles_n : 0;
         // the product with the longer tiles first
         const bool dw_first = !dx || (dwg && tile_cost(pdw) > tile_cost(pdx));
         FfnTiles t = g;
@@ -534,13 +561,16 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
             TRY(repitch(x, ld_x, cx, dp, a.tokens, a.width, st));
             x = cx, ld_x = dp;
         }
-        if (!tma_ok(dwg, ldw) || !tma_ok(dwu, ldw)) {
+        if (slices > 1) {
+            odg = arena.take(slice_bytes(slices, a.width, a.ff)), odu = nullptr, ldw = fp;
+        } else if (!tma_ok(dwg, ldw) || !tma_ok(dwu, ldw)) {
             odg = arena.take(copy_bytes(a.width, a.ff)), odu = arena.take(copy_bytes(a.width, a.ff));
             ldw = fp;
         }
         ok = ok && make_map2(&g.x_mn, x, a.tokens, a.width, ld_x, kDepth) && make_map2(&g.dg_mn, d, a.tokens, a.ff, dpitch, kDepth) &&
-             make_map2(&g.du_mn, d + fp, a.tokens, a.ff, dpitch, kDepth) && make_map2(&g.dwg, odg, a.width, a.ff, ldw, 32) &&
-             make_map2(&g.dwu, odu, a.width, a.ff, ldw, 32);
+             make_map2(&g.du_mn, d + fp, a.tokens, a.ff, dpitch, kDepth);
+        if (slices > 1) ok = ok && make_map2(&g.dwg, odg, 2 * slices * slice_rows(a.width), a.ff, fp, 32, 4);
+        else ok = ok && make_map2(&g.dwg, odg, a.width, a.ff, ldw, 32) && make_map2(&g.dwu, odu, a.width, a.ff, ldw, 32);
         if (split)
             ok = ok && make_map2(&g.dg_lo_mn, d + 2 * fp, a.tokens, a.ff, dpitch, kDepth) &&
                  make_map2(&g.du_lo_mn, d + 3 * fp, a.tokens, a.ff, dpitch, kDepth);
@@ -548,12 +578,17 @@ cudaError_t backward(const FfnArgs& a, const void* dh, int64_t ld_dh, const void
     if (!ok) return kNoMap;
     g.tokens = static_cast<int>(a.tokens), g.width = static_cast<int>(a.width), g.ff = static_cast<int>(a.ff);
     g.f16 = __is_same(T, __half), g.keep = false, g.gelu = false, g.split = split;
+    g.slice_rows = slices > 1 ? static_cast<int>(slice_rows(a.width)) : 0;
     TRY((launch_gemm2<T, false>(g, C, st)));
     if (dx && split)
         TRY(launch_next(k_ffn_dx_join<T>, static_cast<unsigned>((a.tokens * (dp / 4) + 255) / 256), 256, st, static_cast<const float*>(odx), dp,
                         static_cast<T*>(dx), ld_dx, static_cast<int>(a.tokens), static_cast<int>(a.width)));
     else if (odx != dx) TRY(repitch(odx, ldx, dx, ld_dx, a.tokens, a.width, st));
-    if (odg != dwg) {
+    if (dwg && slices > 1) {
+        const dim3 blocks(static_cast<unsigned>(std::min<int64_t>((a.width * (fp / 4) + 255) / 256, 16 * sms)), 2);
+        TRY(launch_next(k_ffn_dw_join<T>, blocks, 256, st, static_cast<const float*>(odg), fp, slice_rows(a.width), slices, static_cast<T*>(dwg),
+                        static_cast<T*>(dwu), ld_dw, a.width, a.ff));
+    } else if (odg != dwg) {
         TRY(repitch(odg, ldw, dwg, ld_dw, a.width, a.ff, st));
         TRY(repitch(odu, ldw, dwu, ld_dw, a.width, a.ff, st));
     }
@@ -569,7 +604,8 @@ int64_t ffn_saved_bytes(int64_t tokens, int64_t ff, int dtype) {
 // `aligned`: no operand needs a copy with another pitch.
 int64_t ffn_workspace(int64_t tokens, int64_t width, int64_t ff, bool backward, bool aligned) {
     int64_t n = 0;
-    if (backward) n += r256(tokens * (splits(tokens) ? 4 : 2) * pitch_of(ff) * 2) + (splits(tokens) ? split_bytes(width) : 0);
+    if (backward) n += r256(tokens * (splits(tokens) ? 4 : 2) * pitch_of(ff) * 2) + (splits(tokens) ? split_bytes(width) : 0) +
+                       (slices_of(tokens) > 1 ? slice_bytes(slices_of(tokens), width, ff) : 0);
     // the weights and x; h, or dx and the weights' gradients
     if (!aligned) n += (backward ? 4 : 2) * copy_bytes(width, ff) + (backward ? 2 : 1) * copy_bytes(tokens, width) +
                        (backward ? 0 : copy_bytes(tokens, ff));

@@ -100,9 +100,16 @@ struct Product {
     int tiles_m, tiles_n, nh;
     int kblocks;    // of one tile, over all segments
     int seg;        // k-blocks of one segment (kDx: dg's F, then du's; kDw: the tokens, with `split` once more)
-    int mats;       // kDw: 2 (dWg's tiles, then dWu's), else 1
+    int mats;       // kDw: 2 (dWg's tiles, then dWu's) for every slice of the tokens, else 1
+    int all;        // k-blocks of all slices
 };
 enum { kGated = 0, kDx = 1, kDw = 2 };
+
+// The tensor core adds a k-block's products to the sum by cutting off what lies below its last places: a sum of one sign
+// loses some 6e-9 of itself with every product, 4e-4 over 2^16 tokens, 6.6e-3 over 2^20.  More than 2^16 tokens are
+// summed in slices of as many, each to fp32 sums in memory, which are added in order (1.4e-3 in all, one rounding to
+// bf16, at any length; the gradient of 131072 x 1024 x 2816 takes 2.28 ms, in one slice 2.21).
+constexpr int kSliceBlocks = 65536 / kDepth;
 
 template <bool FWD>
 struct FfnGemm;
@@ -113,6 +120,7 @@ struct FfnTiles {
     int tokens, width, ff;
     bool f16, keep, gelu;
     bool split;       // dg and du come as sums of two 16-bit values (kDx, kDw; see kSplitTokens)
+    int slice_rows;   // kDw in slices of the tokens (kSliceBlocks): rows of one slice's fp32 sums of a matrix; 0: one slice
     uint32_t* err;
 };
 template <>
@@ -150,7 +158,8 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
 // p[0]'s last round left out for `extra` rounds and then go round all, those clusters first.
 struct TileAt {
     const Product* p;
-    int m0, n0, mat;  // first row of the pair's 256, first column, matrix (kDw)
+    int m0, n0, mat;  // first row of the pair's 256, first column, matrix (kDw: 2 slice + which)
+    int k0, nkb;      // its k-blocks
     bool valid;
 };
 __device__ __forceinline__ TileAt tile_at(const FfnTiles& g, int c, int C, int i) {
@@ -180,6 +189,8 @@ __device__ __forceinline__ TileAt tile_at(const FfnTiles& g, int c, int C, int i
     const int per = r.p->tiles_m * r.p->tiles_n;
     r.mat = t / per;
     t -= r.mat * per;
+    r.k0 = r.p->kind == kDw ? (r.mat >> 1) * r.p->kblocks : 0;
+    r.nkb = min(r.p->kblocks, r.p->all - r.k0);
     // panels of up to 8 tile rows, column by column: the clusters of one round share rows and columns
     const int panel = t / (8 * r.p->tiles_n), in = t - panel * 8 * r.p->tiles_n;
     const int rows = min(8, r.p->tiles_m - panel * 8);
@@ -375,7 +386,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Geometry<FWD>::kThre
                 const Product& q = *t.p;
                 const int m0 = t.m0 + static_cast<int>(crank) * kTileRows;
                 const uint32_t pair_bytes = 2u * (kABytes + static_cast<uint32_t>(q.nh) * kDepth * 2u);
-                for (int kb = 0; kb < q.kblocks; ++kb) {
+                for (int kb = 0; kb < t.nkb; ++kb) {
                     if (!mbar_wait(&empty[stage], phase ^ 1u)) {
                         *abort_flag = 1;
                         atomicOr(p.err, kErrTimeout);
@@ -396,10 +407,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Geometry<FWD>::kThre
                         tma_load_2d_pair(sa, d, bar, k0, p.split ? t.m0 : m0);
                         tma_load_2d_pair(sb, up ? &p.wu_k : &p.wg_k, bar, k0, t.n0 + static_cast<int>(crank) * q.nh);
                     } else {
-                        const bool lo = kb >= q.seg;
-                        const int k0 = (lo ? kb - q.seg : kb) * kDepth, n0 = t.n0 + static_cast<int>(crank) * q.nh;
+                        const int k = t.k0 + kb;
+                        const bool lo = k >= q.seg;
+                        const int k0 = (lo ? k - q.seg : k) * kDepth, n0 = t.n0 + static_cast<int>(crank) * q.nh;
                         for (int m = 0; m < kTileRows; m += 64) tma_load_2d_pair(sa + m * kDepth * 2, &p.x_mn, bar, m0 + m, k0);
-                        const CUtensorMap* d = lo ? (t.mat ? &p.du_lo_mn : &p.dg_lo_mn) : (t.mat ? &p.du_mn : &p.dg_mn);
+                        const bool up = t.mat & 1;
+                        const CUtensorMap* d = lo ? (up ? &p.du_lo_mn : &p.dg_lo_mn) : (up ? &p.du_mn : &p.dg_mn);
                         for (int n = 0; n < q.nh; n += 64) tma_load_2d_pair(sb + n * kDepth * 2, d, bar, n0 + n, k0);
                     }
                     if (++stage == kStages) {
@@ -448,7 +461,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Geometry<FWD>::kThre
                 tc_fence_after();
                 const uint32_t tacc = tmem_base + buf * kAccCols;
                 uint32_t acc = 0;
-                const int nkb = q.kblocks;
+                const int nkb = t.nkb;
                 bool ready = mbar_test(&full[stage], phase);
 #pragma unroll 1
                 for (int kb = 0; kb < nkb; ++kb) {
@@ -493,8 +506,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Geometry<FWD>::kThre
             if (!t.valid) break;
             const Product& q = *t.p;
             const uint32_t buf = i & 1;
-            // (a k-block takes 0.2 to 0.8 us; kDw's sum over all tokens may be of 2^24)
-            if (!__all_sync(0xffffffffu, mbar_wait(&tfull[buf], (i >> 1) & 1, kWaitTimeoutNs * (1u + (q.kblocks >> 20))))) {
+            // (a k-block takes 0.2 to 0.8 us, and a tile has at most 2^15 of them)
+            if (!__all_sync(0xffffffffu, mbar_wait(&tfull[buf], (i >> 1) & 1))) {
                 if (lane == 0) atomicOr(p.err, kErrTimeout);
                 break;
             }
@@ -515,6 +528,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Geometry<FWD>::kThre
                     if (eg * 32 < rows)
                         for (int c0 = half * 64; c0 < 2 * q.nh && t.n0 + c0 < cols; c0 += 128)
                             sums_block(tacc, c0, map, t.n0 + c0, cols, row, st);
+                } else if (q.kind == kDw && p.slice_rows) {
+                    if (row < rows)
+                        for (int c0 = half * 64; c0 < 2 * q.nh && t.n0 + c0 < cols; c0 += 128)
+                            sums_block(tacc, c0, &p.dwg, t.n0 + c0, cols, t.mat * p.slice_rows + row, st);
                 } else if (row < rows)
                     for (int c0 = half * 64; c0 < 2 * q.nh && t.n0 + c0 < cols; c0 += 128)
                         plain_block<T>(tacc, c0, map, t.n0 + c0, row, st);

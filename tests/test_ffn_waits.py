@@ -24,8 +24,12 @@ def test_every_wait_that_gives_up_raises():
         assert "kErrTimeout" in after or "ok = false" in after, after
 
 
-def test_the_wait_for_a_tile_grows_with_its_product():
-    """A tile of dw_gate sums over all tokens, up to 2^30 of them: 2^24 k-blocks, many seconds of work that is no
-    failure.  The epilogue's limit goes by the tile's k-blocks."""
-    wait = re.search(r"mbar_wait\(&tfull\[buf\],([^{;]*)\)\)", SRC)
-    assert wait and "q.kblocks" in wait[1], wait and wait[0]
+def test_no_tile_works_for_as_long_as_a_wait_may_last():
+    """The weights' gradients sum over all tokens, up to 2^30 of them: 2^24 k-blocks, many seconds of work that is no
+    failure.  A tile sums over a slice of them, so that its longest product is dx's, 2 ff, of 2^15 k-blocks."""
+    depth = int(re.search(r"constexpr int kDepth = (\d+)", SRC)[1])
+    tokens = int(re.search(r"constexpr int kSliceBlocks = (\d+) / kDepth;", SRC)[1])
+    longest = max(tokens // depth, 2 * 2 ** 20 // depth)
+    assert longest * 0.8e-6 < 0.1 * 2.0
+    host = open(os.path.join(ROOT, "paper_2607_03011_gb300", "csrc", "ffn.cu")).read()
+    assert re.search(r"kDw,[^;]*std::min\(planes \* kw, kSliceBlocks\)", host)
