@@ -1,4 +1,4 @@
-// tensor_map.h -- the driver's encoder of tensor maps, looked up once (defined in api.cu).
+// tensor_map.h -- the CUDA driver API's encoder of tensor maps, looked up once (defined in api.cu).
 #pragma once
 #include <cuda.h>
 
@@ -8,7 +8,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// cuTensorMapEncodeTiled; nullptr where the driver has none.
+// cuTensorMapEncodeTiled; nullptr where the API has none.
 EncodeTiledFn tensor_map_encoder();
 
 }  // namespace isoloco
