@@ -445,6 +445,75 @@ int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_d
                                 const float* entropy, const float* grad_logp, const float* grad_entropy,
                                 void* grad_logits, int64_t ld_grad, void* stream);
 
+/* Distillation from a teacher's top logits.  Per row, k tokens and the logarithms of the teacher's probabilities for
+ * them (as isoloco_token_logprobs gives its top_logp and top_index: the student's `scale` is then the teacher's too), against the student's
+ * p = softmax(scale * logits):
+ *   tail DROP: q = softmax(top_logp) over the row's list, r = 0;
+ *   tail REST: q = exp(top_logp), and r = max(0, 1 - sum q) is one more outcome, any token outside the list, whose
+ *     probability is the student's P = sum over those tokens of p.  (r counts as 0 where every such token is masked.)
+ *   loss = sum_i q_i (log q_i - log p_i) + r (log r - log P), with 0 log 0 = 0.
+ *   gradient by the logits, with Q = sum_i q_i + r:  grad_loss scale (p_j Q - q_j) for a token of the list (q_j summed
+ *     over its entries, where it has several), grad_loss scale p_j (Q - r / P) for any other.
+ * An entry whose index is outside [0, vocab) is not there.  A row without entries (or, with DROP, whose entries all
+ * have the weight 0) has the loss 0 and the gradient 0, whatever its logits.  Logits of -inf or the type's lowest value are masked and have probability 0: the
+ * loss is +inf where an entry of weight above 0 is masked, and its gradient finite; in a row that is masked altogether the gradient is 0.
+ * A NaN or +inf among a row's logits or top_logp makes its loss and gradient NaN.
+ *   logits: rows x vocab of `dtype`; top_logp: rows x k of logp_dtype; top_index: rows x k of index_bytes (4 or 8), signed;
+ *   1 <= k <= ISOLOCO_MAX_LIST; loss: rows fp32; saved (may be NULL): rows x 2 fp32, for isoloco_distill_grad;
+ *   scale > 0.
+ * With grad_logits (rows x vocab of `dtype`, pitch ld_grad; may be the logits themselves, else NULL) the call also writes
+ * the gradient of sum_r grad_loss[r] loss[r] (grad_loss: rows fp32). */
+#define ISOLOCO_MAX_LIST 256
+typedef enum { ISOLOCO_TAIL_DROP = 0, ISOLOCO_TAIL_REST = 1 } isoloco_tail_t;
+int isoloco_distill(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows, int64_t vocab,
+                    const void* top_logp, int64_t ld_logp, isoloco_dtype_t logp_dtype, const void* top_index,
+                    int64_t ld_index, int index_bytes, int k, float scale, isoloco_tail_t tail, float* loss, float* saved,
+                    const float* grad_loss, void* grad_logits, int64_t ld_grad, void* stream);
+
+/* The same gradient by itself, from what an earlier call on the same operands saved. */
+int isoloco_distill_grad(const float* grad_loss, const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows,
+                         int64_t vocab, const void* top_logp, int64_t ld_logp, isoloco_dtype_t logp_dtype,
+                         const void* top_index, int64_t ld_index, int index_bytes, int k, float scale, isoloco_tail_t tail,
+                         const float* saved, void* grad_logits, int64_t ld_grad, void* stream);
+
+/* One step of a beam search: the continuations of the largest totals among all beams of a batch entry and all tokens.
+ *   total(w, t) = scores[w] + log p_t, p = softmax(scale * logits[w]); a beam that is finished (finished[w] != 0; NULL:
+ *   none is) continues with the token `end` alone, at its own score, and its logits are not read.
+ * The `keep` largest totals, largest first; among equal ones the lower beam, then the larger logit, then the lower token comes first.
+ * Totals are compared in 64 bits before they are rounded to fp32 (log sums are good to some 1e-7).  Masked tokens (logits of -inf or the type's lowest value), a finished
+ * beam's other tokens and all tokens of a beam whose score is -inf or whose tokens are all masked have the total -inf, and rank by
+ * beam and token, so that there are always `keep` answers (in a beam that is not
+ * finished and has unmasked tokens the type's lowest value ranks before -inf).  A beam whose score is NaN or +inf, or whose logits hold a NaN or
+ * +inf while it is not finished, ranks like one of score -inf, and its totals are given as NaN.
+ *   logits: batch * beams rows x vocab of `dtype`; scores: batch x beams fp32; finished: batch x beams bytes;
+ *   1 <= beams <= ISOLOCO_MAX_BEAMS, 1 <= keep <= min(beams * vocab, ISOLOCO_MAX_TOP); `end`: a token, or negative for
+ *   none (finished must then be NULL); out_scores (fp32), out_beams, out_tokens (int64): batch x keep; out_finished (may be NULL):
+ *   batch x keep bytes, 1 where the beam continued was finished or the token is `end`. */
+#define ISOLOCO_MAX_BEAMS 32
+int isoloco_beam_select(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t batch, int64_t beams,
+                        int64_t vocab, const float* scores, const uint8_t* finished, int64_t end, float scale, int keep,
+                        float* out_scores, int64_t* out_beams, int64_t* out_tokens, uint8_t* out_finished, void* stream);
+
+/* What is kept for a beam (a cache, a history of tokens): `outer` pieces of `run` bytes, at byte strides.  The piece
+ * of beam w of batch entry b starts at src + b src_batch + w src_beam + o src_outer. */
+typedef struct {
+    const void* src;
+    void* dst;
+    int64_t src_batch, src_beam, src_outer;
+    int64_t dst_batch, dst_beam, dst_outer;
+    int64_t outer, run;
+} isoloco_state_t;
+
+/* dst[b][w] = src[b][beams[b][w]] for every state; an entry of `beams` outside [0, width) stands for the beam itself.
+ * A state whose dst and strides are its src's is reordered in place.  Otherwise nothing that is written may share
+ * memory with anything else of the call: destinations that overlap themselves, another state's memory, or
+ * cannot be told apart from it by their addresses and strides are refused.
+ *   states: HOST array of `count` entries, read during the call; beams: batch x width entries of id_bytes (4 or 8);
+ *   1 <= width <= ISOLOCO_MAX_BEAMS; strides not negative.  Addresses, strides and runs that are multiples of 16 bytes run
+ *   faster. */
+int isoloco_beam_reorder(const isoloco_state_t* states, int count, int64_t batch, int64_t width, const void* beams,
+                         int id_bytes, void* stream);
+
 /* One tensor of a gradient: n contiguous elements, n up to 2^33. */
 typedef struct {
     void* data;

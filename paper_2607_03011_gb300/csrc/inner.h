@@ -55,6 +55,44 @@ cudaError_t launch_logprobs(const LogprobArgs& a, cudaStream_t st);
 // a.lse and a.entropy are read
 cudaError_t launch_logprobs_grad(const LogprobArgs& a, cudaStream_t st);
 
+struct DistillArgs {
+    const void* logits;
+    int64_t ld, rows, vocab;
+    int dtype;
+    const void* top_logp;
+    int64_t ld_logp;
+    int logp_dtype;
+    const void* top_index;
+    int64_t ld_index;
+    bool index64;
+    int k;
+    float scale;
+    bool rest;
+    float *loss, *saved;
+    const float* grad_loss;
+    void* grad_logits;
+    int64_t ld_grad;
+};
+cudaError_t launch_distill(const DistillArgs& a, cudaStream_t st);
+// a.saved is read; a.loss is not written
+cudaError_t launch_distill_grad(const DistillArgs& a, cudaStream_t st);
+
+struct BeamArgs {
+    const void* logits;
+    int64_t ld, batch, vocab, end;
+    int dtype, beams, keep;
+    const float* scores;
+    const uint8_t* finished;
+    float scale;
+    float* out_scores;
+    int64_t *out_beams, *out_tokens;
+    uint8_t* out_finished;
+};
+cudaError_t launch_beam_select(const BeamArgs& a, cudaStream_t st);
+
+cudaError_t launch_beam_reorder(const isoloco_state_t* states, int count, int64_t batch, int width, const void* beams,
+                                bool ids64, cudaStream_t st);
+
 int64_t grad_norm_workspace(const isoloco_tensor_t* in, int count);
 // clip: false writes the norm only
 cudaError_t launch_clip(const isoloco_tensor_t* in, const isoloco_tensor_t* out, int count, bool clip, float max_norm,

@@ -1,6 +1,8 @@
 // inner_api.cu -- C entry points of the inner step's operators: argument checks, then the launchers.
+#include <algorithm>
 #include <climits>
 #include <string>
+#include <vector>
 
 #include "common.cuh"
 #include "inner.h"
@@ -115,6 +117,131 @@ const char* tensors_problem(const isoloco_tensor_t* t, int count) {
         if (!any_dtype(t[i].dtype)) return "bad element type in the tensor list";
         if (t[i].n < 0 || t[i].n > kMaxTensorElems) return "a tensor's length must be in 0 .. 2^33";
         if (!array_ok(t[i].data, t[i].n, elem_size(t[i].dtype))) return "a tensor's data is NULL or misaligned";
+    }
+    return nullptr;
+}
+
+const char* distill_problem(const DistillArgs& a, int index_bytes, int tail) {
+    if (!any_dtype(a.dtype) || !any_dtype(a.logp_dtype)) return "bad element type";
+    if (!size_ok(a.rows, 0) || !size_ok(a.vocab, 1)) return "rows must be in 0 .. 2^31 - 1, vocab in 1 .. 2^31 - 1";
+    if (a.k < 1 || a.k > ISOLOCO_MAX_LIST) return "k must be in 1 .. 256";
+    if (!matrix_ok(a.logits, a.rows, a.vocab, a.ld, elem_size(a.dtype))) return "logits is NULL, misaligned or its pitch too small";
+    if (!matrix_ok(a.top_logp, a.rows, a.k, a.ld_logp, elem_size(a.logp_dtype))) return "top_logp is NULL, misaligned or its pitch too small";
+    if (index_bytes != 4 && index_bytes != 8) return "index_bytes must be 4 or 8";
+    if (!matrix_ok(a.top_index, a.rows, a.k, a.ld_index, index_bytes)) return "top_index is NULL, misaligned or its pitch too small";
+    if (!(a.scale > 0.f) || a.scale > 1e30f) return "scale must be positive and finite";
+    if (tail != ISOLOCO_TAIL_DROP && tail != ISOLOCO_TAIL_REST) return "bad tail";
+    if (a.grad_logits) {
+        if (!matrix_ok(a.grad_logits, a.rows, a.vocab, a.ld_grad, elem_size(a.dtype))) return "grad_logits is misaligned or its pitch too small";
+        if (!array_ok(a.grad_loss, a.rows, 4)) return "grad_loss is NULL or misaligned";
+    }
+    if (!aligned_to(a.saved, 4)) return "saved is misaligned";
+    return nullptr;
+}
+
+// ---- states that are reordered: what they may share
+
+// The addresses of one side of a state.
+struct Places {
+    uint64_t at;
+    uint64_t batch, beam, outer;  // strides
+    uint64_t pieces, run;
+    bool written;
+    uint64_t block() const { return (pieces - 1) * outer + run; }  // a beam's
+};
+
+// Whether the strides, each over the extent of the smaller ones, keep all pieces apart; their extent.
+bool nested(const Places& p, uint64_t batch, uint64_t beams, uint64_t* extent) {
+    std::pair<uint64_t, uint64_t> dim[3] = {{p.outer, p.pieces}, {p.beam, beams}, {p.batch, batch}};
+    std::sort(dim, dim + 3);
+    uint64_t e = p.run;
+    bool apart = true;
+    for (const auto& d : dim)
+        if (d.second > 1) {
+            apart = apart && d.first >= e;
+            e += (d.second - 1) * d.first;
+        }
+    *extent = e;
+    return apart;
+}
+
+// Whether two ranges of addresses overlap that lie `delta` apart (the second behind the first).
+bool ranges_meet(int64_t delta, uint64_t first, uint64_t second) {
+    return delta < 0 ? static_cast<uint64_t>(-delta) < second : static_cast<uint64_t>(delta) < first;
+}
+
+// Whether no piece of one is known to meet a piece of the other: equal strides of batch and beam, between which the
+// distance of the two leaves room for both beams' blocks, or, with equal strides of pieces too, for both runs.
+bool apart(const Places& a, const Places& b, uint64_t batch, uint64_t beams) {
+    if ((batch > 1 && a.batch != b.batch) || (beams > 1 && a.beam != b.beam)) return false;
+    const bool same_outer = a.outer == b.outer || (a.pieces == 1 && b.pieces == 1);
+    struct Dim {
+        uint64_t stride, n;
+    } dim[3] = {{a.batch, batch}, {a.beam, beams}, {a.outer, same_outer ? std::max(a.pieces, b.pieces) : 1}};
+    uint64_t first = same_outer ? a.run : a.block(), second = same_outer ? b.run : b.block();
+    std::sort(dim, dim + 3, [](const Dim& x, const Dim& y) { return x.stride > y.stride; });
+    // nested strides: the distance less a multiple of the largest, rounded down or up, and so on
+    uint64_t e = std::max(first, second);
+    for (int i = 2; i >= 0; --i)
+        if (dim[i].n > 1) {
+            if (dim[i].stride < e) return false;
+            e += (dim[i].n - 1) * dim[i].stride;
+        }
+    const int64_t delta = static_cast<int64_t>(b.at - a.at);
+    for (int pick = 0; pick < 8; ++pick) {
+        int64_t d = delta;
+        bool there = true;
+        for (int i = 0; i < 3 && there; ++i) {
+            const bool up = pick >> i & 1;
+            if (dim[i].n < 2) {
+                there = !up;
+                continue;
+            }
+            const int64_t s = static_cast<int64_t>(dim[i].stride);
+            int64_t q = d / s - (d % s < 0 ? 1 : 0) + (up ? 1 : 0);
+            const int64_t most = static_cast<int64_t>(dim[i].n) - 1;
+            q = std::min(std::max(q, -most), most);
+            d -= q * s;
+        }
+        if (there && ranges_meet(d, first, second)) return false;
+    }
+    return true;
+}
+
+const char* states_problem(const isoloco_state_t* t, int count, int64_t batch, int64_t width) {
+    constexpr int64_t kFar = int64_t(1) << 46;  // no byte of a state is further from its start
+    if (count < 0 || (count > 0 && !t)) return "bad list of states";
+    std::vector<Places> all;
+    all.reserve(2 * static_cast<size_t>(count));
+    for (int i = 0; i < count; ++i) {
+        const isoloco_state_t& s = t[i];
+        if (s.outer < 0 || s.run < 0 || s.outer > kFar || s.run > kFar) return "a state's pieces and their length must not be negative";
+        if (s.outer == 0 || s.run == 0 || batch == 0) continue;
+        if (!s.src || !s.dst) return "a state's address is NULL";
+        for (const int64_t v : {s.src_batch, s.src_beam, s.src_outer, s.dst_batch, s.dst_beam, s.dst_outer})
+            if (v < 0 || v > kFar) return "a state's strides must be in 0 .. 2^46";
+        const double far = static_cast<double>(batch) * std::max(s.src_batch, s.dst_batch) +
+                           static_cast<double>(width) * std::max(s.src_beam, s.dst_beam) +
+                           static_cast<double>(s.outer) * std::max(s.src_outer, s.dst_outer) + s.run;
+        if (far > static_cast<double>(kFar)) return "a state must lie within 2^46 bytes";
+        const Places src = {reinterpret_cast<uint64_t>(s.src), static_cast<uint64_t>(s.src_batch), static_cast<uint64_t>(s.src_beam),
+                            static_cast<uint64_t>(s.src_outer), static_cast<uint64_t>(s.outer), static_cast<uint64_t>(s.run), false};
+        const Places dst = {reinterpret_cast<uint64_t>(s.dst), static_cast<uint64_t>(s.dst_batch), static_cast<uint64_t>(s.dst_beam),
+                            static_cast<uint64_t>(s.dst_outer), static_cast<uint64_t>(s.outer), static_cast<uint64_t>(s.run), true};
+        const bool in_place = src.at == dst.at && (batch < 2 || src.batch == dst.batch) && (width < 2 || src.beam == dst.beam) &&
+                              (s.outer < 2 || src.outer == dst.outer);
+        uint64_t extent;
+        if (!nested(dst, batch, width, &extent)) return "a state's destination overlaps itself";
+        all.push_back(dst);
+        if (!in_place) all.push_back(src);
+    }
+    std::sort(all.begin(), all.end(), [](const Places& a, const Places& b) { return a.at < b.at; });
+    for (size_t i = 0; i < all.size(); ++i) {
+        uint64_t extent;
+        nested(all[i], batch, width, &extent);
+        for (size_t j = i + 1; j < all.size() && all[j].at < all[i].at + extent; ++j)
+            if ((all[i].written || all[j].written) && !apart(all[i], all[j], batch, width))
+                return "a state's destination shares memory with another state or its own source, or may";
     }
     return nullptr;
 }
@@ -241,6 +368,67 @@ int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_d
     if (rows > 0 && !grad_logits) return invalid("grad_logits is NULL");
     if (grad_entropy && !array_ok(entropy, rows, 4)) return invalid("entropy is NULL or misaligned");
     return cuda_status(launch_logprobs_grad(a, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
+}
+
+int isoloco_distill(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows, int64_t vocab,
+                    const void* top_logp, int64_t ld_logp, isoloco_dtype_t logp_dtype, const void* top_index,
+                    int64_t ld_index, int index_bytes, int k, float scale, isoloco_tail_t tail, float* loss, float* saved,
+                    const float* grad_loss, void* grad_logits, int64_t ld_grad, void* stream) try {
+    const DistillArgs a = {logits, ld_logits, rows, vocab, dtype, top_logp, ld_logp, logp_dtype, top_index, ld_index,
+                           index_bytes == 8, k, scale, tail == ISOLOCO_TAIL_REST, loss, saved, grad_loss, grad_logits, ld_grad};
+    if (const char* p = distill_problem(a, index_bytes, tail)) return invalid(p);
+    if (!array_ok(loss, rows, 4)) return invalid("loss is NULL or misaligned");
+    return cuda_status(launch_distill(a, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
+}
+
+int isoloco_distill_grad(const float* grad_loss, const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows,
+                         int64_t vocab, const void* top_logp, int64_t ld_logp, isoloco_dtype_t logp_dtype,
+                         const void* top_index, int64_t ld_index, int index_bytes, int k, float scale, isoloco_tail_t tail,
+                         const float* saved, void* grad_logits, int64_t ld_grad, void* stream) try {
+    const DistillArgs a = {logits, ld_logits, rows, vocab, dtype, top_logp, ld_logp, logp_dtype, top_index, ld_index,
+                           index_bytes == 8, k, scale, tail == ISOLOCO_TAIL_REST, nullptr, const_cast<float*>(saved), grad_loss,
+                           grad_logits, ld_grad};
+    if (rows > 0 && !grad_logits) return invalid("grad_logits is NULL");
+    if (const char* p = distill_problem(a, index_bytes, tail)) return invalid(p);
+    if (!array_ok(saved, rows, 4)) return invalid("saved is NULL or misaligned");
+    return cuda_status(launch_distill_grad(a, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
+}
+
+int isoloco_beam_select(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t batch, int64_t beams,
+                        int64_t vocab, const float* scores, const uint8_t* finished, int64_t end, float scale, int keep,
+                        float* out_scores, int64_t* out_beams, int64_t* out_tokens, uint8_t* out_finished, void* stream) try {
+    if (!any_dtype(dtype)) return invalid("bad element type");
+    if (beams < 1 || beams > ISOLOCO_MAX_BEAMS) return invalid("beams must be in 1 .. 32");
+    if (!size_ok(batch, 0) || !size_ok(batch * beams, 0) || !size_ok(vocab, 1)) return invalid("batch * beams must be in 0 .. 2^31 - 1, vocab in 1 .. 2^31 - 1");
+    if (keep < 1 || keep > ISOLOCO_MAX_TOP || keep > beams * vocab) return invalid("keep must be in 1 .. min(beams * vocab, 32)");
+    if (!matrix_ok(logits, batch * beams, vocab, ld_logits, elem_size(dtype))) return invalid("logits is NULL, misaligned or its pitch too small");
+    if (!(scale > 0.f) || scale > 1e30f) return invalid("scale must be positive and finite");
+    if (!array_ok(scores, batch, 4)) return invalid("scores is NULL or misaligned");
+    if (end >= vocab) return invalid("end is no token");
+    if (finished && end < 0) return invalid("finished beams need a token to continue with");
+    if (!array_ok(out_scores, batch, 4) || !array_ok(out_beams, batch, 8) || !array_ok(out_tokens, batch, 8))
+        return invalid("out_scores, out_beams or out_tokens is NULL or misaligned");
+    const BeamArgs a = {logits, ld_logits, batch, vocab, end < 0 ? -1 : end, dtype, static_cast<int>(beams), keep, scores, finished, scale,
+                        out_scores, out_beams, out_tokens, out_finished};
+    return cuda_status(launch_beam_select(a, stream_of(stream)));
+} catch (...) {
+    return kNoMemory;
+}
+
+int isoloco_beam_reorder(const isoloco_state_t* states, int count, int64_t batch, int64_t width, const void* beams,
+                         int id_bytes, void* stream) try {
+    if (width < 1 || width > ISOLOCO_MAX_BEAMS) return invalid("width must be in 1 .. 32");
+    if (!size_ok(batch, 0) || !size_ok(batch * width, 0)) return invalid("batch * width must be in 0 .. 2^31 - 1");
+    if (id_bytes != 4 && id_bytes != 8) return invalid("id_bytes must be 4 or 8");
+    if (const char* p = states_problem(states, count, batch, width)) return invalid(p);
+    if (!array_ok(beams, batch, id_bytes)) return invalid("beams is NULL or misaligned");
+    return cuda_status(launch_beam_reorder(states, count, batch, static_cast<int>(width), beams, id_bytes == 8, stream_of(stream)));
 } catch (...) {
     return kNoMemory;
 }

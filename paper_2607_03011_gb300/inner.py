@@ -2,7 +2,9 @@
 
 Between two outer steps a worker looks tokens up in its embedding (`embed`), runs gated feed-forward
 blocks (`gated_ffn`), scores the next tokens from the head's logits (`token_logprobs`) and clips the
-global norm of its gradient (`clip_grads`); the `*_grad` functions are the backward passes.
+global norm of its gradient (`clip_grads`); the `*_grad` functions are the backward passes.  A merged model also
+teaches: from its top tokens, as `token_logprobs` gives them, another learns (`distill`).  And it answers: by a search over
+beams (`beam_select`, `beam_reorder`).
 
 Argument marshalling only, as in `isoloco`: tensors are torch CUDA tensors on the current device, in
 fp32, bf16 or fp16 (the gated block: bf16 or fp16), whose last dimension is contiguous; other strides
@@ -13,7 +15,7 @@ IsolocoError (what the library refuses) before anything is launched.
 
 Nothing here is recorded by autograd, as nothing in `isoloco` is: tensors that require a gradient are taken as they
 are, outputs never require one, and a loss.backward() through them reaches no operand.  Gradients come from the
-`*_grad` functions (and grad_logits of `token_logprobs`) alone, called by the training step itself as `inner_demo`
+`*_grad` functions (and grad_logits of `token_logprobs` and `distill`) alone, called by the training step itself as `inner_demo`
 does, or by a torch.autograd.Function around them.
 """
 from __future__ import annotations
@@ -30,7 +32,10 @@ _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _HALF = {torch.bfloat16: 1, torch.float16: 2}
 _ACT = {"silu": 0, "gelu_tanh": 1}
 _INT = {torch.int32: 4, torch.int64: 8}
+_TAIL = {"drop": 0, "rest": 1}
 MAX_TOP = 32
+MAX_LIST = 256
+MAX_BEAMS = 32
 
 # The smallest of these calls take a few microseconds on the GPU, so the way there is kept short: the
 # current stream's handle and the device's number without objects made for them, where torch has these names.
@@ -281,6 +286,195 @@ def token_logprobs_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.
     if rc:
         _check(rc, "isoloco_token_logprobs_grad")
     return gz
+
+
+class Distilled(NamedTuple):
+    loss: torch.Tensor                     # fp32, one per row
+    saved: Optional[torch.Tensor]          # fp32, rows x 2: what distill_grad needs besides the operands
+    grad_logits: Optional[torch.Tensor]    # as of TokenLogprobs
+
+
+def _distill_operands(logits, top_logp, top_index, tail):
+    z, n, vocab, ld = _rows(logits, "logits")
+    v, rows, k, ldv = _rows(top_logp, "top_logp")
+    i, rows_i, k_i, ldi = _rows(top_index, "top_index", _INT)
+    if rows != n or rows_i != n or k != k_i:
+        raise ValueError(f"top_logp, top_index: {n} rows of one length expected")
+    if k > MAX_LIST:
+        raise ValueError(f"top_logp: at most {MAX_LIST} columns")
+    if tail not in _TAIL:
+        raise ValueError(f"tail: one of {sorted(_TAIL)}")
+    return z, n, vocab, ld, (v.data_ptr(), ldv, _DTYPE[v.dtype], i.data_ptr(), ldi, _INT[i.dtype], k)
+
+
+def distill(logits: torch.Tensor, top_logp: torch.Tensor, top_index: torch.Tensor, scale: float = 1.0, tail: str = "drop",
+            grad_loss: Optional[torch.Tensor] = None, save: bool = False, stream=None) -> Distilled:
+    """Each row's divergence KL(q || softmax(scale * logits)) from a teacher that is given by k tokens (top_index,
+    int32 or int64; an index that is no token is no entry) and its log probabilities for them (top_logp), as
+    token_logprobs(teacher_logits, ..., scale, top=k) returns them.  tail="drop" renormalises the teacher over the row's list;
+    tail="rest" adds one outcome, any other token, with what the list leaves of the teacher's probability.  Entries of
+    one token add up, so a target that is mixed in is one more entry with the logarithm of its weight.
+    With grad_loss (the gradient by each row's loss, known in advance) the same call returns the gradient by the logits; with
+    save=True what distill_grad needs."""
+    if stream is not None:
+        return _on(stream, distill, logits, top_logp, top_index, scale, tail, grad_loss, save)
+    z, n, vocab, ld, lists = _distill_operands(logits, top_logp, top_index, tail)
+    g = _per_row(grad_loss, n, "grad_loss")
+    dev, shape = z.device, logits.shape
+    loss = _empty(shape[:-1], dtype=torch.float32, device=dev)
+    saved = _empty((n, 2), dtype=torch.float32, device=dev) if save else None
+    gz, ldg = _like_rows(z, shape, vocab, ld, dev) if g is not None else (None, ld)
+    rc = lib().isoloco_distill(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, *lists, scale, _TAIL[tail], loss.data_ptr(),
+                               _ptr(saved), g, _ptr(gz), ldg, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "isoloco_distill")
+    return Distilled(loss, saved, gz)
+
+
+def distill_grad(grad_loss: torch.Tensor, logits: torch.Tensor, top_logp: torch.Tensor, top_index: torch.Tensor,
+                 saved: torch.Tensor, scale: float = 1.0, tail: str = "drop", stream=None) -> torch.Tensor:
+    """The gradient by the logits alone, for grad_loss = d loss / d distill(...).loss and what the call saved."""
+    if stream is not None:
+        return _on(stream, distill_grad, grad_loss, logits, top_logp, top_index, saved, scale, tail)
+    z, n, vocab, ld, lists = _distill_operands(logits, top_logp, top_index, tail)
+    if grad_loss is None or saved is None:
+        raise ValueError("grad_loss, saved: needed")
+    g, kept = _per_row(grad_loss, n, "grad_loss"), _per_row(saved, 2 * n, "saved")
+    dev = z.device
+    gz, ldg = _like_rows(z, logits.shape, vocab, ld, dev)
+    rc = lib().isoloco_distill_grad(g, z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, *lists, scale, _TAIL[tail], kept,
+                                    gz.data_ptr(), ldg, _raw_stream(dev.index))
+    if rc:
+        _check(rc, "isoloco_distill_grad")
+    return gz
+
+
+class BeamSelection(NamedTuple):
+    scores: torch.Tensor                   # fp32, ... x keep, largest first
+    beams: torch.Tensor                    # int64: the beam that each continues
+    tokens: torch.Tensor                   # int64: with this token
+    finished: Optional[torch.Tensor]       # bool: its beam was finished, or the token is `end` (None without `end`)
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, keep: Optional[int] = None,
+                finished: Optional[torch.Tensor] = None, end: Optional[int] = None, scale: float = 1.0,
+                stream=None) -> BeamSelection:
+    """The `keep` (default: as many as beams) largest of scores[..., w] + log softmax(scale * logits[..., w, :])[t] over
+    the beams w and tokens t of each batch entry; logits are ... x beams x vocab, scores fp32 ... x beams.  Ties: the lower
+    beam, then the larger logit, then the lower token.  Beams where `finished` (bool) is set go on with the token `end` alone, at their own
+    score.  A first step starts from one beam: scores of -inf for the others."""
+    if stream is not None:
+        return _on(stream, beam_select, logits, scores, keep, finished, end, scale)
+    if logits.dim() < 2:
+        raise ValueError("logits: ... x beams x vocab expected")
+    lead, beams, dev = logits.shape[:-2], logits.shape[-2], logits.device
+    z, n, vocab, ld = _rows(logits, "logits")
+    if not 1 <= beams <= MAX_BEAMS:
+        raise ValueError(f"logits: 1 .. {MAX_BEAMS} beams")
+    keep = beams if keep is None else keep
+    if not 1 <= keep <= min(beams * vocab, MAX_TOP):
+        raise ValueError(f"keep: 1 .. {min(beams * vocab, MAX_TOP)}")
+    if scores.shape != logits.shape[:-1]:
+        raise ValueError("scores: one per row of logits expected")
+    ps, pf = _per_row(scores, n, "scores"), None
+    if finished is not None:
+        if finished.dtype != torch.bool or finished.shape != scores.shape or not finished.is_contiguous() or \
+                finished.get_device() != _current_device():
+            raise ValueError("finished: contiguous bools on the current CUDA device expected, one per score")
+        pf = finished.data_ptr()
+        if end is None:
+            raise ValueError("finished: needs the token `end`")
+    if end is not None and not 0 <= end < vocab:
+        raise ValueError(f"end: 0 .. {vocab - 1}")
+    shape = (*lead, keep)
+    s = _empty(shape, dtype=torch.float32, device=dev)
+    b = _empty(shape, dtype=torch.int64, device=dev)
+    t = _empty(shape, dtype=torch.int64, device=dev)
+    f = None if end is None else _empty(shape, dtype=torch.bool, device=dev)
+    rc = lib().isoloco_beam_select(z.data_ptr(), ld, _DTYPE[z.dtype], n // beams, beams, vocab, ps, pf,
+                                   -1 if end is None else end, scale, keep, s.data_ptr(), b.data_ptr(), t.data_ptr(),
+                                   _ptr(f), _raw_stream(dev.index))
+    if rc:
+        _check(rc, "isoloco_beam_select")
+    return BeamSelection(s, b, t, f)
+
+
+def _fold_state(shape, step, size: int, batch: int, width: int, two: bool, what: str, any_order: bool):
+    """(strides in bytes of batch, beam and piece, pieces, bytes of a piece) of a state."""
+    if two and len(shape) > 1 and shape[0] == batch and shape[1] == width:
+        s_batch, s_beam, at = step[0], step[1], 2
+    elif len(shape) > 0 and shape[0] == batch * width:
+        s_batch, s_beam, at = width * step[0], step[0], 1
+    else:
+        raise ValueError(f"{what}: states of {batch} x {width} (or {batch * width}) beams expected")
+    if 0 in shape:
+        return 0, 0, 0, 0, 0
+    run, outer, s_outer = 1, 1, 0
+    dims = list(zip(step[at:], shape[at:]))[::-1]
+    for s, n in sorted(dims) if any_order else dims:
+        if n == 1:
+            continue
+        if outer == 1 and s == run:
+            run *= n
+        elif outer == 1:
+            outer, s_outer = n, s
+        elif s == outer * s_outer:
+            outer *= n
+        else:
+            raise ValueError(f"{what}: a state's dimensions behind the beams' do not fold into pieces of one pitch")
+    return s_batch * size, s_beam * size, s_outer * size, outer, run * size
+
+
+def _fold_pair(s, d, size: int, batch: int, width: int, two: bool):
+    """The strides of a state and of its result, and the pieces of both."""
+    same = s == d  # (the order of the dimensions is then free)
+    sb, sw, so, n, run = _fold_state(*s, size, batch, width, two, "states", same)
+    if same:
+        return sb, sw, so, sb, sw, so, n, run
+    db, dw, do, nd, rund = _fold_state(*d, size, batch, width, two, "out", False)
+    if run != rund:
+        # one of the two is in one piece where the other is in several: both in the shorter pieces
+        short = min(run, rund)
+        if (n > 1 and run != short) or (nd > 1 and rund != short):
+            raise ValueError("out: the pieces of a state and of its result do not match")
+        so, do = (so if run == short else short), (do if rund == short else short)
+        n, run = n * run // short, short
+    return sb, sw, so, db, dw, do, n, run
+
+
+def beam_reorder(states: Iterable[torch.Tensor], beams: torch.Tensor, out: Optional[Iterable[torch.Tensor]] = None,
+                 stream=None) -> List[torch.Tensor]:
+    """state[b, w] = state[b, beams[b, w]] for what is kept for beams (caches, histories of tokens; any types), in place or
+    into `out`; returns the list of results.  beams: batch x width (or width) of int32 or int64, an entry outside [0, width) stands for
+    the beam itself.  States are batch x width x ... or (batch * width) x ...; the used part of a longer cache is given as a slice (of which the
+    rest stays as it is).  Results may not share memory with one another or with states that they are not made in place of."""
+    states, out = list(states), None if out is None else list(out)
+    if stream is not None:
+        return _on(stream, beam_reorder, states, beams, out)
+    size = _tokens(beams, "beams")
+    if beams.dim() not in (1, 2):
+        raise ValueError("beams: batch x width (or width) entries expected")
+    batch, width = (1, beams.shape[0]) if beams.dim() == 1 else beams.shape
+    if not 1 <= width <= MAX_BEAMS:
+        raise ValueError(f"beams: 1 .. {MAX_BEAMS} of a batch entry")
+    if out is not None and len(out) != len(states):
+        raise ValueError("out: one tensor per state")
+    to, dev, two = states if out is None else out, _current_device(), beams.dim() == 2
+    if set(map(_get_device, states)) - {dev} or set(map(_get_device, to)) - {dev}:
+        raise ValueError("states, out: tensors on the current CUDA device are needed")
+    words, folds = array.array("q"), {}
+    for s, d in zip(states, to):
+        kind = (s.dtype, s.shape, s.stride(), d.dtype, d.shape, d.stride())
+        fold = folds.get(kind)
+        if fold is None:  # (a call's states are mostly alike)
+            if kind[0] != kind[3] or kind[1] != kind[4]:
+                raise ValueError("out: tensors of the states' shapes and types expected")
+            fold = folds[kind] = _fold_pair(kind[1:3], kind[4:6], s.element_size(), batch, width, two)
+        words.extend((s.data_ptr(), d.data_ptr()) + fold)
+    rc = lib().isoloco_beam_reorder(words.buffer_info()[0], len(states), batch, width, beams.data_ptr(), size, _raw_stream(dev))
+    if rc:
+        _check(rc, "isoloco_beam_reorder")
+    return to
 
 
 def _tensor_list(tensors: List[torch.Tensor], what: str):

@@ -47,6 +47,11 @@ class Tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
+class State(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p)] + \
+        [(n, ctypes.c_int64) for n in ("src_batch", "src_beam", "src_outer", "dst_batch", "dst_beam", "dst_outer", "outer", "run")]
+
+
 class Opts(ctypes.Structure):
     _fields_ = [("alpha", ctypes.c_float), ("outer_lr", ctypes.c_float), ("momentum", ctypes.c_float),
                 ("reduce_mean", ctypes.c_int), ("max_iter", ctypes.c_int), ("tol", ctypes.c_float),
@@ -107,6 +112,12 @@ def lib():
                                                  _vp, _vp, i64, _vp]
             L.isoloco_token_logprobs_grad.argtypes = [_vp, i64, ci, i64, i64, _vp, ci, cf, _vp, _vp, _vp, _vp, _vp, i64,
                                                       _vp]
+            L.isoloco_distill.argtypes = [_vp, i64, ci, i64, i64, _vp, i64, ci, _vp, i64, ci, ci, cf, ci, _vp, _vp, _vp, _vp,
+                                          i64, _vp]
+            L.isoloco_distill_grad.argtypes = [_vp, _vp, i64, ci, i64, i64, _vp, i64, ci, _vp, i64, ci, ci, cf, ci, _vp, _vp,
+                                               i64, _vp]
+            L.isoloco_beam_select.argtypes = [_vp, i64, ci, i64, i64, i64, _vp, _vp, i64, cf, ci, _vp, _vp, _vp, _vp, _vp]
+            L.isoloco_beam_reorder.argtypes = [_vp, ci, i64, i64, _vp, ci, _vp]
             L.isoloco_grad_norm.argtypes = [_vp, ci, _vp, _vp, i64, _vp]
             L.isoloco_clip_grads.argtypes = [_vp, _vp, ci, cf, _vp, _vp, i64, _vp]
             L.isoloco_inner_status.argtypes = [_vp]
