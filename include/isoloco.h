@@ -459,7 +459,7 @@ int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_d
  * loss is +inf where an entry of weight above 0 is masked, and its gradient finite; in a row that is masked altogether the gradient is 0.
  * A NaN or +inf among a row's logits or top_logp makes its loss and gradient NaN.
  *   logits: rows x vocab of `dtype`; top_logp: rows x k of logp_dtype; top_index: rows x k of index_bytes (4 or 8), signed;
- *   1 <= k <= ISOLOCO_MAX_LIST; loss: rows fp32; saved (may be NULL): rows x 2 fp32, for isoloco_distill_grad;
+ *   1 <= k <= ISOLOCO_MAX_LIST; loss: rows fp32; saved (may be NULL): rows x 6 fp32, for isoloco_distill_grad;
  *   scale > 0.
  * With grad_logits (rows x vocab of `dtype`, pitch ld_grad; may be the logits themselves, else NULL) the call also writes
  * the gradient of sum_r grad_loss[r] loss[r] (grad_loss: rows fp32). */

@@ -29,15 +29,12 @@
 #include "common.cuh"
 #include "inner.cuh"
 #include "inner.h"
+#include "rows.cuh"
 
 namespace isoloco {
 
 namespace {
 
-constexpr float kLowest = -1000.f;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kGroups = 64;         // of threads, at least 2 ISOLOCO_MAX_TOP
-constexpr int kCandidates = 1024;   // entries a CTA ranks: all that a row of equal logits gives, 32 per group and `top`
 constexpr int kMaxSplit = 8;
 // A row's share of a CTA with gradient: 760 of them at once are 73 MB (4096 x 128000 fp32: 721 us in shares of 64 KB,
 // 957 in shares of 128, 1029 in whole rows).
@@ -49,43 +46,6 @@ constexpr int kUnroll = 4;
 constexpr int threads_per_sm(bool top) { return top ? 1152 : 1280; }
 constexpr int ctas_per_sm(int threads, bool top) { return threads_per_sm(top) / threads > 32 ? 32 : threads_per_sm(top) / threads; }
 
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-// max(d, kLowest); NaN stays
-__device__ __forceinline__ float cut(float d) {
-    float y;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(d), "f"(kLowest));
-    return y;
-}
-
-// Two fp32 operations per instruction (sm_100's packed forms; each rounds as its scalar form does).
-struct F2 {
-    unsigned long long v;
-};
-__device__ __forceinline__ F2 pair(float a, float b) {
-    F2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void unpair(F2 a, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a.v)); }
-__device__ __forceinline__ F2 add2(F2 a, F2 b) {
-    F2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-    F2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-    F2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
 // d of two logits, from -M and c
 __device__ __forceinline__ F2 exponents(float x0, float x1, F2 minus_m, F2 c2, float& d0, float& d1) {
     unpair(mul2(add2(pair(x0, x1), minus_m), c2), d0, d1);
@@ -130,54 +90,6 @@ struct Stat2 {
     }
 };
 
-// Largest entries of vectors: pairs of 16-bit entries (or four fp32 ones) are compared at once.
-template <class T>
-struct Largest {
-    uint32_t w[4];
-    __device__ __forceinline__ void set(const Vec<T>& v) { w[0] = v.raw.x, w[1] = v.raw.y, w[2] = v.raw.z, w[3] = v.raw.w; }
-    static __device__ __forceinline__ uint32_t more(uint32_t a, uint32_t b) {
-        if constexpr (sizeof(T) == 4) {
-            return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
-        } else if constexpr (__is_same(T, __half)) {
-            const __half2 h = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-            return *reinterpret_cast<const uint32_t*>(&h);
-        } else {
-            const __nv_bfloat162 h = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
-            return *reinterpret_cast<const uint32_t*>(&h);
-        }
-    }
-    __device__ __forceinline__ void take(const Largest& o) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = more(w[i], o.w[i]);
-    }
-    __device__ __forceinline__ float value() const {
-        const uint32_t m = more(more(w[0], w[1]), more(w[2], w[3]));
-        if constexpr (sizeof(T) == 4) return __uint_as_float(m);
-        else if constexpr (__is_same(T, __half)) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&m));
-            return fmaxf(f.x, f.y);
-        } else {
-            return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
-        }
-    }
-};
-
-// Order of (value, index): greater values first, then lower indices; -0 and 0 are equal.
-__device__ __forceinline__ uint64_t rank_key(float v, uint32_t idx) {
-    const uint32_t u = __float_as_uint(v + 0.f);
-    const uint32_t o = (u & 0x80000000u) ? ~u : u | 0x80000000u;
-    return (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~idx);
-}
-
-struct TopSmem {
-    uint64_t group[kGroups];
-    uint64_t bound;
-    int count, threads;
-    uint16_t thread[256];  // those whose entries may reach the bound
-    uint64_t cand[kCandidates];
-    uint64_t best[kMaxSplit][ISOLOCO_MAX_TOP];  // of every CTA of the cluster (read in the first)
-};
-
 // A CTA's share of a row: entries before the first 16-byte boundary, vectors, entries behind.
 template <class T>
 struct Share {
@@ -197,6 +109,7 @@ struct Share {
     }
     __device__ __forceinline__ uint32_t tail() const { return head + nvec * V; }
     __device__ __forceinline__ const uint4* vec(uint32_t i) const { return reinterpret_cast<const uint4*>(x + head) + i; }
+    __device__ __forceinline__ uint4 load(uint32_t i) const { return *vec(i); }
 };
 
 // Sums over W lanes (every lane gets them): first the common maximum, then one rescaling.
@@ -224,114 +137,12 @@ __device__ __forceinline__ void merge_cta(Stat& st, float c, Stat* sm) {
     merge_lanes<W>(st, c);
 }
 
-// The CTA's k largest entries, in order, to best[0 .. k) (keys; 0 where there are fewer).  bv, bi: this
-// thread's largest value and an index not below its first place.
-template <class T, int THREADS>
-__device__ __forceinline__ void top_of_cta(TopSmem& sm, const Share<T>& sh, int k, float bv, uint32_t bi, float second, uint64_t* best) {
-    constexpr int kPer = THREADS / kGroups, V = Vec<T>::kN;
-    // keys not above and not below that of the thread's largest entry, which lies within a vector of bi
-    const bool any = bi != 0xffffffffu;
-    const uint64_t least = any ? rank_key(bv, sh.first + bi) : 0, most = any ? rank_key(bv, sh.first + (bi >= V - 1 ? bi - (V - 1) : 0)) : 0;
-    uint64_t g = least;
-#pragma unroll
-    for (int o = 1; o < kPer; o <<= 1) {
-        const uint64_t other = __shfl_xor_sync(0xffffffffu, g, o);
-        g = other > g ? other : g;
-    }
-    if (threadIdx.x % kPer == 0) sm.group[threadIdx.x / kPer] = g;
-    if (threadIdx.x == 0) sm.count = sm.threads = 0;
-    if (threadIdx.x < k) best[threadIdx.x] = 0;
-    __syncthreads();
-    {
-        // ranks of the groups: kPer threads each count a share of the greater ones
-        const int own_at = threadIdx.x / kPer, sub = threadIdx.x % kPer;
-        const uint64_t own = sm.group[own_at];
-        int r = 0;
-#pragma unroll
-        for (int j = 0; j < kGroups / kPer; ++j) {
-            const uint64_t v = sm.group[j * kPer + sub];
-            r += (v > own || (v == own && j * kPer + sub < own_at)) ? 1 : 0;  // (equal keys: groups without entries)
-        }
-#pragma unroll
-        for (int o = 1; o < kPer; o <<= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
-        if (r == k - 1) sm.bound = own;
-    }
-    __syncthreads();
-    const uint64_t bound = sm.bound;
-    auto look = [&](float v, uint32_t i) {
-        if (v != v) return;  // NaN ranks nowhere
-        const uint64_t key = rank_key(v, sh.first + i);
-        if (key >= bound) {
-            const int at = atomicAdd(&sm.count, 1);
-            if (at < kCandidates) sm.cand[at] = key;
-        }
-    };
-    auto look_at = [&](uint32_t i) {
-        Vec<T> v;
-        v.raw = *sh.vec(i);
-        float f[V];
-        v.unpack(f);
-#pragma unroll
-        for (int j = 0; j < V; ++j) look(f[j], sh.head + i * V + j);
-    };
-    static_assert(THREADS <= 256, "TopSmem::thread");
-    if (any && most >= bound) {
-        // the vector with the thread's largest entry, or, where another of its vectors may reach the bound, all of them
-        if (rank_key(second, 0) >= bound) sm.thread[atomicAdd(&sm.threads, 1)] = static_cast<uint16_t>(threadIdx.x);
-        else if (bi >= sh.head && bi < sh.tail()) look_at((bi - sh.head) / V);
-    }
-    __syncthreads();
-    // those threads' vectors, dealt to all
-    const uint32_t found = sm.threads, each = (sh.nvec + THREADS - 1) / THREADS;
-    for (uint32_t e = threadIdx.x; e < found * each; e += THREADS) {
-        const uint32_t i = sm.thread[e / each] + (e % each) * THREADS;
-        if (i < sh.nvec) look_at(i);
-    }
-    if (threadIdx.x < sh.head) look(to_f32(sh.x[threadIdx.x]), threadIdx.x);
-    if (threadIdx.x < sh.n - sh.tail()) look(to_f32(sh.x[sh.tail() + threadIdx.x]), sh.tail() + threadIdx.x);
-    __syncthreads();
-    const int n = sm.count;
-    if (n <= kCandidates) {
-        for (int i = threadIdx.x; i < n; i += THREADS) {
-            const uint64_t own = sm.cand[i];
-            int r = 0;
-            for (int j = 0; j < n; ++j) r += sm.cand[j] > own ? 1 : 0;
-            if (r < k) best[r] = own;
-        }
-    } else {
-        // more entries above the bound than fit (most of the row's largest lie in few threads' shares):
-        // one at a time, the largest below the one before
-        uint64_t below = ~uint64_t(0);
-        for (int q = 0; q < k; ++q) {
-            uint64_t b = 0;
-            for (uint32_t i = threadIdx.x; i < sh.n; i += THREADS) {
-                const float v = to_f32(sh.x[i]);
-                const uint64_t key = v == v ? rank_key(v, sh.first + i) : 0;
-                if (key < below && key > b) b = key;
-            }
-#pragma unroll
-            for (int o = 16; o; o >>= 1) {
-                const uint64_t other = __shfl_xor_sync(0xffffffffu, b, o);
-                b = other > b ? other : b;
-            }
-            __syncthreads();
-            if ((threadIdx.x & 31) == 0) sm.group[threadIdx.x >> 5] = b;
-            __syncthreads();
-            b = 0;
-            for (int i = 0; i < THREADS / 32; ++i) b = sm.group[i] > b ? sm.group[i] : b;
-            if (threadIdx.x == 0) best[q] = b;
-            below = b;
-        }
-    }
-    __syncthreads();
-}
-
 template <class T, class I, int THREADS, bool TOP, bool GRAD>
 __global__ void __launch_bounds__(THREADS, ctas_per_sm(THREADS, TOP)) k_logprobs(LogprobArgs a, uint32_t split) {
     constexpr int V = Vec<T>::kN;
     __shared__ Stat sm[THREADS / 32];
     __shared__ Stat peer[kMaxSplit];  // the sums of every CTA of the cluster
-    __shared__ typename std::conditional<TOP, TopSmem, int>::type top_sm;
+    __shared__ typename std::conditional<TOP, TopSmem<kMaxSplit>, int>::type top_sm;  // (the best of every CTA of the cluster)
     const uint32_t rank = split > 1 ? cluster_ctarank() : 0u;
     const float c = a.scale * kLog2e;
     const uint32_t vocab = static_cast<uint32_t>(a.vocab);

@@ -290,7 +290,7 @@ def token_logprobs_grad(logits: torch.Tensor, targets: torch.Tensor, lse: torch.
 
 class Distilled(NamedTuple):
     loss: torch.Tensor                     # fp32, one per row
-    saved: Optional[torch.Tensor]          # fp32, rows x 2: what distill_grad needs besides the operands
+    saved: Optional[torch.Tensor]          # fp32, rows x 6: what distill_grad needs besides the operands
     grad_logits: Optional[torch.Tensor]    # as of TokenLogprobs
 
 
@@ -322,7 +322,7 @@ def distill(logits: torch.Tensor, top_logp: torch.Tensor, top_index: torch.Tenso
     g = _per_row(grad_loss, n, "grad_loss")
     dev, shape = z.device, logits.shape
     loss = _empty(shape[:-1], dtype=torch.float32, device=dev)
-    saved = _empty((n, 2), dtype=torch.float32, device=dev) if save else None
+    saved = _empty((n, 6), dtype=torch.float32, device=dev) if save else None
     gz, ldg = _like_rows(z, shape, vocab, ld, dev) if g is not None else (None, ld)
     rc = lib().isoloco_distill(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, *lists, scale, _TAIL[tail], loss.data_ptr(),
                                _ptr(saved), g, _ptr(gz), ldg, _raw_stream(dev.index))
@@ -339,7 +339,7 @@ def distill_grad(grad_loss: torch.Tensor, logits: torch.Tensor, top_logp: torch.
     z, n, vocab, ld, lists = _distill_operands(logits, top_logp, top_index, tail)
     if grad_loss is None or saved is None:
         raise ValueError("grad_loss, saved: needed")
-    g, kept = _per_row(grad_loss, n, "grad_loss"), _per_row(saved, 2 * n, "saved")
+    g, kept = _per_row(grad_loss, n, "grad_loss"), _per_row(saved, 6 * n, "saved")
     dev = z.device
     gz, ldg = _like_rows(z, logits.shape, vocab, ld, dev)
     rc = lib().isoloco_distill_grad(g, z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, *lists, scale, _TAIL[tail], kept,
