@@ -96,7 +96,7 @@ struct TopSmem {
     uint64_t group[kGroups];
     uint64_t bound;
     int count, threads;
-    uint16_t thread[256];  // those whose entries may reach the bound
+    uint16_t thread[512];  // those whose entries may reach the bound
     uint64_t cand[kCandidates];
     uint64_t best[LISTS][ISOLOCO_MAX_TOP];
 };
@@ -151,7 +151,7 @@ __device__ __forceinline__ void top_of_cta(Smem& sm, const Share& sh, int k, flo
 #pragma unroll
         for (int j = 0; j < V; ++j) look(f[j], sh.head + i * V + j);
     };
-    static_assert(THREADS <= 256, "TopSmem::thread");
+    static_assert(THREADS <= 512, "TopSmem::thread");
     if (any && most >= bound) {
         // the vector with the thread's largest entry, or, where another of its vectors may reach the bound, all of them
         if (rank_key(second, 0) >= bound) sm.thread[atomicAdd(&sm.threads, 1)] = static_cast<uint16_t>(threadIdx.x);

@@ -21,15 +21,21 @@ def make(b, w, vocab, dtype, seed=0):
 def check(z, scores, keep, finished=None, end=None, scale=1.0, apart=True):
     from paper_2607_03011_gb300 import inner
     total, beams, tokens = ref.select(z, scores, min(keep + 1, z.shape[1] * z.shape[2], 10 ** 6), finished, end, scale)
+    sure = torch.ones(z.shape[0], dtype=torch.bool)
     if apart and total.shape[1] > 1:
-        # totals of different beams that are compared are further apart than sums of powers are good to
+        # totals of different beams that are nearer to each other than sums of powers are good to may come in either order
         gap, other = (total[:, :-1] - total[:, 1:]), beams[:, :-1] != beams[:, 1:]
-        near = other & torch.isfinite(total[:, 1:]) & (gap < 8 * ref.sum_of_powers(z.shape[2]))
-        assert not near.any(), "inputs too close"
+        sure = ~(other & torch.isfinite(total[:, 1:]) & (gap < 8 * ref.sum_of_powers(z.shape[2]))).any(1)
+        assert sure.double().mean() > 0.9
     total, beams, tokens = total[:, :keep], beams[:, :keep], tokens[:, :keep]
     r = inner.beam_select(z.cuda(), scores.cuda(), keep=keep, finished=None if finished is None else finished.cuda(), end=end, scale=scale)
-    assert torch.equal(r.beams.cpu(), beams), (r.beams.cpu() - beams).nonzero()[:5]
-    assert torch.equal(r.tokens.cpu(), tokens), (r.tokens.cpu() - tokens).nonzero()[:5]
+    assert torch.equal(r.beams.cpu()[sure], beams[sure]), (r.beams.cpu() - beams)[sure].nonzero()[:5]
+    assert torch.equal(r.tokens.cpu()[sure], tokens[sure]), (r.tokens.cpu() - tokens)[sure].nonzero()[:5]
+    for i in torch.nonzero(~sure).flatten().tolist():
+        chosen = z[i].double().log_softmax(1)[r.beams[i].cpu(), r.tokens[i].cpu()] if scale == 1.0 and finished is None else None
+        assert chosen is not None and len(set(zip(r.beams[i].tolist(), r.tokens[i].tolist()))) == keep
+        assert ((scores[i].double()[r.beams[i].cpu()] + chosen - total[i]).abs() < 8 * ref.sum_of_powers(z.shape[2])).all()
+        beams[i], tokens[i] = r.beams[i].cpu(), r.tokens[i].cpu()
     got = r.scores.cpu().double()
     assert torch.equal(torch.isnan(got), torch.isnan(total)) and torch.equal(got == -INF, total == -INF)
     fine = torch.isfinite(total)
@@ -128,6 +134,23 @@ def test_nan_and_infinities():
     z[7, 2, 299] = math.nan
     check(z, scores, 9)
     check(z[5:6, :1, :20], scores[5:6, :1], 20)
+
+
+def test_special_rows_in_many_batch_entries():
+    """Finished, dead and masked beams, NaN and ties, among so many rows that the merging is a launch of its own."""
+    z, scores = make(8, 5, 120, F32, seed=9)
+    fin = torch.zeros(8, 5, dtype=torch.bool)
+    fin[0], fin[1, ::2], fin[7, 1] = True, True, True
+    z[2, 1], z[3, 0, 5], z[4, 3, 7] = -INF, math.nan, INF
+    z[5, :, 2:] = ref.LOWEST[F32]
+    scores[6, 2:], scores[7, 0], scores[7, 4] = -INF, math.nan, INF
+    z[6, 0] = 0.25
+    check(z.repeat(30, 1, 1), scores.repeat(30, 1), 10, fin.repeat(30, 1), 3)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_shares_of_rows_in_many_batch_entries(dtype):
+    check(*make(40, 8, 90001, dtype, seed=10), 6)
 
 
 def test_pitch_and_leading_dimensions():
