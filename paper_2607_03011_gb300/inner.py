@@ -44,6 +44,7 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 _empty = torch.empty
 _data_ptr, _numel = torch.Tensor.data_ptr, torch.Tensor.numel
 _is_contiguous, _get_device = torch.Tensor.is_contiguous, torch.Tensor.get_device
+_stride = torch.Tensor.stride
 
 
 def _on(stream, f, *args):
@@ -302,9 +303,10 @@ def _distill_operands(logits, top_logp, top_index, tail):
         raise ValueError(f"top_logp, top_index: {n} rows of one length expected")
     if k > MAX_LIST:
         raise ValueError(f"top_logp: at most {MAX_LIST} columns")
-    if tail not in _TAIL:
+    code = _TAIL.get(tail)
+    if code is None:
         raise ValueError(f"tail: one of {sorted(_TAIL)}")
-    return z, n, vocab, ld, (v.data_ptr(), ldv, _DTYPE[v.dtype], i.data_ptr(), ldi, _INT[i.dtype], k)
+    return z, n, vocab, ld, (v.data_ptr(), ldv, _DTYPE[v.dtype], i.data_ptr(), ldi, _INT[i.dtype], k), code
 
 
 def distill(logits: torch.Tensor, top_logp: torch.Tensor, top_index: torch.Tensor, scale: float = 1.0, tail: str = "drop",
@@ -318,13 +320,13 @@ def distill(logits: torch.Tensor, top_logp: torch.Tensor, top_index: torch.Tenso
     save=True what distill_grad needs."""
     if stream is not None:
         return _on(stream, distill, logits, top_logp, top_index, scale, tail, grad_loss, save)
-    z, n, vocab, ld, lists = _distill_operands(logits, top_logp, top_index, tail)
+    z, n, vocab, ld, lists, code = _distill_operands(logits, top_logp, top_index, tail)
     g = _per_row(grad_loss, n, "grad_loss")
     dev, shape = z.device, logits.shape
     loss = _empty(shape[:-1], dtype=torch.float32, device=dev)
     saved = _empty((n, 6), dtype=torch.float32, device=dev) if save else None
     gz, ldg = _like_rows(z, shape, vocab, ld, dev) if g is not None else (None, ld)
-    rc = lib().isoloco_distill(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, *lists, scale, _TAIL[tail], loss.data_ptr(),
+    rc = lib().isoloco_distill(z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, *lists, scale, code, loss.data_ptr(),
                                _ptr(saved), g, _ptr(gz), ldg, _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_distill")
@@ -336,13 +338,13 @@ def distill_grad(grad_loss: torch.Tensor, logits: torch.Tensor, top_logp: torch.
     """The gradient by the logits alone, for grad_loss = d loss / d distill(...).loss and what the call saved."""
     if stream is not None:
         return _on(stream, distill_grad, grad_loss, logits, top_logp, top_index, saved, scale, tail)
-    z, n, vocab, ld, lists = _distill_operands(logits, top_logp, top_index, tail)
+    z, n, vocab, ld, lists, code = _distill_operands(logits, top_logp, top_index, tail)
     if grad_loss is None or saved is None:
         raise ValueError("grad_loss, saved: needed")
     g, kept = _per_row(grad_loss, n, "grad_loss"), _per_row(saved, 6 * n, "saved")
     dev = z.device
     gz, ldg = _like_rows(z, logits.shape, vocab, ld, dev)
-    rc = lib().isoloco_distill_grad(g, z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, *lists, scale, _TAIL[tail], kept,
+    rc = lib().isoloco_distill_grad(g, z.data_ptr(), ld, _DTYPE[z.dtype], n, vocab, *lists, scale, code, kept,
                                     gz.data_ptr(), ldg, _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_distill_grad")
@@ -410,14 +412,15 @@ def _fold_state(shape, step, size: int, batch: int, width: int, two: bool, what:
     if 0 in shape:
         return 0, 0, 0, 0, 0
     run, outer, s_outer = 1, 1, 0
-    dims = list(zip(step[at:], shape[at:]))[::-1]
+    dims = zip(step[:at - 1:-1], shape[:at - 1:-1])
     for s, n in sorted(dims) if any_order else dims:
         if n == 1:
             continue
-        if outer == 1 and s == run:
-            run *= n
-        elif outer == 1:
-            outer, s_outer = n, s
+        if outer == 1:
+            if s == run:
+                run *= n
+            else:
+                outer, s_outer = n, s
         elif s == outer * s_outer:
             outer *= n
         else:
@@ -425,13 +428,13 @@ def _fold_state(shape, step, size: int, batch: int, width: int, two: bool, what:
     return s_batch * size, s_beam * size, s_outer * size, outer, run * size
 
 
-def _fold_pair(s, d, size: int, batch: int, width: int, two: bool):
+def _fold_pair(shape, step, to_step, size: int, batch: int, width: int, two: bool):
     """The strides of a state and of its result, and the pieces of both."""
-    same = s == d  # (the order of the dimensions is then free)
-    sb, sw, so, n, run = _fold_state(*s, size, batch, width, two, "states", same)
+    same = step == to_step  # (the order of the dimensions is then free)
+    sb, sw, so, n, run = _fold_state(shape, step, size, batch, width, two, "states", same)
     if same:
         return sb, sw, so, sb, sw, so, n, run
-    db, dw, do, nd, rund = _fold_state(*d, size, batch, width, two, "out", False)
+    db, dw, do, nd, rund = _fold_state(shape, to_step, size, batch, width, two, "out", False)
     if run != rund:
         # one of the two is in one piece where the other is in several: both in the shorter pieces
         short = min(run, rund)
@@ -462,15 +465,23 @@ def beam_reorder(states: Iterable[torch.Tensor], beams: torch.Tensor, out: Optio
     to, dev, two = states if out is None else out, _current_device(), beams.dim() == 2
     if set(map(_get_device, states)) - {dev} or set(map(_get_device, to)) - {dev}:
         raise ValueError("states, out: tensors on the current CUDA device are needed")
-    words, folds = array.array("q"), {}
-    for s, d in zip(states, to):
-        kind = (s.dtype, s.shape, s.stride(), d.dtype, d.shape, d.stride())
-        fold = folds.get(kind)
-        if fold is None:  # (a call's states are mostly alike)
-            if kind[0] != kind[3] or kind[1] != kind[4]:
-                raise ValueError("out: tensors of the states' shapes and types expected")
-            fold = folds[kind] = _fold_pair(kind[1:3], kind[4:6], s.element_size(), batch, width, two)
-        words.extend((s.data_ptr(), d.data_ptr()) + fold)
+    types, shapes, steps = [t.dtype for t in states], [t.shape for t in states], list(map(_stride, states))
+    to_steps = steps
+    if out is not None:
+        to_steps = list(map(_stride, out))
+        if [t.dtype for t in out] != types or [t.shape for t in out] != shapes:
+            raise ValueError("out: tensors of the states' shapes and types expected")
+    # isoloco_state_t entries; a call's states are mostly alike, one after the other
+    words, n, i = array.array("q"), len(states), 0
+    while i < n:
+        typ, shape, step, to_step = types[i], shapes[i], steps[i], to_steps[i]
+        k = i + 1
+        while k < n and types[k] is typ and steps[k] == step and shapes[k] == shape and to_steps[k] == to_step:
+            k += 1
+        words.extend(array.array("q", (0, 0, *_fold_pair(shape, step, to_step, typ.itemsize, batch, width, two))) * (k - i))
+        i = k
+    words[0::10] = array.array("q", map(_data_ptr, states))
+    words[1::10] = array.array("q", map(_data_ptr, to))
     rc = lib().isoloco_beam_reorder(words.buffer_info()[0], len(states), batch, width, beams.data_ptr(), size, _raw_stream(dev))
     if rc:
         _check(rc, "isoloco_beam_reorder")
