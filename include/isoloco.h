@@ -446,8 +446,8 @@ int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_d
                                 void* grad_logits, int64_t ld_grad, void* stream);
 
 /* Distillation from a teacher's top logits.  Per row, k tokens and the logarithms of the teacher's probabilities for
- * them (as isoloco_token_logprobs gives its top_logp and top_index: the student's `scale` is then the teacher's too), against the student's
- * p = softmax(scale * logits):
+ * them (as isoloco_token_logprobs gives top_logp and top_index, at the scale that is the student's here), against the
+ * student's p = softmax(scale * logits):
  *   tail DROP: q = softmax(top_logp) over the row's list, r = 0;
  *   tail REST: q = exp(top_logp), and r = max(0, 1 - sum q) is one more outcome, any token outside the list, whose
  *     probability is the student's P = sum over those tokens of p.  (r counts as 0 where every such token is masked.)
@@ -455,14 +455,15 @@ int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_d
  *   gradient by the logits, with Q = sum_i q_i + r:  grad_loss scale (p_j Q - q_j) for a token of the list (q_j summed
  *     over its entries, where it has several), grad_loss scale p_j (Q - r / P) for any other.
  * An entry whose index is outside [0, vocab) is not there.  A row without entries (or, with DROP, whose entries all
- * have the weight 0) has the loss 0 and the gradient 0, whatever its logits.  Logits of -inf or the type's lowest value are masked and have probability 0: the
- * loss is +inf where an entry of weight above 0 is masked, and its gradient finite; in a row that is masked altogether the gradient is 0.
- * A NaN or +inf among a row's logits or top_logp makes its loss and gradient NaN.
- *   logits: rows x vocab of `dtype`; top_logp: rows x k of logp_dtype; top_index: rows x k of index_bytes (4 or 8), signed;
- *   1 <= k <= ISOLOCO_MAX_LIST; loss: rows fp32; saved (may be NULL): rows x 6 fp32, for isoloco_distill_grad;
- *   scale > 0.
- * With grad_logits (rows x vocab of `dtype`, pitch ld_grad; may be the logits themselves, else NULL) the call also writes
- * the gradient of sum_r grad_loss[r] loss[r] (grad_loss: rows fp32). */
+ * have the weight 0) has the loss 0 and the gradient 0, whatever its logits.
+ * Logits of -inf or the type's lowest value are masked and have probability 0 (F16's -65504 where scale is 0.002 or
+ * more).  The loss is +inf where an entry of weight above 0 is masked, and its gradient finite; in a row that is masked
+ * altogether the gradient is 0.  A NaN or +inf among a row's logits, or in an entry's top_logp, makes its loss and gradient NaN.
+ *   logits: rows x vocab of `dtype` (16-byte pieces that hold a row's ends are read whole); top_logp: rows x k of
+ *   logp_dtype; top_index: rows x k of index_bytes (4 or 8), signed; 1 <= k <= ISOLOCO_MAX_LIST; loss: rows fp32; saved (may
+ *   be NULL): rows x 6 fp32, for isoloco_distill_grad; scale > 0.
+ * With grad_logits (rows x vocab of `dtype`, pitch ld_grad; may be the logits themselves, at their pitch, else NULL) the
+ * call also writes the gradient of sum_r grad_loss[r] loss[r] (grad_loss: rows fp32). */
 #define ISOLOCO_MAX_LIST 256
 typedef enum { ISOLOCO_TAIL_DROP = 0, ISOLOCO_TAIL_REST = 1 } isoloco_tail_t;
 int isoloco_distill(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows, int64_t vocab,
@@ -479,16 +480,18 @@ int isoloco_distill_grad(const float* grad_loss, const void* logits, int64_t ld_
 /* One step of a beam search: the continuations of the largest totals among all beams of a batch entry and all tokens.
  *   total(w, t) = scores[w] + log p_t, p = softmax(scale * logits[w]); a beam that is finished (finished[w] != 0; NULL:
  *   none is) continues with the token `end` alone, at its own score, and its logits are not read.
- * The `keep` largest totals, largest first; among equal ones the lower beam, then the larger logit, then the lower token comes first.
- * Totals are compared in 64 bits before they are rounded to fp32 (log sums are good to some 1e-7).  Masked tokens (logits of -inf or the type's lowest value), a finished
- * beam's other tokens and all tokens of a beam whose score is -inf or whose tokens are all masked have the total -inf, and rank by
- * beam and token, so that there are always `keep` answers (in a beam that is not
- * finished and has unmasked tokens the type's lowest value ranks before -inf).  A beam whose score is NaN or +inf, or whose logits hold a NaN or
- * +inf while it is not finished, ranks like one of score -inf, and its totals are given as NaN.
+ * The `keep` largest totals, largest first; among equal ones the lower beam, then the larger logit, then the lower token
+ * comes first.  Totals are compared in 64 bits before they are rounded to fp32; the logarithms in them are good to some
+ * 1e-7, and are the same bits for beams with equal logits.
+ * Masked tokens (logits of -inf or the type's lowest value), a finished beam's other tokens and all tokens of a beam whose
+ * score is -inf or whose tokens are all masked have the total -inf and rank by beam and token, so that there are
+ * always `keep` answers (among the masked tokens of a beam that has others the type's lowest value ranks before -inf).  A beam whose
+ * score is NaN or +inf, or which is not finished and has a NaN or +inf among its logits, ranks like one of score -inf, and its
+ * totals are given as NaN.
  *   logits: batch * beams rows x vocab of `dtype`; scores: batch x beams fp32; finished: batch x beams bytes;
  *   1 <= beams <= ISOLOCO_MAX_BEAMS, 1 <= keep <= min(beams * vocab, ISOLOCO_MAX_TOP); `end`: a token, or negative for
- *   none (finished must then be NULL); out_scores (fp32), out_beams, out_tokens (int64): batch x keep; out_finished (may be NULL):
- *   batch x keep bytes, 1 where the beam continued was finished or the token is `end`. */
+ *   none (finished must then be NULL); out_scores (fp32), out_beams, out_tokens (int64): batch x keep; out_finished (may
+ *   be NULL): batch x keep bytes, 1 where the beam continued was finished or the token is `end`. */
 #define ISOLOCO_MAX_BEAMS 32
 int isoloco_beam_select(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t batch, int64_t beams,
                         int64_t vocab, const float* scores, const uint8_t* finished, int64_t end, float scale, int keep,

@@ -134,6 +134,7 @@ const char* distill_problem(const DistillArgs& a, int index_bytes, int tail) {
     if (a.grad_logits) {
         if (!matrix_ok(a.grad_logits, a.rows, a.vocab, a.ld_grad, elem_size(a.dtype))) return "grad_logits is misaligned or its pitch too small";
         if (!array_ok(a.grad_loss, a.rows, 4)) return "grad_loss is NULL or misaligned";
+        if (a.grad_logits == a.logits && a.rows > 1 && a.ld_grad != a.ld) return "a gradient over the logits needs their pitch";
     }
     if (!aligned_to(a.saved, 4)) return "saved is misaligned";
     return nullptr;
@@ -208,11 +209,11 @@ bool apart(const Places& a, const Places& b, uint64_t batch, uint64_t beams) {
     return true;
 }
 
-const char* states_problem(const isoloco_state_t* t, int count, int64_t batch, int64_t width) {
+const char* states_problem(const isoloco_state_t* t, int count, int64_t batch, int64_t width, const void* beams, int id_bytes) {
     constexpr int64_t kFar = int64_t(1) << 46;  // no byte of a state is further from its start
     if (count < 0 || (count > 0 && !t)) return "bad list of states";
     std::vector<Places> all;
-    all.reserve(2 * static_cast<size_t>(count));
+    all.reserve(2 * static_cast<size_t>(count) + 1);
     for (int i = 0; i < count; ++i) {
         const isoloco_state_t& s = t[i];
         if (s.outer < 0 || s.run < 0 || s.outer > kFar || s.run > kFar) return "a state's pieces and their length must not be negative";
@@ -235,13 +236,17 @@ const char* states_problem(const isoloco_state_t* t, int count, int64_t batch, i
         all.push_back(dst);
         if (!in_place) all.push_back(src);
     }
+    if (beams && batch > 0 && !all.empty()) {
+        const uint64_t id = static_cast<uint64_t>(id_bytes);
+        all.push_back({reinterpret_cast<uint64_t>(beams), id * static_cast<uint64_t>(width), id, 0, 1, id, false});
+    }
     std::sort(all.begin(), all.end(), [](const Places& a, const Places& b) { return a.at < b.at; });
     for (size_t i = 0; i < all.size(); ++i) {
         uint64_t extent;
         nested(all[i], batch, width, &extent);
         for (size_t j = i + 1; j < all.size() && all[j].at < all[i].at + extent; ++j)
             if ((all[i].written || all[j].written) && !apart(all[i], all[j], batch, width))
-                return "a state's destination shares memory with another state or its own source, or may";
+                return "a state's destination shares memory with another state, its own source or beams, or may";
     }
     return nullptr;
 }
@@ -426,7 +431,7 @@ int isoloco_beam_reorder(const isoloco_state_t* states, int count, int64_t batch
     if (width < 1 || width > ISOLOCO_MAX_BEAMS) return invalid("width must be in 1 .. 32");
     if (!size_ok(batch, 0) || !size_ok(batch * width, 0)) return invalid("batch * width must be in 0 .. 2^31 - 1");
     if (id_bytes != 4 && id_bytes != 8) return invalid("id_bytes must be 4 or 8");
-    if (const char* p = states_problem(states, count, batch, width)) return invalid(p);
+    if (const char* p = states_problem(states, count, batch, width, beams, id_bytes)) return invalid(p);
     if (!array_ok(beams, batch, id_bytes)) return invalid("beams is NULL or misaligned");
     return cuda_status(launch_beam_reorder(states, count, batch, static_cast<int>(width), beams, id_bytes == 8, stream_of(stream)));
 } catch (...) {

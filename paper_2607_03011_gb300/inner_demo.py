@@ -5,7 +5,9 @@ token is followed by a fixed other one most of the time).  A replica's inner ste
 `inner` in order: embedding, gated block, log probabilities with their gradient, the block's and the
 embedding's gradients, clipping; the plain products around them are torch's.  After `inner_steps` steps the
 replicas go through the outer step of `isoloco` (Alg. 2), and the merged model is scored on held-out text
-with `token_logprobs`: loss, entropy, and how often the next token is among the five likeliest.
+with `token_logprobs`: loss, entropy, and how often the next token is among the five likeliest.  Then the merged model
+teaches a smaller one from its likeliest tokens (`distill`), and answers prompts by a search over beams (`beam_select`,
+`beam_reorder`).
 """
 from __future__ import annotations
 
@@ -37,22 +39,58 @@ def forward(p: Dict[str, torch.Tensor], ids: torch.Tensor, save: bool):
     return y @ w["head"].t(), (w, x, h, saved, y)
 
 
-def inner_step(replica: torch.Tensor, spec, ids: torch.Tensor, targets: torch.Tensor, lr: float, max_norm: float):
-    """One clipped gradient step on the mean negative log likelihood, in place; returns (loss, norm)."""
-    p = views(replica, spec)
-    logits, (w, x, h, saved, y) = forward(p, ids, save=True)
-    n = ids.numel()
-    r = inner.token_logprobs(logits, targets, grad_logp=torch.full((n,), -1.0 / n, device=ids.device))
-    g: Dict[str, torch.Tensor] = {"head": r.grad_logits.t() @ y}
-    dy = r.grad_logits @ w["head"]
+def backward(kept, ids: torch.Tensor, grad_logits: torch.Tensor) -> Dict[str, torch.Tensor]:
+    """The parameters' gradients from the logits' and what `forward` kept."""
+    w, x, h, saved, y = kept
+    g: Dict[str, torch.Tensor] = {"head": grad_logits.t() @ y}
+    dy = grad_logits @ w["head"]
     g["w_down"] = h.t() @ dy
     dx, g["w_gate"], g["w_up"] = inner.gated_ffn_grad(dy @ w["w_down"].t(), x, w["w_gate"], w["w_up"], saved)
     g["embed"] = inner.embed_grad(dx + dy, ids, w["embed"].shape[0], dtype=torch.float32)
+    return g
+
+
+def update(p: Dict[str, torch.Tensor], spec, g: Dict[str, torch.Tensor], lr: float, max_norm: float) -> torch.Tensor:
+    """A clipped step down the gradient, in place; returns its norm."""
     grads = [g[name].contiguous() for name, _, _ in spec]
     norm = inner.clip_grads(grads, max_norm)
     for (name, _, _), d in zip(spec, grads):
         p[name].sub_(lr * d.float())
+    return norm
+
+
+def inner_step(replica: torch.Tensor, spec, ids: torch.Tensor, targets: torch.Tensor, lr: float, max_norm: float):
+    """One clipped gradient step on the mean negative log likelihood, in place; returns (loss, norm)."""
+    p = views(replica, spec)
+    logits, kept = forward(p, ids, save=True)
+    n = ids.numel()
+    r = inner.token_logprobs(logits, targets, grad_logp=torch.full((n,), -1.0 / n, device=ids.device))
+    norm = update(p, spec, backward(kept, ids, r.grad_logits), lr, max_norm)
     return -r.logp.mean(), norm
+
+
+def taught(student: torch.Tensor, spec, teacher: torch.Tensor, teacher_spec, ids: torch.Tensor, top: int = 16):
+    """(mean divergence from the teacher's `top` likeliest tokens and the rest, the student's gradients)."""
+    t = inner.token_logprobs(forward(views(teacher, teacher_spec), ids, save=False)[0], ids, top=top)
+    logits, kept = forward(views(student, spec), ids, save=True)
+    n = ids.numel()
+    r = inner.distill(logits, t.top_logp, t.top_index, tail="rest", grad_loss=torch.full((n,), 1.0 / n, device=ids.device))
+    return r.loss.mean(), backward(kept, ids, r.grad_logits)
+
+
+def answer(theta: torch.Tensor, spec, prompts: torch.Tensor, beams: int = 4, length: int = 8):
+    """(scores, tokens) of the `beams` best continuations of each prompt (its last token) by `length` tokens."""
+    p, n, dev = views(theta, spec), prompts.numel(), prompts.device
+    tokens = torch.zeros(n, beams, length + 1, dtype=torch.int64, device=dev)
+    tokens[:, :, 0] = prompts[:, None]
+    scores = torch.full((n, beams), -math.inf, device=dev)
+    scores[:, 0] = 0.0  # all beams are the prompt: one of them is continued
+    for i in range(length):
+        logits, _ = forward(p, tokens[:, :, i].contiguous().view(-1), save=False)
+        scores, came, token, _ = inner.beam_select(logits.view(n, beams, -1), scores)
+        inner.beam_reorder([tokens[:, :, :i + 1]], came)
+        tokens[:, :, i + 1] = token
+    return scores, tokens
 
 
 def evaluate(theta: torch.Tensor, spec, ids: torch.Tensor, targets: torch.Tensor):
@@ -98,6 +136,16 @@ def run(workers: int = 4, rounds: int = 4, inner_steps: int = 12, tokens: int = 
         losses.append(held[0])
         report(f"round {rnd}: last inner loss {loss.item():.3f}, gradient norm {norm.item():.2f}; merged model: held-out loss "
                f"{held[0]:.3f}, entropy {held[1]:.3f}, in the top five {100 * held[2]:.1f} %")
+    small = shapes(vocab, width // 2, ff // 2)
+    size = sum(r * c for _, r, c in small)
+    student = torch.randn(size, generator=gen, device=dev) * (0.5 / math.sqrt(width))
+    for _ in range(inner_steps):
+        divergence, g = taught(student, small, theta, spec, text(follow, tokens, gen)[0])
+        norm = update(views(student, small), small, g, lr, max_norm)
+    report(f"a student of {size} parameters: divergence {divergence.item():.3f}, gradient norm {norm.item():.2f}")
+    scores, best = answer(theta, spec, follow[:2], beams=3, length=6)
+    for s, t in zip(scores.tolist(), best.tolist()):
+        report(f"from {t[0][0]}: " + "; ".join(f"{' '.join(map(str, q[1:]))} ({v:.1f})" for q, v in zip(t, s)))
     if inner.status() != isoloco.OK:
         raise isoloco.IsolocoError(inner.status(), isoloco.last_error())
     plan.close()

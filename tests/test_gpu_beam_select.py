@@ -153,6 +153,11 @@ def test_shares_of_rows_in_many_batch_entries(dtype):
     check(*make(40, 8, 90001, dtype, seed=10), 6)
 
 
+@pytest.mark.parametrize("b,w", [(1, 2), (3, 16), (2, 13), (60, 16), (70, 12), (1, 32), (40, 32), (5, 9)])
+def test_deals_of_rows_to_ctas(b, w):
+    check(*make(b, w, 5003, F16, seed=11), min(2 * w, 32))
+
+
 def test_pitch_and_leading_dimensions():
     from paper_2607_03011_gb300 import inner
     z, scores = make(6, 4, 133, F16, seed=8)

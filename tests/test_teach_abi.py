@@ -39,7 +39,7 @@ def test_distill(iso, ptr):
     shared = [dict(z=None), dict(z=odd(p, 2)), dict(ld=7), dict(dt=3), dict(dt=-1), dict(n=-1), dict(n=1 << 31), dict(vocab=0),
               dict(vocab=1 << 31, ld=1 << 32), dict(v=None), dict(v=odd(p)), dict(ldv=3), dict(vt=3), dict(i=None), dict(i=odd(p, 4)), dict(ldi=3), dict(ib=2),
               dict(k=0), dict(k=-1), dict(k=257, ldv=300, ldi=300), dict(scale=0.0), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF),
-              dict(tail=2), dict(tail=-1), dict(saved=odd(p, 2)), dict(gz=p, g=p, ldg=7), dict(gz=odd(p, 2), g=p), dict(gz=p, g=None), dict(gz=p, g=odd(p))]
+              dict(tail=2), dict(tail=-1), dict(saved=odd(p, 2)), dict(gz=p, g=p, ldg=7), dict(z=p, gz=p, g=p, ldg=9), dict(gz=odd(p, 2), g=p), dict(gz=p, g=None), dict(gz=p, g=odd(p))]
     for kw in shared + [dict(loss=None), dict(loss=odd(p))]:
         assert call(**kw) == bad, kw
         assert iso.last_error()
@@ -137,6 +137,13 @@ def test_no_overlap_is_missed(iso):
             assert shared(iso, a, b), (a, b)
         elif (batch_s, beam_s) == (96, 32):
             assert not shared(iso, a, b), (a, b)
+
+
+def test_beams_among_the_states(iso):
+    L = iso.lib()
+    for at in (A, A + 592, A - 40):
+        assert L.isoloco_beam_reorder(states(iso, place(A)), 1, 2, 3, ctypes.c_void_p(at), 8, None) == iso.ERR_INVALID
+        assert "beams" in iso.last_error() and "shares" in iso.last_error()
 
 
 @pytest.mark.parametrize("e", [
