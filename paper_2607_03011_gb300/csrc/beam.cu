@@ -3,10 +3,10 @@
 // Selection: with M the largest logit of beam w's row and S = sum e^{scale (x - M)}, a continuation by t has the total
 // score_w + scale (x_t - M) - ln S.  Within a beam the totals rank as the logits do, so each row gives its `keep` largest logits
 // (found as token_logprobs finds them) and its two sums, in one pass, and the batch entry's best are merged from those lists.
-// What bounds it: for few rows the chain of loads, reductions and barriers (1 x 4 x 32000 bf16 10.6 us: 2.2 thousand cycles for the row,
-// 4 for its search, 4 for the cluster's barrier, 5 for the merging); for many the loads in flight and what SMs have left to do when others are
-// done (64 x 16 x 128000 bf16 60 us, 3.9 TB/s: 922 rows that are read are 6.07 to an SM, in CTAs of two).  The merging in a launch of its own, with a CTA
-// per row, took 63.
+// What bounds it: for few rows the chain of loads, reductions and barriers (1 x 4 x 32000 bf16 10.4 us: 2.2 thousand cycles for the row,
+// 4 for its search, 4 for the cluster's barrier, 5 for the merging); for many the loads in flight and what SMs have left to do when
+// others are done (64 x 16 x 128000 bf16 60 us, 3.9 TB/s: the 922 rows that are read are 6.07 to an SM, in CTAs of two).  The
+// merging in a launch of its own, with a CTA per row, took 63.
 //
 // Every row is cut in the same places, counted from its first entry, wherever that lies: beams with equal logits and
 // scores get equal totals to the last bit, and rank by their numbers.
@@ -26,8 +26,8 @@ namespace {
 
 constexpr int kMaxKeep = ISOLOCO_MAX_TOP;
 constexpr int kMaxLists = ISOLOCO_MAX_BEAMS;  // of a batch entry: rows, or shares of rows
-constexpr int kMaxCtas = 16;   // of a batch entry
-constexpr int kUnroll = 4;
+constexpr int kMaxCtas = 16;                  // of a batch entry
+constexpr int kUnroll = 4;  // (6 or 8 vectors in flight: 63 and 65 us for 60)
 
 __device__ __forceinline__ float value_of(uint64_t key) {
     const uint32_t o = static_cast<uint32_t>(key >> 32);
@@ -508,10 +508,10 @@ cudaError_t select(const BeamArgs& a, cudaStream_t st) {
     int sms = 0;
     const cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;
-    // A row in two, four or eight shares while a batch entry's CTAs have one each, SMs less than two, and shares 4096 entries (1 x 4 x
+    // A row in two, four or eight shares while a batch entry's CTAs have one each, all run at once, and shares 4096 entries (64 x 4 x 32000 fp32 14.8 us, 16.6 in whole rows; 1 x 4 x
     // 128000 bf16 10.5 us; 12.4 in half as many shares; a CTA that takes four shares one after the other 20).
     int split = 1;
-    while (a.beams * split * 2 <= kMaxCtas && a.batch * a.beams * split * 2 <= 2 * sms && a.vocab / (2 * split) >= 4096) split *= 2;
+    while (a.beams * split * 2 <= kMaxCtas && a.batch * a.beams * split * 2 <= 4 * sms && a.vocab / (2 * split) >= 4096) split *= 2;
     // Clusters of up to 16 while all of their CTAs run at once, or where CTAs of 8 would have unequal shares (32 x 16 x 128000 bf16 35 us, 46 with
     // clusters of 8; 100 x 10 x 32000 29 and 38); else of 8 (64 x 16 x 128000 60 us, 73 with 16).
     const int units = a.beams * split;

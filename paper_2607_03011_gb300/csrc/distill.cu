@@ -10,10 +10,10 @@
 // share, which a difference (S less the list's) would lose, and one so small that it is 0 about M still has its logarithm.
 // Without a rest (r = 0) the parting is not needed: the sums are over all tokens, and Mr = M, Sr = S above.
 //
-// What bounds it: HBM (8192 x 32000 bf16 with gradient 173 us, 6.1 TB/s of logits read and gradient written, the copy's rate 157) and close
-// behind the powers, two to an entry at 16 per cycle and SM (113 us).  The list (k tokens scattered over the row, equal ones
-// added up) is a chain of dependent loads and small reductions; a warp of its own goes through it beside the pass over
-// the row (before it: 22 us more).
+// What bounds it: HBM (8192 x 32000 bf16 with gradient 173 us, 6.1 TB/s of logits read and gradient written; the copy's rate
+// allows 157).  Issue slots are half used, the pipe of the powers, two to an entry, a third.  The list (k tokens scattered over the row,
+// equal ones added up) is a chain of dependent loads and small reductions; a warp of its own goes through it beside the pass over the row (before
+// it: 22 us more).
 #include <algorithm>
 
 #include "common.cuh"
@@ -37,7 +37,7 @@ constexpr uint32_t kNone = 0xffffffffu;
 // 173, where reading it again from L2 takes 195 (loss and list in the same threads) and persistent CTAs that start together 247: they stay in
 // step, so that loads, powers and stores do not overlap.  2047 x 50021 fp16 in two shares 82, from L2 106.
 // 16-bit rows of more than kHeldMost entries are four shares or more, whose CTAs wait for one another: 128000 bf16 1205, from L2 in
-// shares of kShareBytes 904 (of 140000 bytes, which L2 does not keep, 985; of 40000 1070).  fp32 rows have half the powers to
+// shares of kShareBytes 904 (of 140000 bytes, which L2 does not keep, 985; of 40000 1070).  fp32 rows have half the entries to
 // a byte: 2048 x 128000 378 held, 400 from L2.
 // Without gradient nothing is held: 4096 x 32000 fp32 79 to 82, held 131.
 constexpr int64_t kHeldBytes = 72 * 1024;

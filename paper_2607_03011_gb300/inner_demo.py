@@ -29,6 +29,12 @@ def views(flat: torch.Tensor, spec) -> Dict[str, torch.Tensor]:
     return {name: flat[off:off + r * c].view(r, c) for (name, _, _), (off, r, c) in zip(spec, param_table(spec))}
 
 
+def initialise(flat: torch.Tensor, spec, gen: torch.Generator):
+    width = spec[0][2]
+    for name, v in views(flat, spec).items():
+        v.copy_(torch.randn(v.shape, generator=gen, device=flat.device) * (1.0 if name == "embed" else 1.0 / math.sqrt(width)))
+
+
 def forward(p: Dict[str, torch.Tensor], ids: torch.Tensor, save: bool):
     """Logits (bf16) and what the backward pass needs."""
     w = {name: v.bfloat16() for name, v in p.items()}
@@ -118,8 +124,7 @@ def run(workers: int = 4, rounds: int = 4, inner_steps: int = 12, tokens: int = 
     table = param_table(spec)
     n = table[-1][0] + table[-1][1] * table[-1][2]
     theta = torch.empty(n, device=dev)
-    for name, v in views(theta, spec).items():
-        v.copy_(torch.randn(v.shape, generator=gen, device=dev) * (1.0 if name == "embed" else 1.0 / math.sqrt(width)))
+    initialise(theta, spec, gen)
     momentum = torch.zeros_like(theta)
     follow = torch.randperm(vocab, generator=gen, device=dev)
     held_out = text(follow, 4 * tokens, gen)
@@ -138,7 +143,8 @@ def run(workers: int = 4, rounds: int = 4, inner_steps: int = 12, tokens: int = 
                f"{held[0]:.3f}, entropy {held[1]:.3f}, in the top five {100 * held[2]:.1f} %")
     small = shapes(vocab, width // 2, ff // 2)
     size = sum(r * c for _, r, c in small)
-    student = torch.randn(size, generator=gen, device=dev) * (0.5 / math.sqrt(width))
+    student = torch.empty(size, device=dev)
+    initialise(student, small, gen)
     for _ in range(inner_steps):
         divergence, g = taught(student, small, theta, spec, text(follow, tokens, gen)[0])
         norm = update(views(student, small), small, g, lr, max_norm)

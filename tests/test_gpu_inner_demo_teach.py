@@ -21,17 +21,18 @@ def test_gradients_of_the_student():
     ids = torch.randint(0, 300, (500,), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
     loss, grads = demo.taught(student, small, teacher, big, ids, top=8)
     t = inner.token_logprobs(demo.forward(demo.views(teacher, big), ids, save=False)[0], ids, top=8)
-    p = {k: v.double().requires_grad_(True) for k, v in demo.views(student, small).items()}
+    top_logp, top_index, ids = t.top_logp.cpu().double(), t.top_index.cpu(), ids.cpu()
+    p = {k: v.cpu().double().requires_grad_(True) for k, v in demo.views(student, small).items()}
     x = p["embed"][ids]
     y = x + (torch.nn.functional.silu(x @ p["w_gate"]) * (x @ p["w_up"])) @ p["w_down"]
     lp = torch.log_softmax(y @ p["head"].t(), 1)
-    q = t.top_logp.double().exp()
-    rest, share = 1 - q.sum(1), 1 - lp.gather(1, t.top_index).exp().sum(1)
-    want = ((q * (q.log() - lp.gather(1, t.top_index))).sum(1) + rest * (rest.log() - share.log())).mean()
+    q = top_logp.exp()
+    rest, share = 1 - q.sum(1), 1 - lp.gather(1, top_index).exp().sum(1)
+    want = ((q * (q.log() - lp.gather(1, top_index))).sum(1) + rest * (rest.log() - share.log())).mean()
     assert abs(loss.item() - want.item()) < 2e-2 * want.item()
     for k, d in zip(p, torch.autograd.grad(want, list(p.values()))):
         # some eight roundings to bf16 (2^-8 each) lie between the definition and a gradient
-        assert ((grads[k].double() - d).norm() / d.norm()).item() < 8 * 2.0 ** -8, k
+        assert ((grads[k].cpu().double() - d).norm() / d.norm()).item() < 8 * 2.0 ** -8, k
 
 
 def test_answers():
