@@ -33,22 +33,25 @@ constexpr int kUnroll = 4;
 constexpr uint32_t kNone = 0xffffffffu;
 
 // ---- which kernel, and how many threads to how much of a row (8192 rows unless said otherwise, us)
-// With gradient a row is held in shared memory (k_distill_held), in shares of at most kHeldBytes, three to an SM: 32000 bf16
-// 173, where reading it again from L2 takes 195 (loss and list in the same threads) and persistent CTAs that start together 247: they stay in
-// step, so that loads, powers and stores do not overlap.  2047 x 50021 fp16 in two shares 82, from L2 106.
-// 16-bit rows of more than kHeldMost entries are four shares or more, whose CTAs wait for one another: 128000 bf16 1205, from L2 in
-// shares of kShareBytes 904 (of 140000 bytes, which L2 does not keep, 985; of 40000 1070).  fp32 rows have half the entries to
-// a byte: 2048 x 128000 378 held, 400 from L2.
+// With gradient a row is held in shared memory (k_distill_held): 32000 bf16 173, where reading it again from L2 takes 195
+// (loss and list in the same threads) and persistent CTAs that start together 247: they stay in step, so that loads, powers and
+// stores do not overlap.
+// In one CTA up to kHeldBytes (two of 512 threads to an SM above kWideHeld, three of 256 below): 50021 fp16 258, in two CTAs that wait for each
+// other 289; 4096 x 54000 bf16 151 and 180; 4096 x 25000 fp32 137 and 141.
+// 16-bit rows of more (kHeldMost entries) are read again from L2, in shares of kShareBytes: 4096 x 64000 bf16 186, held in two shares 198; 128000
+// bf16 904, held in four 1205 (in shares of 140000 bytes, which L2 does not keep, 985; of 40000 1070).  fp32 rows have half the
+// entries to a byte: 2048 x 128000 378 held, 400 from L2.
 // Without gradient nothing is held: 4096 x 32000 fp32 79 to 82, held 131.
-constexpr int64_t kHeldBytes = 72 * 1024;
+constexpr int64_t kHeldBytes = 108 * 1024;
+constexpr int64_t kWideHeld = 72 * 1024;
 constexpr int64_t kMostHeldBytes = 216 * 1024;  // (where few rows are long)
-constexpr int64_t kHeldMost = 72000;
+constexpr int64_t kHeldMost = 55000;
 constexpr int64_t kShareBytes = 98304;
 // 64 threads: held 4000 bf16 43 us, 54 with 128; 8000 60 and 66.  128: held fp32 2048 x 128000 (shares of 16000) 378, 397 with 256.
 constexpr int64_t kSmallHeld = 8192, kMediumHeld = 16384;
 constexpr int64_t kSmall = 8192, kMedium = 16384;
 // CTAs per SM that the registers are cut for
-constexpr int held_ctas(int threads) { return threads == 64 ? 11 : threads == 128 ? 7 : 4; }
+constexpr int held_ctas(int threads) { return threads == 64 ? 11 : threads == 128 ? 7 : threads == 256 ? 4 : 2; }
 constexpr int stream_ctas(int threads) { return threads == 64 ? 14 : threads == 128 ? 8 : 5; }
 // Entries of a share whose marks (of the list's tokens) are kept apart.
 constexpr uint32_t marks_of(int threads) { return threads <= 128 ? 16384 : 65536; }
@@ -819,6 +822,7 @@ cudaError_t run_held(const DistillArgs& a, int sms, cudaStream_t st) {
     const int64_t share = a.vocab / split;
 #define HELD(N) (a.rest ? launch_held<T, N, true>(a, split, err, st) : launch_held<T, N, false>(a, split, err, st))
     if (share <= kSmallHeld) return HELD(64);
+    if (share * static_cast<int64_t>(sizeof(T)) > kWideHeld) return HELD(512);
     return share <= kMediumHeld ? HELD(128) : HELD(256);
 #undef HELD
 }

@@ -367,35 +367,39 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, keep: Optional[int] 
     score.  A first step starts from one beam: scores of -inf for the others."""
     if stream is not None:
         return _on(stream, beam_select, logits, scores, keep, finished, end, scale)
-    if logits.dim() < 2:
+    rows_of = logits.shape[:-1]
+    if not rows_of:
         raise ValueError("logits: ... x beams x vocab expected")
-    lead, beams, dev = logits.shape[:-2], logits.shape[-2], logits.device
     z, n, vocab, ld = _rows(logits, "logits")
+    beams, dev = rows_of[-1], z.device
     if not 1 <= beams <= MAX_BEAMS:
         raise ValueError(f"logits: 1 .. {MAX_BEAMS} beams")
-    keep = beams if keep is None else keep
+    if keep is None:
+        keep = beams
     if not 1 <= keep <= min(beams * vocab, MAX_TOP):
         raise ValueError(f"keep: 1 .. {min(beams * vocab, MAX_TOP)}")
-    if scores.shape != logits.shape[:-1]:
+    if scores.shape != rows_of:
         raise ValueError("scores: one per row of logits expected")
-    ps, pf = _per_row(scores, n, "scores"), None
+    ps, pf, pe, code = _per_row(scores, n, "scores"), None, None, -1
+    shape = (*rows_of[:-1], keep)
+    f = None
+    if end is not None:
+        if not 0 <= end < vocab:
+            raise ValueError(f"end: 0 .. {vocab - 1}")
+        f = _empty(shape, dtype=torch.bool, device=dev)
+        pe, code = f.data_ptr(), end
     if finished is not None:
-        if finished.dtype != torch.bool or finished.shape != scores.shape or not finished.is_contiguous() or \
+        if finished.dtype != torch.bool or finished.shape != rows_of or not finished.is_contiguous() or \
                 finished.get_device() != _current_device():
             raise ValueError("finished: contiguous bools on the current CUDA device expected, one per score")
-        pf = finished.data_ptr()
         if end is None:
             raise ValueError("finished: needs the token `end`")
-    if end is not None and not 0 <= end < vocab:
-        raise ValueError(f"end: 0 .. {vocab - 1}")
-    shape = (*lead, keep)
+        pf = finished.data_ptr()
     s = _empty(shape, dtype=torch.float32, device=dev)
     b = _empty(shape, dtype=torch.int64, device=dev)
     t = _empty(shape, dtype=torch.int64, device=dev)
-    f = None if end is None else _empty(shape, dtype=torch.bool, device=dev)
-    rc = lib().isoloco_beam_select(z.data_ptr(), ld, _DTYPE[z.dtype], n // beams, beams, vocab, ps, pf,
-                                   -1 if end is None else end, scale, keep, s.data_ptr(), b.data_ptr(), t.data_ptr(),
-                                   _ptr(f), _raw_stream(dev.index))
+    rc = lib().isoloco_beam_select(z.data_ptr(), ld, _DTYPE[z.dtype], n // beams, beams, vocab, ps, pf, code, scale, keep,
+                                   s.data_ptr(), b.data_ptr(), t.data_ptr(), pe, _raw_stream(dev.index))
     if rc:
         _check(rc, "isoloco_beam_select")
     return BeamSelection(s, b, t, f)

@@ -113,7 +113,7 @@ def test_pitches_and_offsets(pad, offset, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("vocab", [4096, 4101, 70000, 80001])
+@pytest.mark.parametrize("vocab", [4096, 4101, 50001, 70000, 80001])
 def test_gradient_over_the_logits_and_elsewhere(dtype, vocab):
     """Through the C entry point: the gradient over the logits themselves, and into rows of another alignment whose
     neighbours stay as they are."""
