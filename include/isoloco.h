@@ -354,7 +354,7 @@ int64_t isoloco_plan_launches(isoloco_plan_t plan);
 
 /* ---------------------------------------------------------------------------------------------
  * Operators of a worker's inner step: what a replica computes between two outer steps, and how a
- * merged model is scored.  They need no plan.  Conventions:
+ * merged model is scored, teaches and answers.  They need no plan.  Conventions:
  * - Matrices are row-major with a row pitch `ld_*` in elements (>= the row's length); rows are
  *   contiguous.  Data pointers need their element's alignment only; workspaces 16 bytes.  Sizes that
  *   allow 16-byte accesses (pitches and addresses multiples of 16 bytes) run faster.

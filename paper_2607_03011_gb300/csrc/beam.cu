@@ -474,7 +474,9 @@ cudaError_t launch_select(const BeamArgs& a, int split, int ctas, cudaStream_t s
         int dev = 0, set = 0;
         cudaError_t e = cudaGetDevice(&dev);
         if (e == cudaSuccess)
-            e = ready.get<cudaError_t>(dev, &set, [](int*) { return cudaFuncSetAttribute(k_beam_select<T, THREADS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); });
+            e = ready.get<cudaError_t>(dev, &set, [](int*) {
+                return cudaFuncSetAttribute(k_beam_select<T, THREADS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+            });
         if (e != cudaSuccess) return e;
     }
     const uint32_t per = static_cast<uint32_t>(((a.vocab + split - 1) / split + 63) & ~int64_t(63));
@@ -508,12 +510,13 @@ cudaError_t select(const BeamArgs& a, cudaStream_t st) {
     int sms = 0;
     const cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;
-    // A row in two, four or eight shares while a batch entry's CTAs have one each, all run at once, and shares 4096 entries (64 x 4 x 32000 fp32 14.8 us, 16.6 in whole rows; 1 x 4 x
-    // 128000 bf16 10.5 us; 12.4 in half as many shares; a CTA that takes four shares one after the other 20).
+    // A row in two, four, eight or sixteen shares while a batch entry's CTAs have one each, all run at once, and shares have
+    // 4096 entries (64 x 4 x 32000 fp32 14.8 us, 16.6 in whole rows; 1 x 4 x 128000 bf16 10.5 us, 12.4 in half as many shares,
+    // and 20 where a CTA takes four shares one after the other).
     int split = 1;
     while (a.beams * split * 2 <= kMaxCtas && a.batch * a.beams * split * 2 <= 4 * sms && a.vocab / (2 * split) >= 4096) split *= 2;
-    // Clusters of up to 16 while all of their CTAs run at once, or where CTAs of 8 would have unequal shares (32 x 16 x 128000 bf16 35 us, 46 with
-    // clusters of 8; 100 x 10 x 32000 29 and 38); else of 8 (64 x 16 x 128000 60 us, 73 with 16).
+    // Clusters of up to 16 while all of their CTAs run at once, or where CTAs of 8 would have unequal shares (32 x 16 x 128000
+    // bf16 35 us, 46 with clusters of 8; 100 x 10 x 32000 29 and 38); else of 8 (64 x 16 x 128000 60 us, 73 with 16).
     const int units = a.beams * split;
     const int ctas = units <= 8 || (units % 8 == 0 && a.batch * units > 4 * sms) ? std::min(8, units) : std::min(kMaxCtas, units);
     // 512 threads where an SM has no more than one CTA: 16 x 8 x 50021 fp16 18.7 us, 20.6 with 256 (64 x 5 x 32000 fp32, two CTAs to an SM, 20.6 and 15.2).

@@ -793,7 +793,8 @@ cudaError_t launch_held(const DistillArgs& a, uint32_t split, uint32_t* err, cud
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess)
         e = ready.get<cudaError_t>(dev, &set, [](int*) {
-            return cudaFuncSetAttribute(k_distill_held<T, THREADS, REST>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMostHeldBytes) + 16);
+            return cudaFuncSetAttribute(k_distill_held<T, THREADS, REST>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                        static_cast<int>(kMostHeldBytes) + 16);
         });
     if (e != cudaSuccess) return e;
     const int64_t per = ((a.vocab + split - 1) / split + 63) & ~int64_t(63), bytes = per * static_cast<int64_t>(sizeof(T)) + 16;
@@ -817,7 +818,8 @@ cudaError_t run_held(const DistillArgs& a, int sms, cudaStream_t st) {
     const cudaError_t e = error_word(&err);
     if (e != cudaSuccess) return e;
     uint32_t split = 1;
-    while (split < kMaxSplit && (a.vocab * static_cast<int64_t>(sizeof(T)) > split * kHeldBytes || (a.rows * split * 2 <= 2 * sms && a.vocab / (2 * split) >= 4096)))
+    while (split < kMaxSplit && (a.vocab * static_cast<int64_t>(sizeof(T)) > split * kHeldBytes ||
+                                 (a.rows * split <= sms && a.vocab / (2 * split) >= 4096)))
         split *= 2;
     const int64_t share = a.vocab / split;
 #define HELD(N) (a.rest ? launch_held<T, N, true>(a, split, err, st) : launch_held<T, N, false>(a, split, err, st))
@@ -832,11 +834,12 @@ cudaError_t run(const DistillArgs& a, cudaStream_t st) {
     int sms = 0;
     const cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;
-    if (a.grad_logits && (sizeof(T) == 4 || a.vocab <= kHeldMost) && (a.vocab / kMaxSplit + 64) * static_cast<int64_t>(sizeof(T)) <= kMostHeldBytes) return run_held<T>(a, sms, st);
+    const int64_t least = (a.vocab / kMaxSplit + 64) * static_cast<int64_t>(sizeof(T));
+    if (a.grad_logits && (sizeof(T) == 4 || a.vocab <= kHeldMost) && least <= kMostHeldBytes) return run_held<T>(a, sms, st);
     // CTAs per row: more than one where rows leave SMs idle (of at least 4096 entries each), where the rows that are under way
     // at once would not stay in L2 for the gradient, and where marks would meet
     uint32_t split = 1;
-    while (split < kMaxSplit && ((a.rows * split * 2 <= 2 * sms && a.vocab / (2 * split) >= 4096) ||
+    while (split < kMaxSplit && ((a.rows * split <= sms && a.vocab / (2 * split) >= 4096) ||
                                  (a.grad_logits && a.vocab * static_cast<int64_t>(sizeof(T)) > split * kShareBytes) ||
                                  (a.rest && a.vocab > split * int64_t(marks_of(256)))))
         split *= 2;
