@@ -176,12 +176,7 @@ __device__ __forceinline__ void add_powers(const Vec<T>& v, float m, F2 c2, F2& 
     const F2 minus = pair(-m, -m);
     float f[Vec<T>::kN];
     v.unpack(f);
-#pragma unroll
-    for (int j = 0; j < Vec<T>::kN; j += 2) {
-        float d0, d1;
-        unpair(mul2(add2(pair(f[j], f[j + 1]), minus), c2), d0, d1);
-        s2 = add2(s2, pair(ex2(d0), ex2(d1)));
-    }
+    s2 = add2(s2, powers(f, minus, c2));
 }
 __device__ __forceinline__ float both(F2 s2) {
     float a, b;

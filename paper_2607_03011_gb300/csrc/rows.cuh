@@ -48,6 +48,25 @@ __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
     return r;
 }
+
+// The sum of 2^((f - m) c), of even and odd entries apart, added up as a tree (a sum that takes them one by one rounds
+// more often, and waits for itself).
+template <int N>
+__device__ __forceinline__ F2 powers(const float (&f)[N], F2 minus_m, F2 c2) {
+    F2 p[N / 2];
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) {
+        float d0, d1;
+        unpair(mul2(add2(pair(f[2 * j], f[2 * j + 1]), minus_m), c2), d0, d1);
+        p[j] = pair(ex2(d0), ex2(d1));
+    }
+#pragma unroll
+    for (int n = N / 4; n; n /= 2)
+#pragma unroll
+        for (int j = 0; j < n; ++j) p[j] = add2(p[j], p[j + n]);
+    return p[0];
+}
+
 // Largest entries of vectors: pairs of 16-bit entries (or four fp32 ones) are compared at once.
 template <class T>
 struct Largest {
