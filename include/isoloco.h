@@ -451,9 +451,10 @@ int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_d
  *   tail DROP: q = softmax(top_logp) over the row's list, r = 0;
  *   tail REST: q = exp(top_logp), and r = max(0, 1 - sum q) is one more outcome, any token outside the list, whose
  *     probability is the student's P = sum over those tokens of p.  (r counts as 0 where every such token is masked.)
- *   loss = sum_i q_i (log q_i - log p_i) + r (log r - log P), with 0 log 0 = 0.
- *   gradient by the logits, with Q = sum_i q_i + r:  grad_loss scale (p_j Q - q_j) for a token of the list (q_j summed
- *     over its entries, where it has several), grad_loss scale p_j (Q - r / P) for any other.
+ *   The entries of one token add up: q_j is the sum over token j's entries.
+ *   loss = sum_j q_j (log q_j - log p_j) over the list's tokens + r (log r - log P), with 0 log 0 = 0.
+ *   gradient by the logits, with Q = sum_j q_j + r:  grad_loss scale (p_j Q - q_j) for a token of the list, grad_loss
+ *     scale p_j (Q - r / P) for any other.
  * An entry whose index is outside [0, vocab) is not there.  A row without entries (or, with DROP, whose entries all
  * have the weight 0) has the loss 0 and the gradient 0, whatever its logits.
  * Logits of -inf or the type's lowest value are masked and have probability 0 (F16's -65504 where scale is 0.002 or

@@ -4,7 +4,7 @@
 // and the others:
 //     others: Mr their largest logit, Sr = sum 2^((x - Mr) c)          list: Ml, Sl the same
 //     S = Sl 2^((Ml - M) c) + Sr 2^((Mr - M) c),   lse = scale M + ln S,   P = Sr 2^((Mr - M) c) / S
-//     loss = sum q (ln q - z + lse) + r (ln r - ln P),  Q = sum q + r
+//     loss = sum q (ln q - z + lse) + r (ln r - ln P),  Q = sum q + r    (q of a token: the sum over its entries)
 //     gradient: others 2^((x - Mr) c) (P Q - r) / Sr,  list 2^((x - M) c) / S Q - q
 // The others are summed by themselves and about their own largest: a student that has learned the list leaves them a small
 // share, which a difference (S less the list's) would lose, and one so small that it is 0 about M still has its logarithm.
@@ -104,7 +104,7 @@ struct List {
     bool any;           // there are entries that count
     float weight;       // sum q
     float rest;         // 1 - sum q, at least 0 (DROP: 0)
-    float terms;        // sum q (ln q - scale (x - m))
+    float terms;        // sum over its tokens of q (ln q - scale (x - m))
     float m, s;         // largest logit of its tokens, and the sum of powers about it
     float about, inv;   // q = e^(logp - about) inv
 
@@ -360,11 +360,12 @@ __device__ __forceinline__ List warp_sums(const DistillArgs& a, float c, ListSme
         if (id == kNone) continue;
         const float v = sm.logp[e], x = sm.x[e], we = expf(v - about);
         w += we;
-        if (we != 0.f) t += we * ((v - about) - (x - m) * a.scale);
         float total;
         if (first_of_token(sm, a.k, e, id, total, [&](int j) { return j == e ? we : expf(sm.logp[j] - about); })) {
             sm.q[e] = total;
             s += power(x, m, c);
+            // (its only entry of a weight above 0: the logarithm as it was given)
+            if (total != 0.f) t += total * ((total == we ? v - about : logf(total)) - (x - m) * a.scale);
         }
     }
     l.s = warp_sum(s);
