@@ -454,7 +454,8 @@ def beam_reorder(states: Iterable[torch.Tensor], beams: torch.Tensor, out: Optio
     """state[b, w] = state[b, beams[b, w]] for what is kept for beams (caches, histories of tokens; any types), in place or
     into `out`; returns the list of results.  beams: batch x width (or width) of int32 or int64, an entry outside [0, width) stands for
     the beam itself.  States are batch x width x ... or (batch * width) x ...; the used part of a longer cache is given as a slice (of which the
-    rest stays as it is).  Results may not share memory with one another or with states that they are not made in place of."""
+    rest stays as it is).  Results may not share memory with one another or with states that they are not made in place of, and are lazily conjugated or
+    negated views where the states are."""
     states, out = list(states), None if out is None else list(out)
     if stream is not None:
         return _on(stream, beam_reorder, states, beams, out)
@@ -483,6 +484,11 @@ def beam_reorder(states: Iterable[torch.Tensor], beams: torch.Tensor, out: Optio
         while k < n and types[k] is typ and steps[k] == step and shapes[k] == shape and to_steps[k] == to_step:
             k += 1
         words.extend(array.array("q", (0, 0, *_fold_pair(shape, step, to_step, typ.itemsize, batch, width, two))) * (k - i))
+        # Bytes are moved: what torch conjugates or negates when it is read has to be so on both sides.  (Real tensors that are
+        # negated so are imaginary parts, whose strides are even; asking each tensor costs 0.1 us.)
+        if out is not None and (typ.is_complex or not step[-1] & to_step[-1] & 1) and \
+                any(s.is_conj() != t.is_conj() or s.is_neg() != t.is_neg() for s, t in zip(states[i:k], out[i:k])):
+            raise ValueError("out: conjugated or negated lazily where the states are not, or the other way round")
         i = k
     words[0::10] = array.array("q", map(_data_ptr, states))
     words[1::10] = array.array("q", map(_data_ptr, to))
