@@ -55,6 +55,7 @@ constexpr int held_ctas(int threads) { return threads == 64 ? 11 : threads == 12
 constexpr int stream_ctas(int threads) { return threads == 64 ? 14 : threads == 128 ? 8 : 5; }
 // Entries of a share whose marks (of the list's tokens) are kept apart.
 constexpr uint32_t marks_of(int threads) { return threads <= 128 ? 16384 : 65536; }
+constexpr float kSmallRest = 0.0625f;
 // Vectors per thread of the gradient by itself: 8192 x 128000 bf16 657 us (the copy rate allows 628); 16 667, 8 769, 4 869 (a list for
 // every span).
 constexpr int kSpan = 32;
@@ -119,11 +120,10 @@ struct List {
         const float x = id != kNone ? to_f32(row[id]) : 0.f;
         return x <= masked_at<T>() ? -INFINITY : x;
     }
-    // The rest of it, from the sums of the weights e^(logp - about) and of their terms.
-    __device__ __forceinline__ void finish(const DistillArgs& a, float w, float t) {
+    // The rest of it, from the sums of the weights e^(logp - about) and of their terms, and what they leave of 1.
+    __device__ __forceinline__ void finish(const DistillArgs& a, float w, float t, float left) {
         any = any && (a.rest || w != 0.f);
         if (a.rest) {
-            const float left = 1.f - w;
             inv = 1.f;
             weight = w < INFINITY ? w : NAN;
             rest = w < INFINITY ? fmaxf(left, 0.f) : NAN;
@@ -344,6 +344,42 @@ __device__ __forceinline__ void warp_read(const DistillArgs& a, int64_t r, ListS
     }
     __syncwarp();
 }
+// 1 - sum e^logp, w the sum in fp32.  That is off by some 2^-22, which is nothing beside a large rest, but all of one that a teacher
+// leaves whose list holds nearly everything; rests below kSmallRest are made good to 2^-43 for each entry.  e^v - 1 = hi + lo, two fp32 numbers:
+// Taylor's series at v / 1024, then ten times (1 + p)^2 - 1 = 2 p + p^2, with the roundings of hi + hi + hi^2 kept in lo (off by 2^-44 at most over
+// 800000 numbers tried); the sums as whole numbers of 2^-22 and 2^-45.  8192 x 32000 bf16, lists of 32: 185 us where all rests are small, 178 where
+// none is; with 64-bit floating point, of which an SM makes two operations a cycle, 193.
+__device__ __forceinline__ float left_of(const DistillArgs& a, float w, ListSmem& sm) {
+    if (!(1.f - w < kSmallRest)) return 1.f - w;
+    constexpr int kTimes = 10;
+    constexpr float kCoarse = 1 << 22, kFine = 35184372088832.f;
+    int coarse = 0, fine = 0, count = 0;  // (of 256 entries: at most 2^30, 2^30 and 2^8)
+#pragma unroll 1
+    for (int e = threadIdx.x & 31; e < a.k; e += 32) {
+        const float v = fminf(sm.logp[e], 0.f);  // (one above 0 leaves nothing as it is)
+        if (v < -40.f) continue;                 // nothing in these units (no entry: -inf)
+        const float x = v * (1.f / (1 << kTimes)), xx = __fmul_rn(x, x), half = 0.5f * xx;
+        const float more = x * xx * fmaf(x, fmaf(x, 1.f / 120.f, 1.f / 24.f), 1.f / 6.f);
+        float hi = __fadd_rn(x, half), lo = __fadd_rn(__fadd_rn(x, -hi), half) + fmaf(0.5f, __fmaf_rn(x, x, -xx), more);
+#pragma unroll
+        for (int i = 0; i < kTimes; ++i) {
+            const float two = hi + hi, sq = __fmul_rn(hi, hi), low = fmaf(two, lo, __fmaf_rn(hi, hi, -sq));
+            const float top = __fadd_rn(two, sq), l = __fadd_rn(__fadd_rn(two, -top), sq) + fmaf(2.f, lo, low);
+            hi = __fadd_rn(top, l);
+            lo = __fadd_rn(__fadd_rn(top, -hi), l);
+        }
+        const int n = __float2int_rn(hi * kCoarse);
+        coarse += n;
+        fine += __float2int_rn((fmaf(static_cast<float>(n), -1.f / kCoarse, hi) + lo) * kFine);
+        ++count;
+    }
+    coarse = __reduce_add_sync(0xffffffffu, coarse);
+    fine = __reduce_add_sync(0xffffffffu, fine);
+    count = __reduce_add_sync(0xffffffffu, count);
+    const long long units = (static_cast<long long>(1 - count) * (1 << 22) - coarse) * (1 << 23) - fine;
+    return __ll2float_rn(units) * (1.f / kFine);
+}
+template <bool REST>
 __device__ __forceinline__ List warp_sums(const DistillArgs& a, float c, ListSmem& sm) {
     const int lane = threadIdx.x & 31;
     List l;
@@ -369,7 +405,8 @@ __device__ __forceinline__ List warp_sums(const DistillArgs& a, float c, ListSme
         }
     }
     l.s = warp_sum(s);
-    l.finish(a, warp_sum(w), warp_sum(t));
+    w = warp_sum(w);
+    l.finish(a, w, warp_sum(t), REST ? left_of(a, w, sm) : 0.f);
     return l;
 }
 
@@ -407,7 +444,7 @@ __global__ void __launch_bounds__(THREADS + 32, stream_ctas(THREADS)) k_distill(
             __syncwarp();
             bar_arrive<kMasked>(kAll);
         }
-        const List l = warp_sums(a, c, sm);
+        const List l = warp_sums<REST>(a, c, sm);
         if (lane == 0) list_out = l;
         __syncwarp();
         if (GRAD) bar_arrive<kListed>(kAll);
@@ -646,7 +683,7 @@ __global__ void __launch_bounds__(THREADS + 32, held_ctas(THREADS)) k_distill_he
         if (lane < nvec * V - end) mine[end + lane] = from_f32<T>(-INFINITY);
         __syncwarp();
         bar_arrive<kMasked>(kAll);
-        const List l = warp_sums(a, c, sm);
+        const List l = warp_sums<REST>(a, c, sm);
         if (lane == 0) list_out = l;
         __syncwarp();
         bar_arrive<kListed>(kAll);
