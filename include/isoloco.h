@@ -541,11 +541,15 @@ int isoloco_clip_grads(const isoloco_tensor_t* tensors, const isoloco_tensor_t* 
 
 /* Synchronizes `stream` and returns the device status of the inner step's operators on the current
  * device since the last such call: OK, or TIMEOUT when a kernel's wait gave up, on any of the device's
- * streams (its outputs are then undefined).  Every such error is reported to one caller at least. */
+ * streams (its outputs are then undefined; of isoloco_distill, the row's loss and gradient are NaN).  Every such error is reported to one caller at least. */
 int isoloco_inner_status(void* stream);
 
 /* Testing hook: enqueues a kernel on `stream` that raises the same status as a wait that gave up. */
 int isoloco_debug_raise_inner(void* stream);
+
+/* Testing hook: the next `calls` calls of isoloco_distill (from any thread) do not bring their rows to shared memory where their kernel
+ * holds them there; its waits for them give up after 20 ms.  Returns OK or INVALID. */
+int isoloco_debug_lose_rows(int calls);
 
 /* Thread-local message describing the last error returned on this thread. */
 const char* isoloco_last_error(void);

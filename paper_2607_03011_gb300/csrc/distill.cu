@@ -55,6 +55,7 @@ constexpr int held_ctas(int threads) { return threads == 64 ? 11 : threads == 12
 constexpr int stream_ctas(int threads) { return threads == 64 ? 14 : threads == 128 ? 8 : 5; }
 // Entries of a share whose marks (of the list's tokens) are kept apart.
 constexpr uint32_t marks_of(int threads) { return threads <= 128 ? 16384 : 65536; }
+constexpr uint64_t kLostNs = 20000000;  // the limit of a wait for a row whose copy is not started (DistillArgs::lost)
 constexpr float kSmallRest = 0.0625f;
 // Vectors per thread of the gradient by itself: 8192 x 128000 bf16 657 us (the copy rate allows 628); 16 667, 8 769, 4 869 (a list for
 // every span).
@@ -659,22 +660,25 @@ __global__ void __launch_bounds__(THREADS + 32, held_ctas(THREADS)) k_distill_he
         mbar_init(&bar, 1);
         fence_mbar_init();
         mbar_arrive_expect_tx(&bar, nvec * 16u);
-        bulk_load(held, x - lead, nvec * 16u, &bar);
+        if (!a.lost) bulk_load(held, x - lead, nvec * 16u, &bar);
     }
     __syncthreads();  // (nobody waits for a barrier that is not set up)
     const float c = a.scale * kLog2e;
     const float grad_loss = a.grad_loss[r];
-    auto wait_row = [&] {
-        if (!mbar_wait(&bar, 0u)) {
-            if ((threadIdx.x & 31) == 0) atomicOr(err, kErrTimeout);
-            drain_barriers(1, [&](int, uint64_t*& b, uint32_t& parity) { return b = &bar, parity = 0u, true; });
+    // whether the row is there; where it is not, what is summed is NaN, and so the row's results are
+    auto wait_row = [&]() -> bool {
+        const bool there = mbar_wait(&bar, 0u, a.lost ? kLostNs : kWaitTimeoutNs);
+        if (!there) {
+            atomicOr(err, kErrTimeout);
+            drain_barriers(1, [&](int, uint64_t*& b, uint32_t& parity) { return b = &bar, parity = 0u, !a.lost; });
         }
         __syncwarp();  // (barriers are passed by whole warps)
+        return there;
     };
     if (threadIdx.x >= THREADS) {
         const uint32_t lane = threadIdx.x & 31;
         warp_read<T>(a, r, sm);
-        wait_row();
+        const bool there = __all_sync(0xffffffffu, wait_row());
         T* mine = reinterpret_cast<T*>(held);
         if (REST)
             for (int e = lane; e < a.k; e += 32)
@@ -683,7 +687,8 @@ __global__ void __launch_bounds__(THREADS + 32, held_ctas(THREADS)) k_distill_he
         if (lane < nvec * V - end) mine[end + lane] = from_f32<T>(-INFINITY);
         __syncwarp();
         bar_arrive<kMasked>(kAll);
-        const List l = warp_sums<REST>(a, c, sm);
+        List l = warp_sums<REST>(a, c, sm);
+        if (!there) l.weight = NAN;
         if (lane == 0) list_out = l;
         __syncwarp();
         bar_arrive<kListed>(kAll);
@@ -706,7 +711,7 @@ __global__ void __launch_bounds__(THREADS + 32, held_ctas(THREADS)) k_distill_he
         return;
     }
     const F2 c2 = pair(c, c);
-    wait_row();
+    const bool there = wait_row();
     bar_sync<kMasked>(kAll);
     float m = -FLT_MAX;
     F2 s2 = pair(0.f, 0.f);
@@ -732,7 +737,7 @@ __global__ void __launch_bounds__(THREADS + 32, held_ctas(THREADS)) k_distill_he
     uint32_t i = threadIdx.x;
     for (; i + (kUnroll - 1) * THREADS < nvec; i += kUnroll * THREADS) batch(i, std::true_type());
     if (i < nvec) batch(i, std::false_type());
-    Sum o = {m, both(s2)};
+    Sum o = {m, there ? both(s2) : NAN};
     __syncwarp();
     o.lanes<32>(c);
     if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = o;

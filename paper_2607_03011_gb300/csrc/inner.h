@@ -72,6 +72,7 @@ struct DistillArgs {
     const float* grad_loss;
     void* grad_logits;
     int64_t ld_grad;
+    bool lost;  // rows that are held in shared memory are not brought there (isoloco_debug_lose_rows)
 };
 cudaError_t launch_distill(const DistillArgs& a, cudaStream_t st);
 // a.saved is read; a.loss is not written

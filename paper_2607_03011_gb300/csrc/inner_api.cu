@@ -1,5 +1,6 @@
 // inner_api.cu -- C entry points of the inner step's operators: argument checks, then the launchers.
 #include <algorithm>
+#include <atomic>
 #include <climits>
 #include <string>
 #include <vector>
@@ -32,6 +33,8 @@ cudaError_t error_word(uint32_t** word) {
 using namespace isoloco;
 
 namespace {
+
+std::atomic<int> g_lose_rows{0};  // calls still to be made without their rows' copies (isoloco_debug_lose_rows)
 
 constexpr int64_t kMaxSize = INT_MAX;
 // No exception passes an entry point: what may be thrown here is for want of memory (a message's text).
@@ -381,10 +384,11 @@ int isoloco_distill(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype
                     const void* top_logp, int64_t ld_logp, isoloco_dtype_t logp_dtype, const void* top_index,
                     int64_t ld_index, int index_bytes, int k, float scale, isoloco_tail_t tail, float* loss, float* saved,
                     const float* grad_loss, void* grad_logits, int64_t ld_grad, void* stream) try {
-    const DistillArgs a = {logits, ld_logits, rows, vocab, dtype, top_logp, ld_logp, logp_dtype, top_index, ld_index,
-                           index_bytes == 8, k, scale, tail == ISOLOCO_TAIL_REST, loss, saved, grad_loss, grad_logits, ld_grad};
+    DistillArgs a = {logits, ld_logits, rows, vocab, dtype, top_logp, ld_logp, logp_dtype, top_index, ld_index,
+                     index_bytes == 8, k, scale, tail == ISOLOCO_TAIL_REST, loss, saved, grad_loss, grad_logits, ld_grad, false};
     if (const char* p = distill_problem(a, index_bytes, tail)) return invalid(p);
     if (!array_ok(loss, rows, 4)) return invalid("loss is NULL or misaligned");
+    a.lost = g_lose_rows.load(std::memory_order_relaxed) > 0 && g_lose_rows.fetch_sub(1) > 0;
     return cuda_status(launch_distill(a, stream_of(stream)));
 } catch (...) {
     return kNoMemory;
@@ -396,7 +400,7 @@ int isoloco_distill_grad(const float* grad_loss, const void* logits, int64_t ld_
                          const float* saved, void* grad_logits, int64_t ld_grad, void* stream) try {
     const DistillArgs a = {logits, ld_logits, rows, vocab, dtype, top_logp, ld_logp, logp_dtype, top_index, ld_index,
                            index_bytes == 8, k, scale, tail == ISOLOCO_TAIL_REST, nullptr, const_cast<float*>(saved), grad_loss,
-                           grad_logits, ld_grad};
+                           grad_logits, ld_grad, false};
     if (rows > 0 && !grad_logits) return invalid("grad_logits is NULL");
     if (const char* p = distill_problem(a, index_bytes, tail)) return invalid(p);
     if (!array_ok(saved, rows, 4)) return invalid("saved is NULL or misaligned");
@@ -489,6 +493,12 @@ int isoloco_inner_status(void* stream) try {
     return (bits & kErrTimeout) ? set_error(ISOLOCO_ERR_TIMEOUT, "a wait in an inner-step kernel gave up") : ISOLOCO_OK;
 } catch (...) {
     return kNoMemory;
+}
+
+int isoloco_debug_lose_rows(int calls) {
+    if (calls < 0) return ISOLOCO_ERR_INVALID;
+    g_lose_rows = calls;
+    return ISOLOCO_OK;
 }
 
 int isoloco_debug_raise_inner(void* stream) try {

@@ -1,0 +1,7 @@
+"""The testing hooks of distillation refuse what makes no sense (no GPU needed)."""
+
+
+def test_lose_rows():
+    from paper_2607_03011_gb300 import isoloco
+    L = isoloco.lib()
+    assert L.isoloco_debug_lose_rows(-1) == isoloco.ERR_INVALID and L.isoloco_debug_lose_rows(0) == isoloco.OK
