@@ -551,6 +551,10 @@ int isoloco_debug_raise_inner(void* stream);
  * holds them there; its waits for them give up after 20 ms.  Returns OK or INVALID. */
 int isoloco_debug_lose_rows(int calls);
 
+/* Testing hook: while `refuse` is 1, isoloco_beam_select takes clusters of more than 8 CTAs as not fitting the device, as a restricted
+ * share of a GPU may not have room for them, and makes smaller ones, with the same results; 0: as the device says. */
+int isoloco_debug_refuse_clusters(int refuse);
+
 /* Thread-local message describing the last error returned on this thread. */
 const char* isoloco_last_error(void);
 

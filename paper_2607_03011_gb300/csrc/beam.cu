@@ -11,6 +11,7 @@
 // Every row is cut in the same places, counted from its first entry, wherever that lies: beams with equal logits and
 // scores get equal totals to the last bit, and rank by their numbers.
 #include <algorithm>
+#include <atomic>
 #include <cfloat>
 #include <type_traits>
 
@@ -467,17 +468,45 @@ int unit_of(const isoloco_state_t& s, int64_t batch, int width) {
 
 namespace {
 
+std::atomic<int> g_refuse_clusters{0};
+
+// Whether clusters of kMaxCtas CTAs can run on the current device (a restricted share of a GPU may not have room for them).
+template <class T, int THREADS>
+cudaError_t large_clusters(bool* fit) {
+    static PerDevice known;
+    int dev = 0, n = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess)
+        e = known.get<cudaError_t>(dev, &n, [](int* clusters) {
+            *clusters = 0;
+            cudaLaunchAttribute at[1];
+            at[0].id = cudaLaunchAttributeClusterDimension;
+            at[0].val.clusterDim.x = kMaxCtas;
+            at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(kMaxCtas);
+            cfg.blockDim = dim3(THREADS);
+            cfg.attrs = at;
+            cfg.numAttrs = 1;
+            cudaError_t r = cudaFuncSetAttribute(k_beam_select<T, THREADS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+            if (r == cudaSuccess) r = cudaOccupancyMaxActiveClusters(clusters, k_beam_select<T, THREADS>, &cfg);
+            if (r != cudaSuccess) {  // (refused altogether: smaller ones are made; what else is wrong shows at the launch)
+                *clusters = 0;
+                cudaGetLastError();
+            }
+            return cudaSuccess;
+        });
+    *fit = n > 0 && g_refuse_clusters.load(std::memory_order_relaxed) == 0;
+    return e;
+}
+
 template <class T, int THREADS>
 cudaError_t launch_select(const BeamArgs& a, int split, int ctas, cudaStream_t st) {
     if (ctas > 8) {
-        static PerDevice ready;
-        int dev = 0, set = 0;
-        cudaError_t e = cudaGetDevice(&dev);
-        if (e == cudaSuccess)
-            e = ready.get<cudaError_t>(dev, &set, [](int*) {
-                return cudaFuncSetAttribute(k_beam_select<T, THREADS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-            });
+        bool fit = false;
+        const cudaError_t e = large_clusters<T, THREADS>(&fit);
         if (e != cudaSuccess) return e;
+        if (!fit) ctas = 8;  // (which every device runs; the rows are cut in the same places)
     }
     const uint32_t per = static_cast<uint32_t>(((a.vocab + split - 1) / split + 63) & ~int64_t(63));
     const int64_t most = int64_t(1) << 27;  // batch entries of a grid
@@ -528,6 +557,8 @@ cudaError_t select(const BeamArgs& a, cudaStream_t st) {
 cudaError_t launch_beam_select(const BeamArgs& a, cudaStream_t st) {
     return a.dtype == ISOLOCO_F32 ? select<float>(a, st) : a.dtype == ISOLOCO_BF16 ? select<__nv_bfloat16>(a, st) : select<__half>(a, st);
 }
+
+void refuse_large_clusters(bool refuse) { g_refuse_clusters = refuse; }
 
 cudaError_t launch_beam_reorder(const isoloco_state_t* states, int count, int64_t batch, int width, const void* beams,
                                 bool ids64, cudaStream_t st) {

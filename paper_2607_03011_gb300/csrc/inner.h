@@ -90,6 +90,8 @@ struct BeamArgs {
     uint8_t* out_finished;
 };
 cudaError_t launch_beam_select(const BeamArgs& a, cudaStream_t st);
+// From now on clusters of more than 8 CTAs are taken as not fitting, or as the device says (isoloco_debug_refuse_clusters).
+void refuse_large_clusters(bool refuse);
 
 cudaError_t launch_beam_reorder(const isoloco_state_t* states, int count, int64_t batch, int width, const void* beams,
                                 bool ids64, cudaStream_t st);

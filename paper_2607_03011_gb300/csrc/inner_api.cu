@@ -501,6 +501,12 @@ int isoloco_debug_lose_rows(int calls) {
     return ISOLOCO_OK;
 }
 
+int isoloco_debug_refuse_clusters(int refuse) {
+    if (refuse != 0 && refuse != 1) return ISOLOCO_ERR_INVALID;
+    refuse_large_clusters(refuse == 1);
+    return ISOLOCO_OK;
+}
+
 int isoloco_debug_raise_inner(void* stream) try {
     uint32_t* word = nullptr;
     cudaError_t e = error_word(&word);
