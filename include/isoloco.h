@@ -492,7 +492,8 @@ int isoloco_distill_grad(const float* grad_loss, const void* logits, int64_t ld_
  *   logits: batch * beams rows x vocab of `dtype`; scores: batch x beams fp32; finished: batch x beams bytes;
  *   1 <= beams <= ISOLOCO_MAX_BEAMS, 1 <= keep <= min(beams * vocab, ISOLOCO_MAX_TOP); `end`: a token, or negative for
  *   none (finished must then be NULL); out_scores (fp32), out_beams, out_tokens (int64): batch x keep; out_finished (may
- *   be NULL): batch x keep bytes, 1 where the beam continued was finished or the token is `end`. */
+ *   be NULL): batch x keep bytes, 1 where the beam continued was finished or the token is `end`.  Outputs share no memory with one
+ *   another or with inputs, but where keep == beams out_scores may be scores and out_finished finished. */
 #define ISOLOCO_MAX_BEAMS 32
 int isoloco_beam_select(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t batch, int64_t beams,
                         int64_t vocab, const float* scores, const uint8_t* finished, int64_t end, float scale, int keep,

@@ -287,10 +287,12 @@ __device__ __forceinline__ void merge(const BeamArgs& a, int64_t b, uint32_t liv
     const int64_t at = b * a.keep + lane;
     const uint32_t token = token_of(from, at_p);
     const int w = beam[from];
+    const bool was = a.finished && a.finished[b * a.beams + w];
+    __syncwarp(a.keep == 32 ? 0xffffffffu : (1u << a.keep) - 1);  // (out_finished may be finished)
     a.out_scores[at] = kinds[from] == kNan ? NAN : static_cast<float>(total_of(from, at_p));
     a.out_beams[at] = w;
     a.out_tokens[at] = token;
-    if (a.out_finished) a.out_finished[at] = (a.finished && a.finished[b * a.beams + w]) || static_cast<int64_t>(token) == a.end;
+    if (a.out_finished) a.out_finished[at] = was || static_cast<int64_t>(token) == a.end;
 }
 
 // A cluster of `ctas` CTAs per batch entry: the live beams' rows, each in `split` shares of `per_share` entries (a multiple of 64), are dealt

@@ -143,6 +143,29 @@ const char* distill_problem(const DistillArgs& a, int index_bytes, int tail) {
     return nullptr;
 }
 
+// Whether outputs of a selection share memory with one another or with scores or finished; where as many continuations are kept as there are
+// beams, a batch entry writes the same places of scores and finished that it alone has read.
+bool selection_shares(const BeamArgs& a) {
+    struct Range {
+        const void* p;
+        int64_t bytes;
+        bool meets(const Range& o) const {
+            const uint64_t at = reinterpret_cast<uint64_t>(p), other = reinterpret_cast<uint64_t>(o.p);
+            return p && o.p && at < other + static_cast<uint64_t>(o.bytes) && other < at + static_cast<uint64_t>(bytes);
+        }
+    };
+    const int64_t read = a.batch * a.beams, made = a.batch * a.keep;
+    const Range in[2] = {{a.scores, read * 4}, {a.finished, read}};
+    const Range out[4] = {{a.out_scores, made * 4}, {a.out_finished, made}, {a.out_beams, made * 8}, {a.out_tokens, made * 8}};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < 2; ++j)
+            if (out[i].meets(in[j]) && !(i == j && out[i].p == in[j].p && a.keep == a.beams)) return true;
+        for (int j = 0; j < i; ++j)
+            if (out[i].meets(out[j])) return true;
+    }
+    return false;
+}
+
 // ---- states that are reordered: what they may share
 
 // The addresses of one side of a state.
@@ -425,6 +448,7 @@ int isoloco_beam_select(const void* logits, int64_t ld_logits, isoloco_dtype_t d
         return invalid("out_scores, out_beams or out_tokens is NULL or misaligned");
     const BeamArgs a = {logits, ld_logits, batch, vocab, end < 0 ? -1 : end, dtype, static_cast<int>(beams), keep, scores, finished, scale,
                         out_scores, out_beams, out_tokens, out_finished};
+    if (selection_shares(a)) return invalid("outputs share memory with one another, or with scores or finished otherwise than in place");
     return cuda_status(launch_beam_select(a, stream_of(stream)));
 } catch (...) {
     return kNoMemory;
