@@ -90,7 +90,7 @@ struct Sum {
 
 // A share's sums and its k largest entries, to list `at` of the cluster's first CTA.
 template <class T, int THREADS>
-__device__ __forceinline__ void search(const Part<T>& sh, int k, float c, TopSmem<1>& sm, Sum* sums, Lists& lists, int at, bool remote, bool& wait) {
+__device__ __forceinline__ void search(const Part<T>& sh, int k, float c, TopSmem<1, THREADS>& sm, Sum* sums, Lists& lists, int at, bool remote, bool& wait) {
     constexpr int V = Vec<T>::kN;
     float m = -FLT_MAX, bv = -INFINITY, second = -INFINITY;  // the largest entry, and of the other vectors (and single entries)
     uint32_t bi = 0xffffffffu;
@@ -299,7 +299,7 @@ __device__ __forceinline__ void merge(const BeamArgs& a, int64_t b, uint32_t liv
 // among them, and the first merges.
 template <class T, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_beam_select(BeamArgs a, int ctas, int split, uint32_t per_share) {
-    __shared__ TopSmem<1> sm;
+    __shared__ TopSmem<1, THREADS> sm;
     __shared__ Lists lists;
     __shared__ Sum sums[THREADS / 32];
     const int rank = ctas > 1 ? static_cast<int>(cluster_ctarank()) : 0;

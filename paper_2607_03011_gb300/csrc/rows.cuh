@@ -106,37 +106,31 @@ __device__ __forceinline__ uint64_t rank_key(float v, uint32_t idx) {
     return (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~idx);
 }
 
-constexpr int kGroups = 64;         // of threads, at least 2 ISOLOCO_MAX_TOP
-constexpr int kCandidates = 1024;   // entries a CTA ranks: all that a row of equal logits gives, 32 per group and `top`
+constexpr int kGroups = 64;  // of threads, at least 2 ISOLOCO_MAX_TOP
+// Entries a CTA ranks: all that a row of equal logits gives, a vector of up to 8 of each thread of `top` groups.
+constexpr int candidates_of(int threads) { return ISOLOCO_MAX_TOP * 8 * (threads > 256 ? threads : 256) / kGroups; }
 
-// What the search for a CTA's largest entries needs, and LISTS results.
-template <int LISTS>
+// What the search for the largest entries of a CTA of THREADS (or of up to 256) needs, and LISTS results.
+template <int LISTS, int THREADS = 256>
 struct TopSmem {
     uint64_t group[kGroups];
     uint64_t bound;
     int count, threads;
-    uint16_t thread[512];  // those whose entries may reach the bound
-    uint64_t cand[kCandidates];
+    uint16_t thread[THREADS];  // those whose entries may reach the bound
+    uint64_t cand[candidates_of(THREADS)];
     uint64_t best[LISTS][ISOLOCO_MAX_TOP];
 };
 
-// The CTA's k largest entries, in order, to best[0 .. k) (keys; 0 where there are fewer).  bv, bi: this
-// thread's largest value and an index not below its first place.
-template <class T, int THREADS, class Smem, class Share>
-__device__ __forceinline__ void top_of_cta(Smem& sm, const Share& sh, int k, float bv, uint32_t bi, float second, uint64_t* best) {
-    constexpr int kPer = THREADS / kGroups, V = Vec<T>::kN;
-    // keys not above and not below that of the thread's largest entry, which lies within a vector of bi
-    const bool any = bi != 0xffffffffu;
-    const uint64_t least = any ? rank_key(bv, sh.first + bi) : 0, most = any ? rank_key(bv, sh.first + (bi >= V - 1 ? bi - (V - 1) : 0)) : 0;
-    uint64_t g = least;
+// sm.bound: the k-th largest of the groups' largest g.
+template <int THREADS, class Smem>
+__device__ __forceinline__ void make_bound(Smem& sm, int k, uint64_t g) {
+    constexpr int kPer = THREADS / kGroups;
 #pragma unroll
     for (int o = 1; o < kPer; o <<= 1) {
         const uint64_t other = __shfl_xor_sync(0xffffffffu, g, o);
         g = other > g ? other : g;
     }
     if (threadIdx.x % kPer == 0) sm.group[threadIdx.x / kPer] = g;
-    if (threadIdx.x == 0) sm.count = sm.threads = 0;
-    if (threadIdx.x < k) best[threadIdx.x] = 0;
     __syncthreads();
     {
         // ranks of the groups: kPer threads each count a share of the greater ones
@@ -153,6 +147,19 @@ __device__ __forceinline__ void top_of_cta(Smem& sm, const Share& sh, int k, flo
         if (r == k - 1) sm.bound = own;
     }
     __syncthreads();
+}
+
+// The CTA's k largest entries, in order, to best[0 .. k) (keys; 0 where there are fewer).  bv, bi: this
+// thread's largest value and an index not below its first place.
+template <class T, int THREADS, class Smem, class Share>
+__device__ __forceinline__ void top_of_cta(Smem& sm, const Share& sh, int k, float bv, uint32_t bi, float second, uint64_t* best) {
+    constexpr int V = Vec<T>::kN, kCandidates = candidates_of(THREADS);
+    // keys not above and not below that of the thread's largest entry, which lies within a vector of bi
+    const bool any = bi != 0xffffffffu;
+    const uint64_t least = any ? rank_key(bv, sh.first + bi) : 0, most = any ? rank_key(bv, sh.first + (bi >= V - 1 ? bi - (V - 1) : 0)) : 0;
+    if (threadIdx.x == 0) sm.count = sm.threads = 0;
+    if (threadIdx.x < k) best[threadIdx.x] = 0;
+    make_bound<THREADS>(sm, k, least);
     const uint64_t bound = sm.bound;
     auto look = [&](float v, uint32_t i) {
         if (v != v) return;  // NaN ranks nowhere
@@ -170,7 +177,7 @@ __device__ __forceinline__ void top_of_cta(Smem& sm, const Share& sh, int k, flo
 #pragma unroll
         for (int j = 0; j < V; ++j) look(f[j], sh.head + i * V + j);
     };
-    static_assert(THREADS <= 512, "TopSmem::thread");
+    static_assert(sizeof(sm.thread) >= 2 * THREADS && sizeof(sm.cand) >= 8 * kCandidates, "TopSmem");
     if (any && most >= bound) {
         // the vector with the thread's largest entry, or, where another of its vectors may reach the bound, all of them
         if (rank_key(second, 0) >= bound) sm.thread[atomicAdd(&sm.threads, 1)] = static_cast<uint16_t>(threadIdx.x);
@@ -186,7 +193,27 @@ __device__ __forceinline__ void top_of_cta(Smem& sm, const Share& sh, int k, flo
     if (threadIdx.x < sh.head) look(to_f32(sh.x[threadIdx.x]), threadIdx.x);
     if (threadIdx.x < sh.n - sh.tail()) look(to_f32(sh.x[sh.tail() + threadIdx.x]), sh.tail() + threadIdx.x);
     __syncthreads();
-    const int n = sm.count;
+    int n = sm.count;
+    if constexpr (THREADS > 256)
+        if (n > kGroups * 4 && n <= kCandidates) {
+            // Many equal entries (all tokens masked but a few): a bound once more, from the candidates (k groups or more have some, in any order).
+            // 1 x 4 x 50021 fp16, 8 tokens left, 32 kept: 20 us, 108 where all candidates are ranked against each other, and 72 one at a time.
+            constexpr int kOwn = kCandidates / THREADS;
+            uint64_t own[kOwn], most_own = 0;
+#pragma unroll
+            for (int u = 0; u < kOwn; ++u) {
+                own[u] = threadIdx.x + u * THREADS < n ? sm.cand[threadIdx.x + u * THREADS] : 0;
+                most_own = own[u] > most_own ? own[u] : most_own;
+            }
+            make_bound<THREADS>(sm, k, most_own);
+            if (threadIdx.x == 0) sm.count = 0;
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < kOwn; ++u)
+                if (own[u] && own[u] >= sm.bound) sm.cand[atomicAdd(&sm.count, 1)] = own[u];
+            __syncthreads();
+            n = sm.count;
+        }
     if (n <= kCandidates) {
         for (int i = threadIdx.x; i < n; i += THREADS) {
             const uint64_t own = sm.cand[i];
