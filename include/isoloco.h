@@ -462,7 +462,8 @@ int isoloco_token_logprobs_grad(const void* logits, int64_t ld_logits, isoloco_d
  * altogether the gradient is 0.  A NaN or +inf among a row's logits, or in an entry's top_logp, makes its loss and gradient NaN.
  *   logits: rows x vocab of `dtype` (16-byte pieces that hold a row's ends are read whole); top_logp: rows x k of
  *   logp_dtype; top_index: rows x k of index_bytes (4 or 8), signed; 1 <= k <= ISOLOCO_MAX_LIST; loss: rows fp32; saved (may
- *   be NULL): rows x 6 fp32, for isoloco_distill_grad; scale > 0.
+ *   be NULL): rows x 6 fp32, for isoloco_distill_grad; scale > 0.  Nothing that is written shares memory with anything else, but for
+ *   grad_logits as said below.
  * With grad_logits (rows x vocab of `dtype`, pitch ld_grad; may be the logits themselves, at their pitch, else NULL) the
  * call also writes the gradient of sum_r grad_loss[r] loss[r] (grad_loss: rows fp32). */
 #define ISOLOCO_MAX_LIST 256
@@ -472,7 +473,8 @@ int isoloco_distill(const void* logits, int64_t ld_logits, isoloco_dtype_t dtype
                     int64_t ld_index, int index_bytes, int k, float scale, isoloco_tail_t tail, float* loss, float* saved,
                     const float* grad_loss, void* grad_logits, int64_t ld_grad, void* stream);
 
-/* The same gradient by itself, from what an earlier call on the same operands saved. */
+/* The same gradient by itself, from what an earlier call on the same operands saved.  Entries outside the list may differ from isoloco_distill's
+ * in their last place: that divides with quotients good to two units in the last place, this by exact ones. */
 int isoloco_distill_grad(const float* grad_loss, const void* logits, int64_t ld_logits, isoloco_dtype_t dtype, int64_t rows,
                          int64_t vocab, const void* top_logp, int64_t ld_logp, isoloco_dtype_t logp_dtype,
                          const void* top_index, int64_t ld_index, int index_bytes, int k, float scale, isoloco_tail_t tail,
@@ -484,12 +486,13 @@ int isoloco_distill_grad(const float* grad_loss, const void* logits, int64_t ld_
  * The `keep` largest totals, largest first; among equal ones the lower beam, then the larger logit, then the lower token
  * comes first.  Totals are compared in 64 bits before they are rounded to fp32; the logarithms in them are good to some
  * 1e-7, and are the same bits for beams with equal logits.
- * Masked tokens (logits of -inf or the type's lowest value), a finished beam's other tokens and all tokens of a beam whose
+ * Masked tokens (logits of -inf or the type's lowest value; F16's -65504 still counts in the sum of a row where scale is below
+ * 0.002), a finished beam's other tokens and all tokens of a beam whose
  * score is -inf or whose tokens are all masked have the total -inf and rank by beam and token, so that there are
  * always `keep` answers (among the masked tokens of a beam that has others the type's lowest value ranks before -inf).  A beam whose
  * score is NaN or +inf, or which is not finished and has a NaN or +inf among its logits, ranks like one of score -inf, and its
  * totals are given as NaN.
- *   logits: batch * beams rows x vocab of `dtype`; scores: batch x beams fp32; finished: batch x beams bytes;
+ *   logits: batch * beams rows x vocab of `dtype` (16-byte pieces that hold a row's ends are read whole); scores: batch x beams fp32; finished: batch x beams bytes;
  *   1 <= beams <= ISOLOCO_MAX_BEAMS, 1 <= keep <= min(beams * vocab, ISOLOCO_MAX_TOP); `end`: a token, or negative for
  *   none (finished must then be NULL); out_scores (fp32), out_beams, out_tokens (int64): batch x keep; out_finished (may
  *   be NULL): batch x keep bytes, 1 where the beam continued was finished or the token is `end`.  Outputs share no memory with one
@@ -514,8 +517,8 @@ typedef struct {
  * memory with anything else of the call: destinations that overlap themselves, another state's memory, or
  * cannot be told apart from it by their addresses and strides are refused.
  *   states: HOST array of `count` entries, read during the call; beams: batch x width entries of id_bytes (4 or 8);
- *   1 <= width <= ISOLOCO_MAX_BEAMS; strides not negative.  Addresses, strides and runs that are multiples of 16 bytes run
- *   faster. */
+ *   1 <= width <= ISOLOCO_MAX_BEAMS; strides not negative; of a source that is not reordered in place, 16-byte pieces that hold a run's ends
+ *   may be read whole.  Addresses, strides and runs that are multiples of 16 bytes run faster. */
 int isoloco_beam_reorder(const isoloco_state_t* states, int count, int64_t batch, int64_t width, const void* beams,
                          int id_bytes, void* stream);
 

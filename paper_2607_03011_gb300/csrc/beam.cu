@@ -3,10 +3,11 @@
 // Selection: with M the largest logit of beam w's row and S = sum e^{scale (x - M)}, a continuation by t has the total
 // score_w + scale (x_t - M) - ln S.  Within a beam the totals rank as the logits do, so each row gives its `keep` largest logits
 // (found as token_logprobs finds them) and its two sums, in one pass, and the batch entry's best are merged from those lists.
-// What bounds it: for few rows the chain of loads, reductions and barriers (1 x 4 x 32000 bf16 10.4 us: 2.2 thousand cycles for the row,
+// What bounds it: for few rows the chain of loads, reductions and barriers (1 x 4 x 32000 bf16 10.3 us: 2.2 thousand cycles for the row,
 // 4 for its search, 4 for the cluster's barrier, 5 for the merging); for many the loads in flight and what SMs have left to do when
 // others are done (64 x 16 x 128000 bf16 60 us, 3.9 TB/s: the 922 rows that are read are 6.07 to an SM, in CTAs of two).  The
-// merging in a launch of its own, with a CTA per row, took 63.
+// merging in a launch of its own, with a CTA per row, took 63.  (Calls in graphs of their own, one after the other; "in a row" below: of many
+// calls in one graph, where a call takes some 3 us less.)
 //
 // Every row is cut in the same places, counted from its first entry, wherever that lies: beams with equal logits and
 // scores get equal totals to the last bit, and rank by their numbers.
@@ -336,8 +337,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_beam_select(BeamArg
 
 constexpr int kStates = 32;               // of a launch
 constexpr double kShiftLeast = 1 << 20;  // bytes
-// CTAs per SM that the registers are cut for (3.2 GB of 16-byte units, us with 5, 4 and 3 CTAs): four beams 408, 449, 449; eight 748, 738, 834 (6.8
-// TB/s read and written), 1066 where every beam's address has registers of its own; twelve 695, 644, 549; sixteen 914, 823, 721.
+// CTAs per SM that the registers are cut for, us with 5, 4, 3 and 2 of them (GB read and written in 16-byte units): four beams (4.73) 786, 866, 865, 865; eight
+// (4.68) 703, 690, 776, 985, half as much again where every beam's address has registers of its own; twelve (4.66) 883, 816, 705, 851; sixteen (4.96)
+// 916, 831, 728, 850; twenty-four (4.71) 1442, 1215, 1137, 881; thirty-two (4.96) 1497, 1263, 1122, 893.  At these cuts the beams' units do not all
+// stay in registers: of 4, 8, 16 and 32 beams a thread spills 24, 104, 320 and 752 bytes, and moves 64 to 512.  8 and 16 beams reach 6.8 TB/s, 17
+// to 32 5.3 to 5.5.
 constexpr int reorder_ctas(int width) { return width <= 4 ? 5 : width <= 8 ? 4 : width <= 16 ? 3 : 2; }
 struct StateArgs {
     const char* src;
@@ -542,15 +546,16 @@ cudaError_t select(const BeamArgs& a, cudaStream_t st) {
     const cudaError_t e = device_sms(&sms);
     if (e != cudaSuccess) return e;
     // A row in two, four, eight or sixteen shares while a batch entry's CTAs have one each, all run at once, and shares have
-    // 4096 entries (64 x 4 x 32000 fp32 14.8 us, 16.6 in whole rows; 1 x 4 x 128000 bf16 10.5 us, 12.4 in half as many shares,
-    // and 20 where a CTA takes four shares one after the other).
+    // 4096 entries (in a row: 64 x 4 x 32000 fp32 11.4 us, 12.9 in whole rows; 1 x 4 x 128000 bf16 7.8 and 11.2; 16 x 8 x 50021 fp16 15.2 and 16.7).
     int split = 1;
     while (a.beams * split * 2 <= kMaxCtas && a.batch * a.beams * split * 2 <= 4 * sms && a.vocab / (2 * split) >= 4096) split *= 2;
-    // Clusters of up to 16 while all of their CTAs run at once, or where CTAs of 8 would have unequal shares (32 x 16 x 128000
-    // bf16 35 us, 46 with clusters of 8; 100 x 10 x 32000 29 and 38); else of 8 (64 x 16 x 128000 60 us, 73 with 16).
+    // Clusters of up to 16 while all of their CTAs run at once, or where CTAs of 8 would have unequal shares (in a row: 32 x 16 x 128000
+    // bf16 34 us, 43 with clusters of 8; 100 x 10 x 32000 26 and 36); else of 8 (64 x 16 x 128000 57 us, 70 with 16).
     const int units = a.beams * split;
     const int ctas = units <= 8 || (units % 8 == 0 && a.batch * units > 4 * sms) ? std::min(8, units) : std::min(kMaxCtas, units);
-    // 512 threads where an SM has no more than one CTA: 16 x 8 x 50021 fp16 18.7 us, 20.6 with 256 (64 x 5 x 32000 fp32, two CTAs to an SM, 20.6 and 15.2).
+    // 512 threads where an SM has no more than one CTA, for long shares (in a row, with 512 and 256 threads: 9 x 16 x 128000 bf16 19.6 and 23.2, fp32 24.6
+    // and 32.8; 4 x 32 x 128000 25.9 and 34.3; 8 x 8 x 50021 fp16 13.5 with either; short ones lose, 9 x 16 x 32000 bf16 12.2 and 11.5, 8 x 16 x 1000
+    // 10.6 and 9.2); 256 where it has more (64 x 5 x 32000 fp32 19.9 and 15.2; 16 x 8 x 50021 19.3 and 15.2).
     return a.batch * ctas <= sms ? launch_select<T, 512>(a, split, ctas, st) : launch_select<T, 256>(a, split, ctas, st);
 }
 
@@ -573,9 +578,9 @@ cudaError_t launch_beam_reorder(const isoloco_state_t* states, int count, int64_
         a.beams = beams;
         a.first[0] = 0;
     }
-    // By shifted pieces, where there is enough of it to pay for a launch of its own (4 us), what no 16-byte unit divides: 29 MB of fp32 rows
-    // of 33 26 us, by units of 4 87.  In place by units: a thread's places of two beams, cut at their own boundaries, would not be
-    // the same.
+    // By shifted pieces, where there is enough of it to pay for a launch of its own (4 us), what no 16-byte unit divides: 3 x 5 beams, 55 MB of fp32 rows
+    // of 33 written, 27 us (3.6 TB/s read and written: beams go in groups of four, so five take two rounds of loads and stores), by units of 4 73.  In
+    // place by units, 62: a thread's places of two beams, cut at their own boundaries, would not be the same.
     auto may_shift = [](const isoloco_state_t& s, int unit) { return s.src != s.dst && unit < 16 && s.run >= 64 && s.run < (1 << 30); };
     double large = 0.0;
     for (int i = 0; i < count; ++i)
