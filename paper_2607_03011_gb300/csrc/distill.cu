@@ -348,13 +348,13 @@ __device__ __forceinline__ void warp_read(const DistillArgs& a, int64_t r, ListS
 // 1 - sum e^logp, w the sum in fp32.  That is off by some 2^-22, which is nothing beside a large rest, but all of one that a teacher
 // leaves whose list holds nearly everything; rests below kSmallRest are made good to 2^-43 for each entry.  e^v - 1 = hi + lo, two fp32 numbers:
 // Taylor's series at v / 1024, then ten times (1 + p)^2 - 1 = 2 p + p^2, with the roundings of hi + hi + hi^2 kept in lo (off by 2^-44 at most over
-// 800000 numbers tried); the sums as whole numbers of 2^-22 and 2^-45.  8192 x 32000 bf16, lists of 32: 185 us where all rests are small, 178 where
+// 800000 numbers tried); the sums as whole numbers of 2^-22 and 2^-45.  8192 x 32000 bf16, lists of 32: 185 us where all rests are small, 180 where
 // none is; with 64-bit floating point, of which an SM makes two operations a cycle, 193.
 __device__ __forceinline__ float left_of(const DistillArgs& a, float w, ListSmem& sm) {
     if (!(1.f - w < kSmallRest)) return 1.f - w;
     constexpr int kTimes = 10;
     constexpr float kCoarse = 1 << 22, kFine = 35184372088832.f;
-    int coarse = 0, fine = 0, count = 0;  // (of 256 entries: at most 2^30, 2^30 and 2^8)
+    int coarse = 0, fine = 0;  // (of 256 entries: at most 2^30 each)
 #pragma unroll 1
     for (int e = threadIdx.x & 31; e < a.k; e += 32) {
         const float v = fminf(sm.logp[e], 0.f);  // (one above 0 leaves nothing as it is)
@@ -370,14 +370,12 @@ __device__ __forceinline__ float left_of(const DistillArgs& a, float w, ListSmem
             lo = __fadd_rn(__fadd_rn(top, -hi), l);
         }
         const int n = __float2int_rn(hi * kCoarse);
-        coarse += n;
+        coarse += n + (1 << 22);
         fine += __float2int_rn((fmaf(static_cast<float>(n), -1.f / kCoarse, hi) + lo) * kFine);
-        ++count;
     }
     coarse = __reduce_add_sync(0xffffffffu, coarse);
     fine = __reduce_add_sync(0xffffffffu, fine);
-    count = __reduce_add_sync(0xffffffffu, count);
-    const long long units = (static_cast<long long>(1 - count) * (1 << 22) - coarse) * (1 << 23) - fine;
+    const long long units = static_cast<long long>((1 << 22) - coarse) * (1 << 23) - fine;
     return __ll2float_rn(units) * (1.f / kFine);
 }
 template <bool REST>
