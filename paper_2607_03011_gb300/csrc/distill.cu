@@ -56,7 +56,7 @@ constexpr int stream_ctas(int threads) { return threads == 64 ? 14 : threads == 
 // Entries of a share whose marks (of the list's tokens) are kept apart.
 constexpr uint32_t marks_of(int threads) { return threads <= 128 ? 16384 : 65536; }
 constexpr uint64_t kLostNs = 20000000;  // the limit of a wait for a row whose copy is not started (DistillArgs::lost)
-constexpr float kSmallRest = 0.0625f;
+constexpr float kSmallRest = 0.0625f;  // rests of a teacher below this are made good (left_of)
 // Vectors per thread of the gradient by itself: 8192 x 128000 bf16 657 us (the copy rate allows 628); 16 667, 8 769, 4 869 (a list for
 // every span).
 constexpr int kSpan = 32;
